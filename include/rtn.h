@@ -431,6 +431,68 @@ int rtn_epilogue_reparam_conv2d(const int32_t *acc, int64_t Nb, int64_t C, int64
                                 rtn_pad_mode pad_mode, const rtn_epilogue *ep, float *y_out,
                                 void *stream);
 
+/* ---- Ternary linear layer of 16-bit activations -------------------------------------------------
+ * The weight-only ternary layer as language models use it: activations in bfloat16 or float16, ternary weights
+ * alpha_w * t_w, and bias, activation and residual behind the product,
+ *   z[m][n] = alpha_w[n] * sum_k x[m][k] * t_w[n][k] + bias[n]
+ *   y[m][n] = act(z[m][n]) + residual[m][n]
+ * from one token (m) to many.  The products with -1, 0, +1 are exact, the sums are held in fp32 and y is rounded
+ * once; the order of the sums follows from the sizes, so the same arguments give the same bits.
+ * dt: RTN_BF16 or RTN_F16, the type of x, bias, residual and y.  x, residual and y are row-major with their rows ldx, ldr,
+ * ldy elements apart (at least the row's length); alpha_w: RTN_SCALAR (host) or RTN_VECTOR (device, [N]); bias and residual may
+ * be NULL.  y may be the residual (the same rows at the same pitch), and may not overlap anything else.
+ * act: RTN_ACT_NONE, RTN_ACT_RELU, RTN_ACT_GELU (z times the normal distribution function), RTN_ACT_SILU (z / (1 + exp(-z))).
+ * M = 0 is a call with nothing to do.  N, K <= 2^21, pitches <= 2^31, 2-byte aligned; rows of 16-byte units
+ * (pointer 16-byte aligned, pitch and row length multiples of 8 elements) are read and written fastest.
+ * workspace: rtn_linear_workspace_bytes() of the same x, ldx, M, K and z_ckpt != NULL, 0 wherever rows can be read where they
+ * lie; 16-byte aligned.
+ * z_ckpt (nullable): receives the 8-bit checkpoint (below) of z, for rtn_linear_backward: rtn_checkpoint_bytes(M, N) bytes. */
+typedef enum { RTN_BF16 = 0, RTN_F16 = 1, RTN_F32 = 2 } rtn_dtype;
+typedef enum { RTN_ACT_NONE = 0, RTN_ACT_RELU = 1, RTN_ACT_GELU = 2, RTN_ACT_SILU = 3 } rtn_act;
+
+/* Weight side, once for a model that answers and once a step in training: ternary codes [N][Kpad] in any format, as
+ * rtn_ternarize_pack writes them, to two bits a weight in the order the matrix instruction takes.  prepared (rows n, for
+ * rtn_linear): rtn_linear_prepared_bytes(N, K) bytes; prepared_t (rows k, for rtn_linear_backward's dx):
+ * rtn_linear_prepared_bytes(K, N).  Either may be NULL, not both.  16-byte aligned.  The layout belongs to the
+ * build of the library: prepare again, do not store the buffers. */
+size_t rtn_linear_prepared_bytes(int64_t N, int64_t K);
+int rtn_linear_prepare(rtn_code_format fmt, const void *w_codes, int64_t N, int64_t K, void *prepared,
+                       size_t prepared_bytes, void *prepared_t, size_t prepared_t_bytes, void *stream);
+size_t rtn_linear_workspace_bytes(const void *x, int64_t ldx, int64_t M, int64_t K, int keeps_z);
+int rtn_linear(rtn_dtype dt, const void *x, int64_t ldx, const void *prepared, int64_t M, int64_t N, int64_t K,
+               const float *alpha_w, rtn_gran gran_w, const void *bias, rtn_act act, const void *residual, int64_t ldr,
+               void *y, int64_t ldy, void *z_ckpt, size_t z_ckpt_bytes, void *workspace, size_t workspace_bytes,
+               void *stream);
+
+/* ---- Activations kept in 8 bits for the backward pass --------------------------------------------
+ * Of a [M][C] tensor v of type dt, groups of 32 consecutive tokens of one channel share a power of two 2^e, and a value is
+ * kept as q = rint(v / 2^e) (ties to even), |q| <= 127:
+ *   e = floor(log2(max |v|)) - 6, one more where max |v| / 2^e would round to 128; at least -126 (RTN_BF16) or -24 (RTN_F16)
+ *   and at most 121 or 9 (64 times the next power would be infinite in dt; |v| / 2^e beyond 127 there is kept as 127)
+ * so the error is at most 2^e / 2 (2^e there), 1/128 of the group's largest magnitude, and what is read back, q 2^e, is exact in dt.  A
+ * group that holds an infinity or NaN reads back as NaN.  rtn_checkpoint_bytes(M, C) = 264 bytes per 32 tokens and 8 channels,
+ * 16-byte aligned; the layout belongs to the build of the library.  M = 0: nothing to do. */
+size_t rtn_checkpoint_bytes(int64_t M, int64_t C);
+int rtn_checkpoint_pack(rtn_dtype dt, const void *x, int64_t ldx, int64_t M, int64_t C, void *ckpt, size_t ckpt_bytes,
+                        void *stream);
+int rtn_checkpoint_unpack(rtn_dtype dt, const void *ckpt, size_t ckpt_bytes, int64_t M, int64_t C, void *y, int64_t ldy,
+                          void *stream);
+
+/* Gradients of the layer from dy = dL/dy [M][N] (rows lddy apart), with z^ and x^ read back from their checkpoints:
+ *   dz = dy * act'(z^)                       (act' of a relu at 0 is 0)
+ *   dx[m][k] = sum_n dz[m][n] alpha_w[n] t_w[n][k]     dw[n][k] = sum_m dz[m][n] x^[m][k]     dbias[n] = sum_m dz[m][n]
+ * dw is the gradient of the reparameterized weights alpha_w * t_w: as RTN_F32 it is what rtn_weight_backward takes.  The
+ * gradient of the residual is dy.  dx (rows lddx apart) and dbias have type dt, dw type dw_type (dt or RTN_F32) in dense rows;
+ * each may be NULL, not all.  dz and dz * alpha_w are rounded to dt once, on their way into the products; the sums and dbias'
+ * terms are fp32.  The sums' order follows from the sizes (no atomics): the same arguments give the same bits.
+ * x_ckpt is needed for dw, prepared_t for dx, z_ckpt unless act is RTN_ACT_NONE.  M = 0 writes zeros to dw and dbias.
+ * dx may not overlap dy.  workspace: rtn_linear_backward_workspace_bytes(M, N, K), 16-byte aligned. */
+size_t rtn_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int rtn_linear_backward(rtn_dtype dt, const void *dy, int64_t lddy, const void *x_ckpt, size_t x_ckpt_bytes,
+                        const void *z_ckpt, size_t z_ckpt_bytes, rtn_act act, const void *prepared_t, int64_t M, int64_t N,
+                        int64_t K, const float *alpha_w, rtn_gran gran_w, void *dx, int64_t lddx, void *dw,
+                        rtn_dtype dw_type, void *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -22,6 +22,8 @@ RTN_SCALAR, RTN_VECTOR = 0, 1
 RTN_ROWS_K_CONTIG, RTN_NCHW = 0, 1
 RTN_PAD_TRUE_ZERO, RTN_PAD_CODE_ZERO = 0, 1
 RTN_PATH_AUTO, RTN_PATH_MFMA_I8, RTN_PATH_POPC, RTN_PATH_MFMA_FP4 = 0, 1, 2, 3
+RTN_BF16, RTN_F16, RTN_F32 = 0, 1, 2
+RTN_ACT_NONE, RTN_ACT_RELU, RTN_ACT_GELU, RTN_ACT_SILU = 0, 1, 2, 3
 
 EXPORTS = ["rtn_status_string", "rtn_last_hip_error", "rtn_num_tile_configs", "rtn_set_tile_config", "rtn_padded_k", "rtn_padded_k_format",
            "rtn_codes_bytes",
@@ -36,7 +38,10 @@ EXPORTS = ["rtn_status_string", "rtn_last_hip_error", "rtn_num_tile_configs", "r
            "rtn_activation_backward_static_max_n", "rtn_activation_backward_static", "rtn_weight_backward",
            "rtn_epilogue_reparam",
            "rtn_epilogue_reparam_conv2d", "rtn_quaternary_pack", "rtn_quaternary_gemm",
-           "rtn_ternary_depthwise_conv2d"]
+           "rtn_ternary_depthwise_conv2d",
+           "rtn_linear_prepared_bytes", "rtn_linear_prepare", "rtn_linear_workspace_bytes", "rtn_linear",
+           "rtn_checkpoint_bytes", "rtn_checkpoint_pack", "rtn_checkpoint_unpack",
+           "rtn_linear_backward_workspace_bytes", "rtn_linear_backward"]
 
 
 class RtnEpilogue(C.Structure):
@@ -133,6 +138,25 @@ def lib():
         L.rtn_epilogue_reparam_conv2d.restype = ci
         L.rtn_epilogue_reparam_conv2d.argtypes = [vp, i64, i64, i64, i64, i64, ci, ci, ci, ci, ci, vp,
                                                   vp, vp]
+        sz = C.c_size_t
+        L.rtn_linear_prepared_bytes.restype = sz
+        L.rtn_linear_prepared_bytes.argtypes = [i64, i64]
+        L.rtn_linear_prepare.restype = ci
+        L.rtn_linear_prepare.argtypes = [ci, vp, i64, i64, vp, sz, vp, sz, vp]
+        L.rtn_linear_workspace_bytes.restype = sz
+        L.rtn_linear_workspace_bytes.argtypes = [vp, i64, i64, i64, ci]
+        L.rtn_linear.restype = ci
+        L.rtn_linear.argtypes = [ci, vp, i64, vp, i64, i64, i64, vp, ci, vp, ci, vp, i64, vp, i64, vp, sz, vp, sz, vp]
+        L.rtn_checkpoint_bytes.restype = sz
+        L.rtn_checkpoint_bytes.argtypes = [i64, i64]
+        L.rtn_checkpoint_pack.restype = ci
+        L.rtn_checkpoint_pack.argtypes = [ci, vp, i64, i64, i64, vp, sz, vp]
+        L.rtn_checkpoint_unpack.restype = ci
+        L.rtn_checkpoint_unpack.argtypes = [ci, vp, sz, i64, i64, vp, i64, vp]
+        L.rtn_linear_backward_workspace_bytes.restype = sz
+        L.rtn_linear_backward_workspace_bytes.argtypes = [i64, i64, i64]
+        L.rtn_linear_backward.restype = ci
+        L.rtn_linear_backward.argtypes = [ci, vp, i64, vp, sz, vp, sz, ci, vp, i64, i64, i64, vp, ci, vp, i64, vp, ci, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -505,3 +529,73 @@ def ternary_depthwise_conv2d(a_codes, w_codes, Nb, Cc, H, W, KH, KW, stride, pad
                              None if ep is None else ep.addr, y_out)
     _check(rc, "rtn_ternary_depthwise_conv2d")
     return acc_out, y_out
+
+
+def linear_prepare(w_codes, N, K, fmt=RTN_CODE_I8, backward=False):
+    """Weights of the ternary linear layer from codes [N, Kpad] in format fmt (as ternarize_pack returns them), in the order
+    its products take: the buffer linear() reads, and with backward=True also the one linear_backward() reads."""
+    _check_codes(w_codes, N, K, fmt, "w_codes")
+    dev = w_codes.device
+    w = torch.empty(lib().rtn_linear_prepared_bytes(N, K), dtype=torch.uint8, device=dev)
+    wt = torch.empty(lib().rtn_linear_prepared_bytes(K, N), dtype=torch.uint8, device=dev) if backward else None
+    rc = lib().rtn_linear_prepare(fmt, w_codes.data_ptr(), N, K, w.data_ptr(), w.numel(), None if wt is None else wt.data_ptr(),
+                                  0 if wt is None else wt.numel(), _stream())
+    _check(rc, "rtn_linear_prepare")
+    return (w, wt) if backward else w
+
+
+def linear(x, prepared, N, alpha_w, bias=None, act=RTN_ACT_NONE, residual=None, y_out=None, z_ckpt=None, workspace=None):
+    """y = act(alpha_w * (x t^T) + bias) + residual: x cuda bfloat16 / float16 [M, K] (rows may lie apart), prepared from
+    linear_prepare(), alpha_w a python float or cuda float32 [N], bias [N] and residual [M, N] in x's type.  z_ckpt, from
+    checkpoint_empty(M, N), receives the 8-bit checkpoint of the value before the activation.  Returns y [M, N]."""
+    M, K = x.shape
+    if y_out is None:
+        y_out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    if workspace is None:
+        need = lib().rtn_linear_workspace_bytes(x.data_ptr(), x.stride(0) if M > 1 else K, M, K, z_ckpt is not None)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    rc = _native().linear(x, prepared, M, N, K, alpha_w, bias, act, residual, y_out, z_ckpt, workspace)
+    _check(rc, "rtn_linear")
+    return y_out
+
+
+def checkpoint_empty(M, Cc, device="cuda"):
+    """A buffer for the 8-bit checkpoint of an [M, Cc] tensor."""
+    return torch.empty(lib().rtn_checkpoint_bytes(M, Cc), dtype=torch.uint8, device=device)
+
+
+def checkpoint_pack(x, ckpt=None):
+    """8-bit checkpoint of x, cuda bfloat16 / float16 [M, C] (rows may lie apart)."""
+    if ckpt is None:
+        ckpt = checkpoint_empty(x.shape[0], x.shape[1], x.device)
+    _check(_native().checkpoint(x, ckpt, True), "rtn_checkpoint_pack")
+    return ckpt
+
+
+def checkpoint_unpack(ckpt, M, Cc, dtype, out=None):
+    """What the checkpoint of an [M, Cc] tensor stands for, in bfloat16 or float16."""
+    if out is None:
+        out = torch.empty((M, Cc), dtype=dtype, device=ckpt.device)
+    _check(_native().checkpoint(out, ckpt, False), "rtn_checkpoint_unpack")
+    return out
+
+
+def linear_backward(dy, prepared_t, K, alpha_w, x_ckpt, act=RTN_ACT_NONE, z_ckpt=None, want_dx=True, want_dw=True, want_dbias=True,
+                    dw_dtype=None, dx=None, dw=None, dbias=None, workspace=None):
+    """Gradients of linear() from dy [M, N] (rows may lie apart) and the checkpoints of its input and, unless act is
+    RTN_ACT_NONE, of its value before the activation.  Returns (dx [M, K], dw [N, K], dbias [N]) or None in the place of
+    what is not wanted; dw, the gradient of alpha_w * t, is of dy's type or dw_dtype=torch.float32."""
+    M, N = dy.shape
+    dev = dy.device
+    if want_dx and dx is None:
+        dx = torch.empty((M, K), dtype=dy.dtype, device=dev)
+    if want_dw and dw is None:
+        dw = torch.empty((N, K), dtype=dw_dtype or dy.dtype, device=dev)
+    if want_dbias and dbias is None:
+        dbias = torch.empty(N, dtype=dy.dtype, device=dev)
+    if workspace is None:
+        workspace = torch.empty(lib().rtn_linear_backward_workspace_bytes(M, N, K), dtype=torch.uint8, device=dev)
+    rc = _native().linear_backward(dy, x_ckpt, z_ckpt, act, prepared_t, M, N, K, alpha_w, dx, dw, dbias, workspace)
+    _check(rc, "rtn_linear_backward")
+    return dx, dw, dbias

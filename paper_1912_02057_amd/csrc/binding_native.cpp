@@ -317,9 +317,122 @@ PyObject* weight_backward(PyObject*, Args a, Py_ssize_t n)
     });
 }
 
+// Row pitch of a [rows][len] device tensor of type `type` whose rows are dense; its data pointer.  None -> NULL.
+void* rows2d(PyObject* o, c10::ScalarType type, int64_t rows, int64_t len, const char* what, int64_t& ld)
+{
+    ld = len;
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = tensor(o, what);
+    if (!t.is_cuda() || t.scalar_type() != type || t.dim() != 2 || t.size(0) != rows || t.size(1) != len ||
+        (len > 1 && t.stride(1) != 1))
+        fail(PyExc_AssertionError, "%s: a device tensor of the documented type and shape, its rows dense, is required", what);
+    if (rows > 1) ld = t.stride(0);
+    return t.data_ptr();
+}
+rtn_dtype dtype(c10::ScalarType t, const char* what, bool f32 = false)
+{
+    if (t == c10::kBFloat16) return RTN_BF16;
+    if (t == c10::kHalf) return RTN_F16;
+    if (!f32 || t != c10::kFloat) fail(PyExc_AssertionError, "%s: bfloat16 or float16 is required", what);
+    return RTN_F32;
+}
+// A buffer of bytes on the device that holds at least `need`.
+void* bytes_of(PyObject* o, size_t need, const char* what)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = tensor(o, what);
+    if (!(t.is_cuda() && t.is_contiguous() && t.nbytes() >= need)) {
+        PyErr_Format(PyExc_ValueError, "%s: a device buffer of %zu bytes is required", what, need);
+        throw PyError();
+    }
+    return t.data_ptr();
+}
+
+// x, prepared, M, N, K, alpha_w, bias, act, residual, y, z_ckpt, workspace
+PyObject* linear(PyObject*, Args a, Py_ssize_t n)
+{
+    return call(12, n, [&] {
+        const c10::ScalarType type = tensor(a[0], "x").scalar_type();
+        const rtn_dtype dt = dtype(type, "x");
+        const int64_t M = integer(a[2]), N = integer(a[3]), K = integer(a[4]);
+        int64_t ldx, ldr, ldy;
+        const void* x = rows2d(a[0], type, M, K, "x", ldx);
+        const void* w = bytes_of(a[1], rtn_linear_prepared_bytes(N, K), "prepared");
+        const Gran al(a[5], "alpha_w");
+        if (al.gran == RTN_VECTOR && tensor(a[5], "alpha_w").numel() != N) fail(PyExc_AssertionError, "%s: one entry per output is required", "alpha_w");
+        const void* bias = dev(a[6], type, "bias");
+        if (bias && tensor(a[6], "bias").numel() != N) fail(PyExc_AssertionError, "%s: one entry per output is required", "bias");
+        const rtn_act act = (rtn_act)integer(a[7]);
+        const void* res = rows2d(a[8], type, M, N, "residual", ldr);
+        void* y = rows2d(a[9], type, M, N, "y_out", ldy);
+        void* z = bytes_of(a[10], rtn_checkpoint_bytes(M, N), "z_ckpt");
+        const size_t zb = raw_bytes(a[10], "z_ckpt");
+        void* ws = raw(a[11], "workspace");
+        const size_t wsb = raw_bytes(a[11], "workspace");
+        void* st = stream();
+        const Unlocked u;
+        return rtn_linear(dt, x, ldx, w, M, N, K, al.ptr, al.gran, bias, act, res, ldr, y, ldy, z, zb, ws, wsb, st);
+    });
+}
+
+// x, ckpt, pack (else unpack)
+PyObject* checkpoint(PyObject*, Args a, Py_ssize_t n)
+{
+    return call(3, n, [&] {
+        const at::Tensor& t = tensor(a[0], "x");
+        const rtn_dtype dt = dtype(t.scalar_type(), "x");
+        if (t.dim() != 2) fail(PyExc_AssertionError, "%s: a matrix is required", "x");
+        const int64_t M = t.size(0), C = t.size(1);
+        int64_t ld;
+        void* x = rows2d(a[0], t.scalar_type(), M, C, "x", ld);
+        void* k = bytes_of(a[1], rtn_checkpoint_bytes(M, C), "ckpt");
+        const size_t kb = raw_bytes(a[1], "ckpt");
+        const int pack = truth(a[2]);
+        void* st = stream();
+        const Unlocked u;
+        return pack ? rtn_checkpoint_pack(dt, x, ld, M, C, k, kb, st) : rtn_checkpoint_unpack(dt, k, kb, M, C, x, ld, st);
+    });
+}
+
+// dy, x_ckpt, z_ckpt, act, prepared_t, M, N, K, alpha_w, dx, dw, dbias, workspace
+PyObject* linear_backward(PyObject*, Args a, Py_ssize_t n)
+{
+    return call(13, n, [&] {
+        const c10::ScalarType type = tensor(a[0], "dy").scalar_type();
+        const rtn_dtype dt = dtype(type, "dy");
+        const int64_t M = integer(a[5]), N = integer(a[6]), K = integer(a[7]);
+        int64_t lddy, lddx, lddw;
+        const void* dy = rows2d(a[0], type, M, N, "dy", lddy);
+        const void* x = bytes_of(a[1], rtn_checkpoint_bytes(M, K), "x_ckpt");
+        const void* z = bytes_of(a[2], rtn_checkpoint_bytes(M, N), "z_ckpt");
+        const size_t xb = raw_bytes(a[1], "x_ckpt"), zb = raw_bytes(a[2], "z_ckpt");
+        const rtn_act act = (rtn_act)integer(a[3]);
+        const void* w = bytes_of(a[4], rtn_linear_prepared_bytes(K, N), "prepared_t");
+        const Gran al(a[8], "alpha_w");
+        if (al.gran == RTN_VECTOR && tensor(a[8], "alpha_w").numel() != N) fail(PyExc_AssertionError, "%s: one entry per output is required", "alpha_w");
+        void* dx = rows2d(a[9], type, M, K, "dx", lddx);
+        void* dw = nullptr;
+        rtn_dtype dwt = dt;
+        if (a[10] != Py_None) {
+            const c10::ScalarType t = tensor(a[10], "dw").scalar_type();
+            dwt = dtype(t, "dw", true);
+            dw = rows2d(a[10], t, N, K, "dw", lddw);
+            if (lddw != K) fail(PyExc_AssertionError, "%s: a contiguous tensor is required", "dw");
+        }
+        void* db = dev(a[11], type, "dbias");
+        if (db && tensor(a[11], "dbias").numel() != N) fail(PyExc_AssertionError, "%s: one entry per output is required", "dbias");
+        void* ws = raw(a[12], "workspace");
+        const size_t wsb = raw_bytes(a[12], "workspace");
+        void* st = stream();
+        const Unlocked u;
+        return rtn_linear_backward(dt, dy, lddy, x, xb, z, zb, act, w, M, N, K, al.ptr, al.gran, dx, lddx, dw, dwt, db, ws, wsb, st);
+    });
+}
+
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(pack), FAST(gemm), FAST(conv2d), FAST(conv2d_ternarize), FAST(depthwise), FAST(weight_gemm),
-                         FAST(weight_conv2d_prepared), FAST(activation_backward), FAST(weight_backward), {nullptr, nullptr, 0, nullptr}};
+                         FAST(weight_conv2d_prepared), FAST(activation_backward), FAST(weight_backward),
+                         FAST(linear), FAST(checkpoint), FAST(linear_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,328 @@
+// Activations kept in 8 bits between the forward and the backward pass (CkptShape): into 8 bits, back, and into the operand
+// order of the weight gradient's product, there together with the gradient that it meets.
+//
+// All of them are one pass over memory.  A lane has 8 tokens of 8 channels: 8 rows of 16 bytes of a 16-bit tensor (16 lanes
+// beside each other read 256 bytes of a row), 64 bytes in a row of a checkpoint, and 16 bytes per channel of an operand.
+#include "linear_math.h"
+#include "rtn_kernels.h"
+
+namespace rtn {
+
+namespace {
+
+struct Micro {  // what a lane owns
+    int64_t mb, c;  // block of 32 tokens; its first channel
+    int t0;         // first of its 8 tokens in the block
+};
+// Wave `unit` of a tensor of cb blocks of 8 channels: 32 tokens x 128 channels.
+__device__ __forceinline__ Micro micro_of(int64_t mb, int64_t strip)
+{
+    const int lane = threadIdx.x & 63;
+    return {mb, (strip * 16 + (lane & 15)) * 8, (lane >> 4) * 8};
+}
+
+// 8 channels of a row as they are; zeros past the end
+__device__ __forceinline__ u32x4 load_row(const unsigned short* x, int64_t ld, int64_t m, int64_t M, int64_t c, int64_t C, bool vec)
+{
+    u32x4 v = {0, 0, 0, 0};
+    if (m >= M) return v;
+    const unsigned short* r = x + m * ld + c;
+    if (vec && c + 8 <= C) return *(const u32x4*)r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c + i < C) v[i >> 1] |= (unsigned)r[i] << (16 * (i & 1));
+    return v;
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void k_ckpt_pack(CkptArgs a, int strips, int vec)
+{
+    const CkptShape cs(a.M, a.C);
+    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (unit >= cs.tb * strips) return;
+    const int64_t mb = unit / strips;
+    const Micro u = micro_of(mb, unit - mb * strips);
+    u32x4 v[8];
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+        v[t] = load_row((const unsigned short*)a.x, a.ld, mb * 32 + u.t0 + t, a.M, u.c, a.C, vec);
+    unsigned ex[2] = {0, 0};
+    float inv[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        unsigned am = 0;  // as bits: a NaN is larger than an infinity, and that than any number
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            const unsigned b = (v[t][i >> 1] >> (16 * (i & 1))) & 0x7fffu;
+            am = b > am ? b : am;
+        }
+#pragma unroll
+        for (int d = 16; d < 64; d *= 2) {
+            const unsigned o = (unsigned)__shfl_xor((int)am, d);
+            am = o > am ? o : am;
+        }
+        const int e = ckpt_exponent<T>(T::to_float((unsigned short)am));
+        ex[i >> 2] |= (unsigned)e << (8 * (i & 3));
+        inv[i] = ckpt_inverse(e);
+    }
+    if (u.c >= a.C) return;
+    const int64_t blk = mb * cs.cb + (u.c >> 3);
+    unsigned w[16];
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            unsigned r = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int c = 4 * q + i;
+                r |= ckpt_code(half_of<T>(v[t][c >> 1], c & 1), inv[c]) << (8 * i);
+            }
+            w[t * 2 + q] = r;
+        }
+    uint4* out = (uint4*)(a.ckpt + blk * 256 + u.t0 * 8);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    if (u.t0 == 0) *(uint2*)(a.ckpt + cs.codes() + blk * 8) = make_uint2(ex[0], ex[1]);
+}
+
+// The 8 tokens x 8 channels of a lane of a checkpoint: codes and scales.
+struct MicroCkpt {
+    uint4 q[4];
+    uint2 e;
+    __device__ __forceinline__ void load(const int8_t* ckpt, const CkptShape& cs, const Micro& u)
+    {
+        const int64_t blk = u.mb * cs.cb + (u.c >> 3);
+        const uint4* p = (const uint4*)(ckpt + blk * 256 + u.t0 * 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = p[i];
+        e = *(const uint2*)(ckpt + cs.codes() + blk * 8);
+    }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = make_uint4(0, 0, 0, 0);
+        e = make_uint2(0, 0);
+    }
+    __device__ __forceinline__ float scale(int i) const { return ckpt_scale((int)((i < 4 ? e.x : e.y) >> (8 * (i & 3)) & 255)); }
+    // channel i of token t, to be multiplied by scale(i)
+    __device__ __forceinline__ float code(int t, int i) const
+    {
+        const uint4& r = q[t >> 1];
+        const unsigned w = t & 1 ? (i < 4 ? r.z : r.w) : (i < 4 ? r.x : r.y);
+        return (float)((int)(w << (24 - 8 * (i & 3))) >> 24);
+    }
+};
+
+template <class T>
+__global__ __launch_bounds__(256) void k_ckpt_unpack(CkptArgs a, int strips, int vec)
+{
+    const CkptShape cs(a.M, a.C);
+    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (unit >= cs.tb * strips) return;
+    const int64_t mb = unit / strips;
+    const Micro u = micro_of(mb, unit - mb * strips);
+    if (u.c >= a.C) return;
+    MicroCkpt k;
+    k.load(a.ckpt, cs, u);
+    float s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = k.scale(i);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+        const int64_t m = mb * 32 + u.t0 + t;
+        if (m >= a.M) break;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = k.code(t, i) * s[i];
+        unsigned short* y = (unsigned short*)a.y + m * a.ld + u.c;
+        if (vec && u.c + 8 <= a.C) {
+            *(u32x4*)y = u32x4{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (u.c + i < a.C) y[i] = T::from_float(v[i]);
+        }
+    }
+}
+
+// 8 tokens x 8 channels (values of type T in v[channel][token pair]) -> the operand order of the weight gradient.
+__device__ __forceinline__ void store_operand(char* out, int64_t blocks, const Micro& u, const u32x4 (&v)[8])
+{
+    char* p = out + operand_offset(u.mb, u.c >> 5, blocks) + (u.t0 >> 4) * 1024 + ((u.t0 >> 3 & 1) * 32 + (int)(u.c & 31)) * 16;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) *(u32x4*)(p + i * 16) = v[i];
+}
+
+template <class T, int ACT>
+__device__ __forceinline__ void grad_unit(const GradArgs& a, int64_t tb0, int64_t strip)
+{
+    const int64_t nb = (a.N + 31) / 32, tbs = (a.M + 31) / 32;
+    const CkptShape cs(a.M, a.N);
+    float sum[8], al[8];
+    const int64_t c = micro_of(0, strip).c;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        sum[i] = 0.f;
+        al[i] = c + i < a.N ? (a.alpha.ptr ? a.alpha.ptr[c + i] : a.alpha.s) : 0.f;
+    }
+    for (int64_t mb = tb0; mb < tb0 + a.per && mb < tbs; ++mb) {
+        const Micro u = micro_of(mb, strip);
+        u32x4 v[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) v[t] = load_row((const unsigned short*)a.dy, a.lddy, mb * 32 + u.t0 + t, a.M, u.c, a.N, a.vec_dy);
+        MicroCkpt k;
+        if constexpr (ACT != kActNone) {
+            if (u.c < a.N)
+                k.load(a.zq, cs, u);
+            else
+                k.zero();
+        }
+        u32x4 o[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            float d[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                d[i] = half_of<T>(v[t][i >> 1], i & 1);
+                if constexpr (ACT != kActNone) {
+                    // a group that held an infinity or NaN makes the slopes of its real tokens NaN, not those past the end
+                    const float g = d[i] * act_slope<ACT>(k.code(t, i) * k.scale(i));
+                    d[i] = mb * 32 + u.t0 + t < a.M ? g : 0.f;
+                }
+                sum[i] += d[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const unsigned b = ACT == kActNone ? v[t][i >> 1] >> (16 * (i & 1)) & 0xffffu : (unsigned)T::from_float(d[i]);
+                o[i][t >> 1] = t & 1 ? o[i][t >> 1] | b << 16 : b;
+            }
+            const int64_t m = mb * 32 + u.t0 + t;
+            if (a.dza && m < a.M && u.c < a.lda)
+                *(u32x4*)((unsigned short*)a.dza + m * a.lda + u.c) =
+                    u32x4{pack2<T>(d[0] * al[0], d[1] * al[1]), pack2<T>(d[2] * al[2], d[3] * al[3]), pack2<T>(d[4] * al[4], d[5] * al[5]),
+                          pack2<T>(d[6] * al[6], d[7] * al[7])};
+        }
+        if (a.dzt && u.c < nb * 32) store_operand(a.dzt, nb, u, o);
+    }
+    if (!a.part) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        sum[i] += __shfl_xor(sum[i], 16);
+        sum[i] += __shfl_xor(sum[i], 32);
+    }
+    const int64_t row = tb0 / a.per;
+    if ((threadIdx.x & 63) < 16)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i < a.N) a.part[row * a.N + c + i] = sum[i];
+}
+
+// The gradient before the activation, dz = dy act'(z^), as the two products take it: times alpha, row-major (dx), and in
+// operand order (dw); its sums over a run of tokens (dbias); and the layer's input from its checkpoint in operand order.
+template <class T>
+__global__ __launch_bounds__(256) void k_linear_grad(GradArgs a)
+{
+    int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (unit < a.dz_units) {
+        const int64_t run = unit / a.dz_strips, strip = unit - run * a.dz_strips, tb0 = run * a.per;
+        if (a.act == kActNone)
+            grad_unit<T, kActNone>(a, tb0, strip);
+        else if (a.act == kActRelu)
+            grad_unit<T, kActRelu>(a, tb0, strip);
+        else if (a.act == kActGelu)
+            grad_unit<T, kActGelu>(a, tb0, strip);
+        else
+            grad_unit<T, kActSilu>(a, tb0, strip);
+        return;
+    }
+    unit -= a.dz_units;
+    if (unit >= a.x_units) return;
+    const int64_t mb = unit / a.x_strips;
+    const Micro u = micro_of(mb, unit - mb * a.x_strips);
+    const int64_t kb = (a.K + 31) / 32;
+    if (u.c >= kb * 32) return;
+    const CkptShape cs(a.M, a.K);
+    MicroCkpt k;
+    if (u.c < a.K)
+        k.load(a.xq, cs, u);
+    else
+        k.zero();
+    u32x4 o[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float s = k.scale(i);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int64_t m = mb * 32 + u.t0 + 2 * t;
+            o[i][t] = pack2<T>(m < a.M ? k.code(2 * t, i) * s : 0.f, m + 1 < a.M ? k.code(2 * t + 1, i) * s : 0.f);
+        }
+    }
+    store_operand(a.xt, kb, u, o);
+}
+
+// dbias[n] = sum of the runs' partial sums, in their order
+template <class T>
+__global__ __launch_bounds__(64) void k_bias_sum(const float* part, int64_t runs, int64_t N, unsigned short* out)
+{
+    const int64_t n = (int64_t)blockIdx.x * 64 + threadIdx.x;
+    if (n >= N) return;
+    float s = 0.f;
+    for (int64_t r = 0; r < runs; ++r) s += part[r * N + n];
+    out[n] = T::from_float(s);
+}
+
+bool rows_of_16(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
+
+}  // namespace
+
+hipError_t launch_checkpoint_pack(const CkptArgs& a, hipStream_t st)
+{
+    const int64_t strips = (a.C + 127) / 128, blocks = ((a.M + 31) / 32 * strips + 3) / 4;
+    const int vec = rows_of_16(a.x, a.ld);
+    if (a.f16)
+        k_ckpt_pack<F16><<<(unsigned)blocks, 256, 0, st>>>(a, (int)strips, vec);
+    else
+        k_ckpt_pack<BF16><<<(unsigned)blocks, 256, 0, st>>>(a, (int)strips, vec);
+    return hipGetLastError();
+}
+
+hipError_t launch_checkpoint_unpack(const CkptArgs& a, hipStream_t st)
+{
+    const int64_t strips = (a.C + 127) / 128, blocks = ((a.M + 31) / 32 * strips + 3) / 4;
+    const int vec = rows_of_16(a.y, a.ld);
+    if (a.f16)
+        k_ckpt_unpack<F16><<<(unsigned)blocks, 256, 0, st>>>(a, (int)strips, vec);
+    else
+        k_ckpt_unpack<BF16><<<(unsigned)blocks, 256, 0, st>>>(a, (int)strips, vec);
+    return hipGetLastError();
+}
+
+hipError_t launch_linear_grad(GradArgs a, int f16, hipStream_t st)
+{
+    const int64_t tbs = (a.M + 31) / 32;
+    a.dz_strips = a.dzt || a.dza || a.part ? (a.N + 127) / 128 : 0;
+    a.dz_units = (tbs + a.per - 1) / a.per * a.dz_strips;
+    a.x_strips = a.xt ? (a.K + 127) / 128 : 0;
+    a.x_units = tbs * a.x_strips;
+    a.vec_dy = rows_of_16(a.dy, a.lddy);
+    const int64_t blocks = (a.dz_units + a.x_units + 3) / 4;
+    if (!blocks) return hipSuccess;
+    if (f16)
+        k_linear_grad<F16><<<(unsigned)blocks, 256, 0, st>>>(a);
+    else
+        k_linear_grad<BF16><<<(unsigned)blocks, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_bias_sum(const float* part, int64_t runs, int64_t N, void* out, int f16, hipStream_t st)
+{
+    const unsigned blocks = (unsigned)((N + 63) / 64);
+    if (f16)
+        k_bias_sum<F16><<<blocks, 64, 0, st>>>(part, runs, N, (unsigned short*)out);
+    else
+        k_bias_sum<BF16><<<blocks, 64, 0, st>>>(part, runs, N, (unsigned short*)out);
+    return hipGetLastError();
+}
+
+}  // namespace rtn

@@ -1,0 +1,285 @@
+// Gradients of the ternary linear layer from 8-bit checkpoints of its input and of the value before its activation.
+//
+//   dz = dy act'(z^)     dbias = sum_m dz     dx = (dz alpha) t     dw = dz^T x^
+//
+// One pass (k_linear_grad) writes dz as each product takes it; dx is the forward product on the transposed prepared weights;
+// dw, which contracts over tokens, has a kernel of its own here: both operands lie in the order the matrix instruction takes
+// them, so its loads and fragment reads are consecutive.
+#include "linear_math.h"
+#include "tmm_kernel.h"
+
+namespace rtn {
+
+namespace {
+
+struct WgParams {
+    const char *x, *d;  // x^ and dz in operand order
+    int N, K, nk;       // nk: blocks of 32 tokens
+    int64_t xpitch, dpitch;  // bytes from one block of tokens to the next
+    int tilesN, ntiles, band_tiles;
+    FastDiv div_band, div_lastband;
+    void* dw;
+    int vec;
+};
+
+template <int BN, int BK, int NS>
+struct WgTile {
+    static constexpr int WN = BN / 2, WK = BK / 2, TN = WN / 32, TK = WK / 32, NM = TN * TK;
+    static constexpr int XBYTES = BK * 64, STAGE = XBYTES + BN * 64, XDMA = BK / 64, DDMA = BN / 64, DPS = XDMA + DDMA;  // 1 KiB / wave
+    static constexpr int ZPITCH = WK * 4 + 16, ZBYTES = 32 * ZPITCH;
+    static constexpr int LDS = NS * STAGE > 4 * ZBYTES ? NS * STAGE : 4 * ZBYTES;
+};
+
+// A block of 4 waves (2 x 2) owns BN x BK of dw; a ring of NS stages of 32 tokens, a barrier per stage before the second
+// of its two 16-token slices, fragments read one slice ahead.
+template <class T, int BN, int BK, int NS, bool F32>
+__global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgParams p)
+{
+    using L = WgTile<BN, BK, NS>;
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wn = wave >> 1, wk = wave & 1, l32 = lane & 31, h = lane >> 5;
+    int tn, tk;
+    {
+        const int chunk = (int)(gridDim.x >> 3), bid = (int)(blockIdx.x & 7) * chunk + (int)(blockIdx.x >> 3);
+        if (bid >= p.ntiles) return;
+        band_tile(bid, p.tilesN, p.band_tiles, [&](int n) { return (int)fastdiv((uint32_t)n, p.div_band); },
+                  [&](int n) { return (int)fastdiv((uint32_t)n, p.div_lastband); }, tn, tk);
+    }
+    const int n0 = tn * BN, k0 = tk * BK, nk = p.nk;
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+    const char* xg = p.x + (int64_t)(k0 / 32) * 2048 + wave * L::XDMA * 1024;
+    const char* dg = p.d + (int64_t)(n0 / 32) * 2048 + wave * L::DDMA * 1024;
+    auto issue = [&](int step, int slot) {
+        const unsigned base = lds0 + (unsigned)(slot * L::STAGE);
+        const int8_t* xs = uniform_ptr((const int8_t*)xg + step * p.xpitch);
+        const int8_t* ds = uniform_ptr((const int8_t*)dg + step * p.dpitch);
+        asm volatile("s_nop 4" : "+s"(xs), "+s"(ds));  // five wait states: they may just have left vector registers
+        for_each_index(
+            [&](auto index) {
+                constexpr int i = decltype(index)::value;
+                dma16_base<i * 1024>(xs, (unsigned)(lane * 16 + i * 1024), base + (unsigned)(wave * L::XDMA * 1024));
+            },
+            std::make_integer_sequence<int, L::XDMA>{});
+        for_each_index(
+            [&](auto index) {
+                constexpr int i = decltype(index)::value;
+                dma16_base<L::XBYTES + i * 1024>(ds, (unsigned)(lane * 16 + i * 1024), base + (unsigned)(wave * L::DDMA * 1024));
+            },
+            std::make_integer_sequence<int, L::DDMA>{});
+    };
+
+    f32x16 acc[L::TK][L::TN];
+#pragma unroll
+    for (int i = 0; i < L::TK; ++i)
+#pragma unroll
+        for (int j = 0; j < L::TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    u32x4 xf[2][L::TK], df[2][L::TN];
+    const int xbase = wk * L::TK * 2048 + lane * 16, dbase = L::XBYTES + wn * L::TN * 2048 + lane * 16;
+
+    int issued = 0;
+    for (; issued < NS - 1 && issued < nk; ++issued) issue(issued, issued);
+    wait_groups<L::DPS>(issued - 1);
+    block_barrier();
+    int slot = 0;
+#pragma unroll
+    for (int i = 0; i < L::TK; ++i) xf[0][i] = *(const u32x4*)(smem + xbase + i * 2048);
+#pragma unroll
+    for (int i = 0; i < L::TN; ++i) df[0][i] = *(const u32x4*)(smem + dbase + i * 2048);
+
+    for (int step = 0; step < nk; ++step) {
+        const int next = slot + 1 == NS ? 0 : slot + 1;
+        auto slice = [&](auto index) {
+            constexpr int j = decltype(index)::value, cur = j, nxt = j ^ 1;
+            if constexpr (j == 1) {
+                // step + 1 has landed for this wave, then for all; and all are done with step - 1, whose slot is filled again
+                const int later = nk - 2 - step;
+                wait_groups<L::DPS>(later < NS - 3 ? later : NS - 3);
+                block_barrier();
+                if (issued < nk) {
+                    issue(issued, slot == 0 ? NS - 1 : slot - 1);
+                    ++issued;
+                }
+            }
+            const char* stage = smem + (j == 1 ? next : slot) * L::STAGE + (j == 0 ? 1024 : 0);
+            for_each_index(
+                [&](auto mi) {
+                    constexpr int n = decltype(mi)::value, i = n / L::TN, k = n % L::TN;
+                    // the next slice's fragments, early in this one's products
+                    constexpr int NF = L::TK + L::TN, PER = (NF + L::NM - 1) / L::NM;
+#pragma unroll
+                    for (int f = n * PER; f < (n + 1) * PER && f < NF; ++f) {
+                        if (f < L::TK)
+                            xf[nxt][f] = *(const u32x4*)(stage + xbase + f * 2048);
+                        else
+                            df[nxt][f - L::TK] = *(const u32x4*)(stage + dbase + (f - L::TK) * 2048);
+                    }
+                    acc[i][k] = T::mfma(xf[cur][i], df[cur][k], acc[i][k]);
+                    if constexpr (L::NM > 2) __builtin_amdgcn_sched_barrier(0);
+                },
+                std::make_integer_sequence<int, L::NM>{});
+        };
+        slice(std::integral_constant<int, 0>{});
+        slice(std::integral_constant<int, 1>{});
+        slot = next;
+    }
+
+    __syncthreads();
+    constexpr int CL = L::WK / 8, TPL = CL / 2;
+    char* zs = smem + wave * L::ZBYTES;
+    const int k8 = k0 + wk * L::WK + (lane % CL) * 8, t0 = (lane / CL) * TPL;
+#pragma unroll 1
+    for (int k = 0; k < L::TN; ++k) {
+        auto put = [&](auto index) {
+            constexpr int kk = decltype(index)::value;
+            if (kk != k) return;
+#pragma unroll
+            for (int i = 0; i < L::TK; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *(float4*)(zs + l32 * L::ZPITCH + (i * 32 + q * 8 + h * 4) * 4) =
+                        make_float4(acc[i][kk][4 * q], acc[i][kk][4 * q + 1], acc[i][kk][4 * q + 2], acc[i][kk][4 * q + 3]);
+        };
+        for_each_index(put, std::make_integer_sequence<int, L::TN>{});
+        wait_lgkm0();
+        const int nt = n0 + wn * L::WN + k * 32;
+        if (nt >= p.N || k8 >= p.K) continue;
+#pragma unroll
+        for (int t = 0; t < TPL; ++t) {
+            const int n = nt + t0 + t;
+            const float* row = (const float*)(zs + (t0 + t) * L::ZPITCH + (lane % CL) * 32);
+            const float4 a = *(const float4*)row, b = *(const float4*)(row + 4);
+            if (n >= p.N) continue;
+            const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            if constexpr (F32) {
+                float* o = (float*)p.dw + (int64_t)n * p.K + k8;
+                if (p.vec && k8 + 8 <= p.K) {
+                    *(float4*)o = a;
+                    *(float4*)(o + 4) = b;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (k8 + i < p.K) o[i] = v[i];
+                }
+            } else {
+                unsigned short* o = (unsigned short*)p.dw + (int64_t)n * p.K + k8;
+                if (p.vec && k8 + 8 <= p.K) {
+                    *(u32x4*)o = u32x4{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])};
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (k8 + i < p.K) o[i] = T::from_float(v[i]);
+                }
+            }
+        }
+    }
+}
+
+template <class T, int BN, int BK, int NS, bool F32>
+hipError_t run_tile(WgParams& p, hipStream_t st)
+{
+    using L = WgTile<BN, BK, NS>;
+    p.tilesN = (p.N + BN - 1) / BN;
+    const int tilesK = (p.K + BK - 1) / BK;
+    const int64_t nt = (int64_t)p.tilesN * tilesK;
+    if (nt > 0x7fffff00) return hipErrorInvalidValue;
+    p.ntiles = (int)nt;
+    p.band_tiles = 8 * tilesK;
+    p.div_band = make_fastdiv((uint32_t)p.band_tiles);
+    p.div_lastband = make_fastdiv((uint32_t)(p.tilesN % 8 ? p.tilesN % 8 : 8));
+    static LdsLimit limit;
+    const hipError_t e = limit.raise((const void*)&k_wgrad<T, BN, BK, NS, F32>, L::LDS);
+    if (e != hipSuccess) return e;
+    k_wgrad<T, BN, BK, NS, F32><<<(unsigned)((nt + 7) / 8 * 8), 256, L::LDS, st>>>(p);
+    return hipGetLastError();
+}
+
+template <class T, bool F32>
+hipError_t run(WgParams& p, hipStream_t st)
+{
+    const int64_t t256 = (int64_t)((p.N + 255) / 256) * ((p.K + 255) / 256), t128 = (int64_t)((p.N + 127) / 128) * ((p.K + 127) / 128);
+    if (t256 >= 192) return run_tile<T, 256, 256, 4, F32>(p, st);
+    if (t128 >= 192) return run_tile<T, 128, 128, 4, F32>(p, st);
+    return run_tile<T, 64, 64, 4, F32>(p, st);
+}
+
+int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+// Runs of token blocks whose sums of dz are kept apart: few for a long batch, one block each while there are few waves.
+int64_t blocks_per_run(int64_t M, int64_t N)
+{
+    const int64_t units = (M + 31) / 32 * ((N + 127) / 128);
+    return units >= 8 * 4096 ? 8 : units >= 2 * 4096 ? 2 : 1;
+}
+
+struct BwdWork {
+    int64_t dza, dzt, xt, part, total;
+    BwdWork(int64_t M, int64_t N, int64_t K)
+    {
+        dza = 0;
+        dzt = dza + round_up(M * round_up(N, 64) * 2, 256);
+        xt = dzt + operand_bytes(M, N);
+        part = xt + operand_bytes(M, K);
+        const int64_t tb = (M + 31) / 32, per = blocks_per_run(M, N);
+        total = part + round_up((tb + per - 1) / per * N * 4, 256);
+    }
+};
+
+}  // namespace
+
+hipError_t launch_linear_wgrad(const WgradArgs& a, hipStream_t st)
+{
+    WgParams p = {};
+    p.x = a.xt, p.d = a.dzt;
+    p.N = (int)a.N, p.K = (int)a.K, p.nk = (int)((a.M + 31) / 32);
+    p.xpitch = (a.K + 31) / 32 * 2048, p.dpitch = (a.N + 31) / 32 * 2048;
+    p.dw = a.dw;
+    p.vec = ((uintptr_t)a.dw & 15) == 0 && a.K % 8 == 0;
+    if (a.f16) return a.dw_f32 ? run<F16, true>(p, st) : run<F16, false>(p, st);
+    return a.dw_f32 ? run<BF16, true>(p, st) : run<BF16, false>(p, st);
+}
+
+size_t linear_backward_workspace(int64_t M, int64_t N, int64_t K) { return (size_t)BwdWork(M, N, K).total; }
+
+hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t st)
+{
+    const BwdWork w(a.M, a.N, a.K);
+    // a gradient that is dy itself, with one factor for all outputs, is multiplied where it lies
+    const bool direct = a.act == kActNone && !a.alpha.ptr;
+    GradArgs g = {};
+    g.dy = a.dy, g.zq = a.zq, g.xq = a.xq;
+    g.M = a.M, g.N = a.N, g.K = a.K, g.lddy = a.lddy, g.lda = round_up(a.N, 64);
+    g.alpha = a.alpha, g.act = a.act;
+    g.per = blocks_per_run(a.M, a.N);
+    g.dza = a.dx && !direct ? a.workspace + w.dza : nullptr;
+    g.dzt = a.dw ? a.workspace + w.dzt : nullptr;
+    g.xt = a.dw ? a.workspace + w.xt : nullptr;
+    g.part = a.dbias ? (float*)(a.workspace + w.part) : nullptr;
+    hipError_t e;
+    if (a.M && (e = launch_linear_grad(g, a.f16, st)) != hipSuccess) return e;
+    if (a.dx && a.M) {
+        LinearArgs l = {};
+        l.x = direct ? a.dy : g.dza;
+        l.ldx = direct ? a.lddy : g.lda;
+        l.w = a.wt;
+        l.M = a.M, l.N = a.K, l.K = direct ? a.N : g.lda;
+        l.alpha.s = direct ? a.alpha.s : 1.f;
+        l.y = a.dx, l.ldy = a.lddx;
+        l.f16 = a.f16;
+        l.workspace = a.workspace + w.dza;
+        if ((e = launch_linear(l, st)) != hipSuccess) return e;
+    }
+    if (a.dw) {
+        WgradArgs d = {g.dzt, g.xt, a.M, a.N, a.K, a.dw, a.f16, a.dw_f32};
+        if ((e = launch_linear_wgrad(d, st)) != hipSuccess) return e;
+    }
+    if (a.dbias) {
+        const int64_t tb = (a.M + 31) / 32;
+        if ((e = launch_bias_sum(g.part, (tb + g.per - 1) / g.per, a.N, a.dbias, a.f16, st)) != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace rtn

@@ -1,0 +1,138 @@
+// What the kernels of the ternary linear layer and of the 8-bit activation checkpoints share: the 16-bit types,
+// the activations and their slopes, the checkpoint's layout and the layout of prepared weights.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace rtn {
+
+// ---- 8-bit checkpoint of a [M][C] tensor ------------------------------------------------------------------------
+// Groups of 32 consecutive tokens of one channel share a power of two 2^e; a value is q 2^e, |q| <= 127.
+//   codes   [ceil(M / 32)][ceil(C / 8)][32 tokens][8 channels] int8: 256 bytes per (32 tokens, 8 channels), so a thread
+//           that has 8 tokens of 8 channels reads or writes 64 bytes in a row
+//   scales  [ceil(M / 32)][8 ceil(C / 8)] uint8 behind them, e + 127 (E8M0); 255: the group held an infinity or NaN
+// Tokens and channels past the end are zero.
+struct CkptShape {
+    int64_t tb, cb;  // blocks of 32 tokens, of 8 channels
+    __host__ __device__ CkptShape(int64_t M, int64_t C) : tb((M + 31) / 32), cb((C + 7) / 8) {}
+    __host__ __device__ int64_t codes() const { return tb * cb * 256; }
+    __host__ __device__ int64_t bytes() const { return tb * cb * 264; }
+};
+
+// ---- prepared ternary weights of `rows` outputs over `cols` inputs ----------------------------------------------------
+// Two bits a weight in the order the matrix instruction takes its operand (32 rows x 16 columns, lane l holding row l & 31,
+// columns 8 (l >> 5) .. + 7): [ceil(rows / 32)][ceil(cols / 64)][64 lanes] of 8 bytes.  Word s of a lane holds its codes of the
+// 16-column slices 2 s and 2 s + 1 of the 64 columns.  A code is (sign, non-zero) at bits 15:14 of a 16-bit half, which
+// as bfloat16 and as float16 alike is -2, 0 or +2; the word keeps 8 codes per half, the one of register r at bits 15 - 2 r,
+// 14 - 2 r, so an operand register of two weights is (word << 2 r) & 0xC000C000.  Padding is code 0.
+struct WeightShape {
+    int64_t rb, cb;
+    __host__ __device__ WeightShape(int64_t rows, int64_t cols) : rb((rows + 31) / 32), cb((cols + 63) / 64) {}
+    __host__ __device__ int64_t bytes() const { return rb * cb * 512; }
+};
+constexpr unsigned kCodeMask = 0xC000C000u;
+
+// ---- operand order of a [tokens][channels] 16-bit tensor whose product contracts over tokens (weight gradient) -------------
+// [ceil(M / 32)][ceil(C / 32)][2 slices of 16 tokens][64 lanes][8 tokens]: lane l holds channel l & 31, tokens 8 (l >> 5) .. + 7.
+// Tokens and channels past the end are zero.
+__host__ __device__ inline int64_t operand_offset(int64_t tb, int64_t cb, int64_t blocks) { return (tb * blocks + cb) * 2048; }
+// bytes; a tile of 256 channels at the last blocks reads on behind them, values that reach no output
+__host__ __device__ inline int64_t operand_bytes(int64_t M, int64_t C) { return (M + 31) / 32 * ((C + 31) / 32) * 2048 + 8 * 2048; }
+
+constexpr int kFewTokens = 32;  // up to here a layer streams its weights through k_linear_few
+
+enum LinearAct { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };
+
+#if defined(__HIPCC__)
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+struct BF16 {
+    // of a checkpoint's scale: 2^-126 is the least normal; 127 x 2^121 is finite, 64 x 2^122 is not
+    static constexpr int kLeastExp = -126, kMostExp = 121;
+    static __device__ __forceinline__ float to_float(unsigned short v) { return __uint_as_float((unsigned)v << 16); }
+    static __device__ __forceinline__ unsigned short from_float(float f)
+    {
+        return __builtin_bit_cast(unsigned short, (__bf16)f);
+    }
+    static __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+struct F16 {
+    // every float16 is a multiple of 2^-24, and so is what a checkpoint gives back; 64 x 2^10 is infinite
+    static constexpr int kLeastExp = -24, kMostExp = 9;
+    static __device__ __forceinline__ float to_float(unsigned short v) { return (float)__builtin_bit_cast(_Float16, v); }
+    static __device__ __forceinline__ unsigned short from_float(float f)
+    {
+        return __builtin_bit_cast(unsigned short, (_Float16)f);
+    }
+    static __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+};
+template <class T>
+__device__ __forceinline__ unsigned pack2(float lo, float hi)
+{
+    return (unsigned)T::from_float(lo) | (unsigned)T::from_float(hi) << 16;
+}
+template <class T>
+__device__ __forceinline__ float half_of(unsigned pair, int i)
+{
+    return T::to_float((unsigned short)(i ? pair >> 16 : pair & 0xffffu));
+}
+
+// phi(z) in fp32.  gelu is z Phi(z) with the normal distribution's Phi through erf, silu z / (1 + exp(-z)).
+template <int ACT>
+__device__ __forceinline__ float act_value(float z)
+{
+    if constexpr (ACT == kActRelu) return z > 0.f ? z : (z == z ? 0.f : z);
+    if constexpr (ACT == kActGelu) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    if constexpr (ACT == kActSilu) return z * __builtin_amdgcn_rcpf(1.f + __expf(-z));
+    return z;
+}
+// phi'(z): 1 / 0 of a relu (0 at 0, and a NaN gives NaN), Phi(z) + z times the normal density, s (1 + z (1 - s)).
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z)
+{
+    if constexpr (ACT == kActRelu) return z > 0.f ? 1.f : (z == z ? 0.f : z);
+    if constexpr (ACT == kActGelu)
+        return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
+    if constexpr (ACT == kActSilu) {
+        const float s = __builtin_amdgcn_rcpf(1.f + __expf(-z));
+        return s * (1.f + z * (1.f - s));
+    }
+    return 1.f;
+}
+
+// The scale of a group whose largest magnitude is `amax`: the exponent e, so that rint(amax 2^-e) is 64 .. 127 (amax 2^-e
+// in [127.5, 128) would round to 128 and takes the next one), within T's range.  Returned as e + 127; 255: not finite.
+template <class T>
+__device__ __forceinline__ int ckpt_exponent(float amax)
+{
+    const unsigned u = __float_as_uint(amax);
+    if (u >= 0x7f800000u) return 255;
+    const int biased = (int)(u >> 23) - 6 + ((u & 0x7fffffu) >= 0x7f0000u);  // 127.5 / 64 = 1.1111111b
+    constexpr int lo = T::kLeastExp + 127, hi = T::kMostExp + 127;
+    return biased < lo ? lo : biased > hi ? hi : biased;
+}
+// v / 2^e as a code; beyond +-127 are only values at the end of T's range (and, of a float16 layer, z beyond it)
+__device__ __forceinline__ unsigned ckpt_code(float v, float inverse)
+{
+    return (unsigned)(int)__builtin_amdgcn_fmed3f(rintf(v * inverse), -127.f, 127.f) & 255u;
+}
+__device__ __forceinline__ float ckpt_scale(int biased) { return __uint_as_float(biased == 255 ? 0x7fc00000u : (unsigned)biased << 23); }
+// 2^-e; for e in -126 .. 122 both are normal
+__device__ __forceinline__ float ckpt_inverse(int biased) { return __uint_as_float((unsigned)(biased == 255 ? 0 : 254 - biased) << 23); }
+
+}  // namespace
+#endif
+
+}  // namespace rtn

@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include "linear_math.h"
 #include "rtn_kernels.h"
 
 namespace {
@@ -88,6 +89,14 @@ int make_geom(int64_t Nb, int64_t C, int64_t H, int64_t W, int64_t O, int KH, in
     g.div_ow = rtn::make_fastdiv((uint32_t)OW);
     return RTN_OK;
 }
+
+// Ternary linear layer: features (a row of operands stays within 32-bit offsets), rows of a 16-bit tensor, and the waves
+// of the passes over checkpoints.
+constexpr int64_t kMaxFeatures = 1LL << 21;
+bool linear_dims(int64_t N, int64_t K) { return N > 0 && K > 0 && N <= kMaxFeatures && K <= kMaxFeatures; }
+bool linear_rows(int64_t M, int64_t len, int64_t ld) { return M >= 0 && M <= kMaxDim && ld >= len && ld <= (1LL << 31); }
+bool ckpt_units(int64_t M, int64_t C) { return (double)((M + 31) / 32) * (double)((C + 127) / 128) < (double)(1LL << 31); }
+bool known_act(rtn_act act) { return act >= RTN_ACT_NONE && act <= RTN_ACT_SILU; }
 
 }  // namespace
 
@@ -667,6 +676,133 @@ int rtn_epilogue_reparam_conv2d(const int32_t* acc, int64_t Nb, int64_t C, int64
     if ((rc = make_epilogue(ep, true, e)) != RTN_OK) return rc;
     const hipError_t he = rtn::launch_epilogue_conv(acc, g, e, y_out, (hipStream_t)stream);
     return he == hipSuccess ? RTN_OK : hip_fail(he);
+}
+
+size_t rtn_linear_prepared_bytes(int64_t N, int64_t K)
+{
+    return linear_dims(N, K) ? (size_t)rtn::WeightShape(N, K).bytes() : 0;
+}
+
+int rtn_linear_prepare(rtn_code_format fmt, const void* w_codes, int64_t N, int64_t K, void* prepared,
+                       size_t prepared_bytes, void* prepared_t, size_t prepared_t_bytes, void* stream)
+{
+    if (!w_codes || (!prepared && !prepared_t)) return RTN_ERR_NULL;
+    if (fmt != RTN_CODE_I8 && fmt != RTN_CODE_BITPLANE && fmt != RTN_CODE_FP4) return RTN_ERR_UNSUPPORTED;
+    if (!linear_dims(N, K)) return RTN_ERR_SHAPE;
+    if (prepared && prepared_bytes < rtn_linear_prepared_bytes(N, K)) return RTN_ERR_WORKSPACE;
+    if (prepared_t && prepared_t_bytes < rtn_linear_prepared_bytes(K, N)) return RTN_ERR_WORKSPACE;
+    if (!aligned(w_codes, 16) || !aligned(prepared, 16) || !aligned(prepared_t, 16)) return RTN_ERR_ALIGN;
+    rtn::LinearPrepArgs a = {w_codes, N, K, padk(fmt, K), prepared, prepared_t};
+    const hipError_t e = rtn::launch_linear_prepare(a, (int)fmt, (hipStream_t)stream);
+    return e == hipSuccess ? RTN_OK : hip_fail(e);
+}
+
+size_t rtn_linear_workspace_bytes(const void* x, int64_t ldx, int64_t M, int64_t K, int keeps_z)
+{
+    if (!linear_dims(1, K) || M <= 0 || M > kMaxDim || ldx < K) return 0;
+    rtn::LinearArgs a = {};
+    a.x = x, a.M = M, a.K = K, a.ldx = ldx;
+    a.zq = keeps_z ? (int8_t*)16 : nullptr;
+    return rtn::linear_copies_x(a) ? (size_t)M * (size_t)((K + 63) / 64 * 128) : 0;
+}
+
+int rtn_linear(rtn_dtype dt, const void* x, int64_t ldx, const void* prepared, int64_t M, int64_t N, int64_t K,
+               const float* alpha_w, rtn_gran gran_w, const void* bias, rtn_act act, const void* residual, int64_t ldr,
+               void* y, int64_t ldy, void* z_ckpt, size_t z_ckpt_bytes, void* workspace, size_t workspace_bytes,
+               void* stream)
+{
+    if (!prepared || !alpha_w || (M != 0 && (!x || !y))) return RTN_ERR_NULL;
+    if ((dt != RTN_BF16 && dt != RTN_F16) || !known_act(act)) return RTN_ERR_UNSUPPORTED;
+    if (!linear_dims(N, K) || !linear_rows(M, K, ldx) || !linear_rows(M, N, ldy) || (residual && !linear_rows(M, N, ldr)))
+        return RTN_ERR_SHAPE;
+    if (!aligned(x, 2) || !aligned(y, 2) || !aligned(bias, 2) || !aligned(residual, 2) || !aligned(prepared, 16) ||
+        !aligned(z_ckpt, 16))
+        return RTN_ERR_ALIGN;
+    rtn::LinearArgs a = {};
+    const int rc = make_param(alpha_w, gran_w, false, a.alpha);
+    if (rc != RTN_OK) return rc;
+    if (z_ckpt && z_ckpt_bytes < rtn_checkpoint_bytes(M, N)) return RTN_ERR_WORKSPACE;
+    if (M == 0) return RTN_OK;
+    const size_t need = rtn_linear_workspace_bytes(x, ldx, M, K, z_ckpt != nullptr);
+    if (need && (!workspace || workspace_bytes < need)) return RTN_ERR_WORKSPACE;
+    if (need && !aligned(workspace, 16)) return RTN_ERR_ALIGN;
+    a.x = x, a.w = prepared;
+    a.M = M, a.N = N, a.K = K, a.ldx = ldx, a.ldr = ldr, a.ldy = ldy;
+    a.bias = bias, a.res = residual, a.y = y;
+    a.zq = (int8_t*)z_ckpt;
+    a.act = (int)act, a.f16 = dt == RTN_F16;
+    a.workspace = workspace;
+    const hipError_t e = rtn::launch_linear(a, (hipStream_t)stream);
+    return e == hipSuccess ? RTN_OK : hip_fail(e);
+}
+
+size_t rtn_checkpoint_bytes(int64_t M, int64_t C)
+{
+    return M > 0 && C > 0 && M <= kMaxDim && C <= kMaxDim ? (size_t)rtn::CkptShape(M, C).bytes() : 0;
+}
+
+int rtn_checkpoint_pack(rtn_dtype dt, const void* x, int64_t ldx, int64_t M, int64_t C, void* ckpt, size_t ckpt_bytes,
+                        void* stream)
+{
+    if (M != 0 && (!x || !ckpt)) return RTN_ERR_NULL;
+    if (dt != RTN_BF16 && dt != RTN_F16) return RTN_ERR_UNSUPPORTED;
+    if (C <= 0 || C > kMaxDim || !linear_rows(M, C, ldx) || !ckpt_units(M, C)) return RTN_ERR_SHAPE;
+    if (!aligned(x, 2) || !aligned(ckpt, 16)) return RTN_ERR_ALIGN;
+    if (ckpt_bytes < rtn_checkpoint_bytes(M, C)) return RTN_ERR_WORKSPACE;
+    if (M == 0) return RTN_OK;
+    rtn::CkptArgs a = {};
+    a.x = x, a.M = M, a.C = C, a.ld = ldx, a.ckpt = (int8_t*)ckpt, a.f16 = dt == RTN_F16;
+    const hipError_t e = rtn::launch_checkpoint_pack(a, (hipStream_t)stream);
+    return e == hipSuccess ? RTN_OK : hip_fail(e);
+}
+
+int rtn_checkpoint_unpack(rtn_dtype dt, const void* ckpt, size_t ckpt_bytes, int64_t M, int64_t C, void* y, int64_t ldy,
+                          void* stream)
+{
+    if (M != 0 && (!y || !ckpt)) return RTN_ERR_NULL;
+    if (dt != RTN_BF16 && dt != RTN_F16) return RTN_ERR_UNSUPPORTED;
+    if (C <= 0 || C > kMaxDim || !linear_rows(M, C, ldy) || !ckpt_units(M, C)) return RTN_ERR_SHAPE;
+    if (!aligned(y, 2) || !aligned(ckpt, 16)) return RTN_ERR_ALIGN;
+    if (ckpt_bytes < rtn_checkpoint_bytes(M, C)) return RTN_ERR_WORKSPACE;
+    if (M == 0) return RTN_OK;
+    rtn::CkptArgs a = {};
+    a.y = y, a.M = M, a.C = C, a.ld = ldy, a.ckpt = (int8_t*)const_cast<void*>(ckpt), a.f16 = dt == RTN_F16;
+    const hipError_t e = rtn::launch_checkpoint_unpack(a, (hipStream_t)stream);
+    return e == hipSuccess ? RTN_OK : hip_fail(e);
+}
+
+size_t rtn_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K)
+{
+    return linear_dims(N, K) && M >= 0 && M <= kMaxDim ? rtn::linear_backward_workspace(M, N, K) : 0;
+}
+
+int rtn_linear_backward(rtn_dtype dt, const void* dy, int64_t lddy, const void* x_ckpt, size_t x_ckpt_bytes,
+                        const void* z_ckpt, size_t z_ckpt_bytes, rtn_act act, const void* prepared_t, int64_t M, int64_t N,
+                        int64_t K, const float* alpha_w, rtn_gran gran_w, void* dx, int64_t lddx, void* dw,
+                        rtn_dtype dw_type, void* dbias, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if ((!dx && !dw && !dbias) || !alpha_w || (M != 0 && !dy)) return RTN_ERR_NULL;
+    if ((dt != RTN_BF16 && dt != RTN_F16) || !known_act(act)) return RTN_ERR_UNSUPPORTED;
+    if (dw && dw_type != dt && dw_type != RTN_F32) return RTN_ERR_UNSUPPORTED;
+    if ((dx && !prepared_t) || (M != 0 && ((dw && !x_ckpt) || (act != RTN_ACT_NONE && !z_ckpt)))) return RTN_ERR_NULL;
+    if (!linear_dims(N, K) || !linear_rows(M, N, lddy) || (dx && !linear_rows(M, K, lddx))) return RTN_ERR_SHAPE;
+    if (!ckpt_units(M, N) || !ckpt_units(M, K)) return RTN_ERR_SHAPE;
+    if (!aligned(dy, 2) || !aligned(dx, 2) || !aligned(dw, dw_type == RTN_F32 ? 4 : 2) || !aligned(dbias, 2) ||
+        !aligned(prepared_t, 16) || !aligned(x_ckpt, 16) || !aligned(z_ckpt, 16) || !aligned(workspace, 16))
+        return RTN_ERR_ALIGN;
+    rtn::LinearBwdArgs a = {};
+    const int rc = make_param(alpha_w, gran_w, false, a.alpha);
+    if (rc != RTN_OK) return rc;
+    if (dw && x_ckpt_bytes < rtn_checkpoint_bytes(M, K)) return RTN_ERR_WORKSPACE;
+    if (act != RTN_ACT_NONE && z_ckpt_bytes < rtn_checkpoint_bytes(M, N)) return RTN_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < rtn_linear_backward_workspace_bytes(M, N, K)) return RTN_ERR_WORKSPACE;
+    a.dy = dy, a.xq = (const int8_t*)x_ckpt, a.zq = (const int8_t*)z_ckpt, a.wt = prepared_t;
+    a.M = M, a.N = N, a.K = K, a.lddy = lddy, a.lddx = lddx;
+    a.act = (int)act, a.f16 = dt == RTN_F16, a.dw_f32 = dw_type == RTN_F32;
+    a.dx = dx, a.dw = dw, a.dbias = dbias;
+    a.workspace = (char*)workspace;
+    const hipError_t e = rtn::launch_linear_backward(a, (hipStream_t)stream);
+    return e == hipSuccess ? RTN_OK : hip_fail(e);
 }
 
 }  // extern "C"

@@ -226,4 +226,82 @@ hipError_t launch_epilogue_gemm(const int32_t* acc, int64_t M, int64_t N, int64_
 hipError_t launch_epilogue_conv(const int32_t* acc, const ConvGeom& g, const EpiArgs& ep, float* y,
                                 hipStream_t st);
 
+// Ternary linear layer of 16-bit activations and its 8-bit checkpoints (layouts: linear_math.h).
+struct LinearPrepArgs {
+    const void* codes;  // [N][Kpad] in the code format
+    int64_t N, K, Kpad;
+    void* out;    // nullable: rows n over columns k
+    void* out_t;  // nullable: rows k over columns n
+};
+hipError_t launch_linear_prepare(const LinearPrepArgs& a, int fmt, hipStream_t st);
+
+// y[m][n] = act(scale alpha[n] sum_k x[m][k] t[n][k] + bias[n]) + residual[m][n]
+struct LinearArgs {
+    const void* x;      // [M][K] 16 bit, row pitch ldx elements
+    const void* w;      // prepared weights, [N][K]
+    int64_t M, N, K, ldx, ldr, ldy;
+    Param alpha;        // scalar or per n
+    const void* bias;   // nullable, 16 bit [N]
+    const void* res;    // nullable, 16 bit
+    void* y;            // 16 bit
+    int8_t* zq;         // nullable: 8-bit checkpoint of the value before the activation
+    int act;            // LinearAct
+    int f16;            // 1: float16, 0: bfloat16
+    void* workspace;    // x in rows of whole steps, where its own are not (linear_copies_x)
+};
+bool linear_copies_x(const LinearArgs& a);
+hipError_t launch_linear(const LinearArgs& a, hipStream_t st);
+
+struct CkptArgs {
+    const void* x;      // pack: [M][C] 16 bit, row pitch ld
+    void* y;            // unpack: the same
+    int64_t M, C, ld;
+    int8_t* ckpt;
+    int f16;
+};
+hipError_t launch_checkpoint_pack(const CkptArgs& a, hipStream_t st);
+hipError_t launch_checkpoint_unpack(const CkptArgs& a, hipStream_t st);
+
+// What k_linear_grad writes, each of the outputs nullable.
+struct GradArgs {
+    const void* dy;
+    const int8_t *zq, *xq;
+    int64_t M, N, K, lddy, lda;
+    Param alpha;
+    int act;
+    void* dza;    // dz alpha, row-major [M][lda], lda whole steps of 64, zeros past N
+    char *dzt;    // dz in operand order
+    char *xt;     // x^ in operand order
+    float* part;  // [runs][N]: sums of dz over runs of `per` blocks of 32 tokens
+    int64_t per;
+    // set by launch_linear_grad
+    int64_t dz_strips, dz_units, x_strips, x_units;
+    int vec_dy;
+};
+hipError_t launch_linear_grad(GradArgs a, int f16, hipStream_t st);
+hipError_t launch_bias_sum(const float* part, int64_t runs, int64_t N, void* out, int f16, hipStream_t st);
+
+// dw[n][k] = sum_m dz[m][n] x^[m][k], both operands in operand order
+struct WgradArgs {
+    const char *dzt, *xt;
+    int64_t M, N, K;
+    void* dw;  // [N][K]
+    int f16, dw_f32;
+};
+hipError_t launch_linear_wgrad(const WgradArgs& a, hipStream_t st);
+
+struct LinearBwdArgs {
+    const void* dy;     // [M][N] 16 bit, row pitch lddy
+    const int8_t* xq;   // checkpoint of x [M][K] (nullable without dw)
+    const int8_t* zq;   // checkpoint of z [M][N] (nullable without an activation)
+    const void* wt;     // prepared transposed weights (nullable without dx)
+    int64_t M, N, K, lddy, lddx;
+    Param alpha;
+    int act, f16, dw_f32;
+    void *dx, *dw, *dbias;  // each nullable
+    char* workspace;
+};
+size_t linear_backward_workspace(int64_t M, int64_t N, int64_t K);
+hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t st);
+
 }  // namespace rtn

@@ -1,0 +1,121 @@
+"""What the entry points of the ternary linear layer and of the 8-bit checkpoints refuse, on a host without a GPU: every
+check comes before any launch."""
+import ctypes as C
+import os
+
+import pytest
+import torch
+
+from paper_1912_02057_amd import binding as B
+
+FAKE, OTHER = C.c_void_p(0x10000), C.c_void_p(0x20000)   # never dereferenced: validation fails first
+ODD, HALF = C.c_void_p(0x10001), C.c_void_p(0x10002)
+BIG = 1 << 40
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(B.LIB_PATH):
+        from paper_1912_02057_amd.build import build_lib
+        build_lib()
+    return B.lib()
+
+
+def _f(v):
+    return C.cast(C.pointer(C.c_float(v)), C.c_void_p)
+
+
+def _refuses(call, ok, cases):
+    for change, status in cases:
+        a = list(ok)
+        for i, v in change.items():
+            a[i] = v
+        assert call(*a) == status, (change, status)
+
+
+def test_sizes(L):
+    assert L.rtn_linear_prepared_bytes(1, 1) == 512
+    assert L.rtn_linear_prepared_bytes(33, 65) == 2 * 2 * 512
+    assert L.rtn_linear_prepared_bytes(4096, 4096) == 4096 * 4096 // 4
+    assert L.rtn_linear_prepared_bytes(0, 5) == 0 and L.rtn_linear_prepared_bytes(5, (1 << 21) + 1) == 0
+    assert L.rtn_checkpoint_bytes(1, 1) == 264
+    assert L.rtn_checkpoint_bytes(33, 9) == 4 * 264
+    assert L.rtn_checkpoint_bytes(0, 9) == 0 and L.rtn_checkpoint_bytes(5, -1) == 0
+    # rows of whole 16 bytes are read where they lie, others are copied; a few tokens never are
+    assert L.rtn_linear_workspace_bytes(FAKE, 128, 500, 128, 0) == 0
+    assert L.rtn_linear_workspace_bytes(FAKE, 131, 500, 128, 0) == 500 * 128 * 2
+    assert L.rtn_linear_workspace_bytes(FAKE, 136, 500, 130, 0) == 500 * 192 * 2
+    assert L.rtn_linear_workspace_bytes(HALF, 128, 500, 128, 0) == 500 * 128 * 2
+    assert L.rtn_linear_workspace_bytes(HALF, 131, 1, 130, 0) == 0
+    assert L.rtn_linear_workspace_bytes(FAKE, 100, 500, 128, 0) == 0          # a pitch below the row's length
+    assert L.rtn_linear_backward_workspace_bytes(100, 64, 0) == 0
+    assert L.rtn_linear_backward_workspace_bytes(100, 64, 64) > 100 * 64 * 4
+
+
+def test_prepare_refuses(L):
+    ok = [B.RTN_CODE_I8, FAKE, 64, 64, FAKE, BIG, OTHER, BIG, None]
+    _refuses(L.rtn_linear_prepare, ok, [
+        ({1: None}, B.RTN_ERR_NULL), ({4: None, 6: None}, B.RTN_ERR_NULL), ({0: 9}, B.RTN_ERR_UNSUPPORTED), ({2: 0}, B.RTN_ERR_SHAPE),
+        ({3: -1}, B.RTN_ERR_SHAPE), ({3: (1 << 21) + 1}, B.RTN_ERR_SHAPE), ({5: 1023}, B.RTN_ERR_WORKSPACE), ({7: 1023}, B.RTN_ERR_WORKSPACE),
+        ({1: HALF}, B.RTN_ERR_ALIGN), ({4: HALF}, B.RTN_ERR_ALIGN), ({6: HALF}, B.RTN_ERR_ALIGN)])
+
+
+def test_linear_refuses(L):
+    a = _f(0.5)
+    #     0 dt       1 x  2 ldx 3 w   4 M  5 N 6 K 7 a 8 gran     9 b   10 act 11 r 12 ldr 13 y  14 ldy 15 z 16 zb 17 ws 18 wsb 19 stream
+    ok = [B.RTN_BF16, FAKE, 64, FAKE, 100, 64, 64, a, B.RTN_SCALAR, FAKE, 0, FAKE, 64, OTHER, 64, FAKE, BIG, FAKE, BIG, None]
+    _refuses(L.rtn_linear, ok, [
+        ({1: None}, B.RTN_ERR_NULL), ({3: None}, B.RTN_ERR_NULL), ({7: None}, B.RTN_ERR_NULL), ({13: None}, B.RTN_ERR_NULL),
+        ({0: B.RTN_F32}, B.RTN_ERR_UNSUPPORTED), ({0: 5}, B.RTN_ERR_UNSUPPORTED), ({10: 4}, B.RTN_ERR_UNSUPPORTED), ({10: -1}, B.RTN_ERR_UNSUPPORTED),
+        ({8: 7}, B.RTN_ERR_UNSUPPORTED), ({4: -1}, B.RTN_ERR_SHAPE), ({5: 0}, B.RTN_ERR_SHAPE), ({6: 0}, B.RTN_ERR_SHAPE),
+        ({2: 63}, B.RTN_ERR_SHAPE), ({14: 63}, B.RTN_ERR_SHAPE), ({12: 63}, B.RTN_ERR_SHAPE), ({2: 1 << 32}, B.RTN_ERR_SHAPE),
+        ({6: (1 << 21) + 1, 2: 1 << 22}, B.RTN_ERR_SHAPE), ({1: ODD}, B.RTN_ERR_ALIGN), ({13: ODD}, B.RTN_ERR_ALIGN), ({9: ODD}, B.RTN_ERR_ALIGN),
+        ({11: ODD}, B.RTN_ERR_ALIGN), ({3: HALF}, B.RTN_ERR_ALIGN), ({15: HALF}, B.RTN_ERR_ALIGN),
+        ({16: 4 * 8 * 264 - 1}, B.RTN_ERR_WORKSPACE),
+        ({1: HALF, 17: None}, B.RTN_ERR_WORKSPACE), ({1: HALF, 18: 100 * 128 - 1}, B.RTN_ERR_WORKSPACE), ({1: HALF, 17: HALF}, B.RTN_ERR_ALIGN)])
+    assert L.rtn_linear(*[0 if i == 4 else None if i in (1, 13) else v for i, v in enumerate(ok)]) == B.RTN_OK   # nothing to do
+
+
+def test_checkpoint_refuses(L):
+    ok = [B.RTN_F16, FAKE, 64, 100, 64, OTHER, BIG, None]
+    _refuses(L.rtn_checkpoint_pack, ok, [
+        ({1: None}, B.RTN_ERR_NULL), ({5: None}, B.RTN_ERR_NULL), ({0: B.RTN_F32}, B.RTN_ERR_UNSUPPORTED), ({2: 63}, B.RTN_ERR_SHAPE),
+        ({3: -1}, B.RTN_ERR_SHAPE), ({4: 0}, B.RTN_ERR_SHAPE), ({1: ODD}, B.RTN_ERR_ALIGN), ({5: HALF}, B.RTN_ERR_ALIGN),
+        ({6: 4 * 8 * 264 - 1}, B.RTN_ERR_WORKSPACE)])
+    ok = [B.RTN_F16, OTHER, BIG, 100, 64, FAKE, 64, None]
+    _refuses(L.rtn_checkpoint_unpack, ok, [
+        ({1: None}, B.RTN_ERR_NULL), ({5: None}, B.RTN_ERR_NULL), ({0: B.RTN_F32}, B.RTN_ERR_UNSUPPORTED), ({6: 63}, B.RTN_ERR_SHAPE),
+        ({3: -1}, B.RTN_ERR_SHAPE), ({4: 0}, B.RTN_ERR_SHAPE), ({5: ODD}, B.RTN_ERR_ALIGN), ({1: HALF}, B.RTN_ERR_ALIGN),
+        ({2: 4 * 8 * 264 - 1}, B.RTN_ERR_WORKSPACE)])
+    assert L.rtn_checkpoint_pack(B.RTN_F16, None, 64, 0, 64, None, 0, None) == B.RTN_OK
+
+
+def test_backward_refuses(L):
+    a = _f(0.5)
+    #     0 dt       1 dy 2 ld 3 x8 4   5 z8  6   7 act 8 wt  9 M 10 N 11 K 12 a 13 gran   14 dx 15 ld 16 dw  17 type     18 db 19 ws 20 wsb 21
+    ok = [B.RTN_BF16, FAKE, 64, FAKE, BIG, FAKE, BIG, 2, FAKE, 100, 64, 64, a, B.RTN_SCALAR, FAKE, 64, FAKE, B.RTN_F32, FAKE, FAKE, BIG, None]
+    need = L.rtn_linear_backward_workspace_bytes(100, 64, 64)
+    _refuses(L.rtn_linear_backward, ok, [
+        ({1: None}, B.RTN_ERR_NULL), ({3: None}, B.RTN_ERR_NULL), ({5: None}, B.RTN_ERR_NULL), ({8: None}, B.RTN_ERR_NULL),
+        ({12: None}, B.RTN_ERR_NULL), ({14: None, 16: None, 18: None}, B.RTN_ERR_NULL), ({0: B.RTN_F32}, B.RTN_ERR_UNSUPPORTED),
+        ({7: 4}, B.RTN_ERR_UNSUPPORTED), ({17: B.RTN_F16}, B.RTN_ERR_UNSUPPORTED), ({13: 2}, B.RTN_ERR_UNSUPPORTED), ({2: 63}, B.RTN_ERR_SHAPE),
+        ({15: 63}, B.RTN_ERR_SHAPE), ({9: -1}, B.RTN_ERR_SHAPE), ({10: 0}, B.RTN_ERR_SHAPE), ({11: (1 << 21) + 1, 15: 1 << 22}, B.RTN_ERR_SHAPE),
+        ({1: ODD}, B.RTN_ERR_ALIGN), ({14: ODD}, B.RTN_ERR_ALIGN), ({16: HALF}, B.RTN_ERR_ALIGN), ({18: ODD}, B.RTN_ERR_ALIGN),
+        ({3: HALF}, B.RTN_ERR_ALIGN), ({5: HALF}, B.RTN_ERR_ALIGN), ({8: HALF}, B.RTN_ERR_ALIGN), ({19: HALF}, B.RTN_ERR_ALIGN),
+        ({4: 4 * 8 * 264 - 1}, B.RTN_ERR_WORKSPACE), ({6: 4 * 8 * 264 - 1}, B.RTN_ERR_WORKSPACE), ({19: None}, B.RTN_ERR_WORKSPACE),
+        ({20: need - 1}, B.RTN_ERR_WORKSPACE)])
+
+
+def test_binding_refuses_tensors_it_cannot_pass_on():
+    x = torch.zeros(4, 64, dtype=torch.bfloat16)
+    w = torch.zeros(512 * 2, dtype=torch.uint8)
+    with pytest.raises(AssertionError):
+        B.linear(x, w, 64, 1.0)                              # not on a device
+    with pytest.raises(AssertionError):
+        B.linear(x.float(), w, 64, 1.0)
+    with pytest.raises(AssertionError):
+        B.checkpoint_pack(x, torch.zeros(8 * 264, dtype=torch.uint8))
+    with pytest.raises(AssertionError):
+        B.linear_backward(x, w, 64, 1.0, w)
+    with pytest.raises(ValueError):
+        B.linear_prepare(torch.zeros((64, 64), dtype=torch.int8), 64, 64)

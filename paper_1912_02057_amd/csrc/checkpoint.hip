@@ -22,12 +22,15 @@ __device__ __forceinline__ Micro micro_of(int64_t mb, int64_t strip)
 }
 
 // 8 channels of a row as they are; zeros past the end
-__device__ __forceinline__ u32x4 load_row(const unsigned short* x, int64_t ld, int64_t m, int64_t M, int64_t c, int64_t C, bool vec)
+__device__ __forceinline__ u32x4 load_row(const unsigned short* x, int64_t ld, int64_t m, int64_t M, int64_t c, int64_t C)
 {
     u32x4 v = {0, 0, 0, 0};
     if (m >= M) return v;
     const unsigned short* r = x + m * ld + c;
-    if (vec && c + 8 <= C) return *(const u32x4*)r;
+    if (c + 8 <= C) {  // wherever the row starts: global accesses need no alignment on this target
+        __builtin_memcpy(&v, r, 16);
+        return v;
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (c + i < C) v[i >> 1] |= (unsigned)r[i] << (16 * (i & 1));
@@ -35,7 +38,7 @@ __device__ __forceinline__ u32x4 load_row(const unsigned short* x, int64_t ld, i
 }
 
 template <class T>
-__global__ __launch_bounds__(256) void k_ckpt_pack(CkptArgs a, int strips, int vec)
+__global__ __launch_bounds__(256) void k_ckpt_pack(CkptArgs a, int strips)
 {
     const CkptShape cs(a.M, a.C);
     const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -45,9 +48,10 @@ __global__ __launch_bounds__(256) void k_ckpt_pack(CkptArgs a, int strips, int v
     u32x4 v[8];
 #pragma unroll
     for (int t = 0; t < 8; ++t)
-        v[t] = load_row((const unsigned short*)a.x, a.ld, mb * 32 + u.t0 + t, a.M, u.c, a.C, vec);
+        v[t] = load_row((const unsigned short*)a.x, a.ld, mb * 32 + u.t0 + t, a.M, u.c, a.C);
     unsigned ex[2] = {0, 0};
     float inv[8];
+    bool end = false;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         unsigned am = 0;  // as bits: a NaN is larger than an infinity, and that than any number
@@ -64,22 +68,18 @@ __global__ __launch_bounds__(256) void k_ckpt_pack(CkptArgs a, int strips, int v
         const int e = ckpt_exponent<T>(T::to_float((unsigned short)am));
         ex[i >> 2] |= (unsigned)e << (8 * (i & 3));
         inv[i] = ckpt_inverse(e);
+        end |= e == T::kMostExp + 127;
     }
+    const bool clamp = __any(end);
     if (u.c >= a.C) return;
     const int64_t blk = mb * cs.cb + (u.c >> 3);
     unsigned w[16];
 #pragma unroll
     for (int t = 0; t < 8; ++t)
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            unsigned r = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int c = 4 * q + i;
-                r |= ckpt_code(half_of<T>(v[t][c >> 1], c & 1), inv[c]) << (8 * i);
-            }
-            w[t * 2 + q] = r;
-        }
+        for (int q = 0; q < 2; ++q)
+            w[t * 2 + q] = ckpt_codes(half_of<T>(v[t][2 * q], 0), half_of<T>(v[t][2 * q], 1), half_of<T>(v[t][2 * q + 1], 0),
+                                      half_of<T>(v[t][2 * q + 1], 1), inv[4 * q], inv[4 * q + 1], inv[4 * q + 2], inv[4 * q + 3], clamp);
     uint4* out = (uint4*)(a.ckpt + blk * 256 + u.t0 * 8);
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
@@ -115,7 +115,7 @@ struct MicroCkpt {
 };
 
 template <class T>
-__global__ __launch_bounds__(256) void k_ckpt_unpack(CkptArgs a, int strips, int vec)
+__global__ __launch_bounds__(256) void k_ckpt_unpack(CkptArgs a, int strips)
 {
     const CkptShape cs(a.M, a.C);
     const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -136,8 +136,9 @@ __global__ __launch_bounds__(256) void k_ckpt_unpack(CkptArgs a, int strips, int
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = k.code(t, i) * s[i];
         unsigned short* y = (unsigned short*)a.y + m * a.ld + u.c;
-        if (vec && u.c + 8 <= a.C) {
-            *(u32x4*)y = u32x4{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])};
+        if (u.c + 8 <= a.C) {
+            const u32x4 o = {pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])};
+            __builtin_memcpy(y, &o, 16);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -157,7 +158,7 @@ __device__ __forceinline__ void store_operand(char* out, int64_t blocks, const M
 template <class T, int ACT>
 __device__ __forceinline__ void grad_unit(const GradArgs& a, int64_t tb0, int64_t strip)
 {
-    const int64_t nb = (a.N + 31) / 32, tbs = (a.M + 31) / 32;
+    const int64_t nb = (a.N + 31) / 32, tbs = operand_blocks(a.M);
     const CkptShape cs(a.M, a.N);
     float sum[8], al[8];
     const int64_t c = micro_of(0, strip).c;
@@ -170,10 +171,10 @@ __device__ __forceinline__ void grad_unit(const GradArgs& a, int64_t tb0, int64_
         const Micro u = micro_of(mb, strip);
         u32x4 v[8];
 #pragma unroll
-        for (int t = 0; t < 8; ++t) v[t] = load_row((const unsigned short*)a.dy, a.lddy, mb * 32 + u.t0 + t, a.M, u.c, a.N, a.vec_dy);
+        for (int t = 0; t < 8; ++t) v[t] = load_row((const unsigned short*)a.dy, a.lddy, mb * 32 + u.t0 + t, a.M, u.c, a.N);
         MicroCkpt k;
         if constexpr (ACT != kActNone) {
-            if (u.c < a.N)
+            if (u.c < a.N && mb < cs.tb)
                 k.load(a.zq, cs, u);
             else
                 k.zero();
@@ -244,7 +245,7 @@ __global__ __launch_bounds__(256) void k_linear_grad(GradArgs a)
     if (u.c >= kb * 32) return;
     const CkptShape cs(a.M, a.K);
     MicroCkpt k;
-    if (u.c < a.K)
+    if (u.c < a.K && mb < cs.tb)
         k.load(a.xq, cs, u);
     else
         k.zero();
@@ -261,51 +262,55 @@ __global__ __launch_bounds__(256) void k_linear_grad(GradArgs a)
     store_operand(a.xt, kb, u, o);
 }
 
-// dbias[n] = sum of the runs' partial sums, in their order
+// dbias[n] = sum of the runs' partial sums: 16 strands of every 16th run, each in order, then the strands in order
 template <class T>
-__global__ __launch_bounds__(64) void k_bias_sum(const float* part, int64_t runs, int64_t N, unsigned short* out)
+__global__ __launch_bounds__(256) void k_bias_sum(const float* part, int64_t runs, int64_t N, unsigned short* out)
 {
-    const int64_t n = (int64_t)blockIdx.x * 64 + threadIdx.x;
-    if (n >= N) return;
+    __shared__ float sums[16][16];
+    const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
+    const int64_t n = (int64_t)blockIdx.x * 16 + c;
     float s = 0.f;
-    for (int64_t r = 0; r < runs; ++r) s += part[r * N + n];
+    if (n < N) {
+#pragma unroll 4
+        for (int64_t r = g; r < runs; r += 16) s += part[r * N + n];
+    }
+    sums[g][c] = s;
+    __syncthreads();
+    if (g || n >= N) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s += sums[i][c];
     out[n] = T::from_float(s);
 }
-
-bool rows_of_16(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
 
 }  // namespace
 
 hipError_t launch_checkpoint_pack(const CkptArgs& a, hipStream_t st)
 {
     const int64_t strips = (a.C + 127) / 128, blocks = ((a.M + 31) / 32 * strips + 3) / 4;
-    const int vec = rows_of_16(a.x, a.ld);
     if (a.f16)
-        k_ckpt_pack<F16><<<(unsigned)blocks, 256, 0, st>>>(a, (int)strips, vec);
+        k_ckpt_pack<F16><<<(unsigned)blocks, 256, 0, st>>>(a, (int)strips);
     else
-        k_ckpt_pack<BF16><<<(unsigned)blocks, 256, 0, st>>>(a, (int)strips, vec);
+        k_ckpt_pack<BF16><<<(unsigned)blocks, 256, 0, st>>>(a, (int)strips);
     return hipGetLastError();
 }
 
 hipError_t launch_checkpoint_unpack(const CkptArgs& a, hipStream_t st)
 {
     const int64_t strips = (a.C + 127) / 128, blocks = ((a.M + 31) / 32 * strips + 3) / 4;
-    const int vec = rows_of_16(a.y, a.ld);
     if (a.f16)
-        k_ckpt_unpack<F16><<<(unsigned)blocks, 256, 0, st>>>(a, (int)strips, vec);
+        k_ckpt_unpack<F16><<<(unsigned)blocks, 256, 0, st>>>(a, (int)strips);
     else
-        k_ckpt_unpack<BF16><<<(unsigned)blocks, 256, 0, st>>>(a, (int)strips, vec);
+        k_ckpt_unpack<BF16><<<(unsigned)blocks, 256, 0, st>>>(a, (int)strips);
     return hipGetLastError();
 }
 
 hipError_t launch_linear_grad(GradArgs a, int f16, hipStream_t st)
 {
-    const int64_t tbs = (a.M + 31) / 32;
+    const int64_t tbs = operand_blocks(a.M);
     a.dz_strips = a.dzt || a.dza || a.part ? (a.N + 127) / 128 : 0;
     a.dz_units = (tbs + a.per - 1) / a.per * a.dz_strips;
     a.x_strips = a.xt ? (a.K + 127) / 128 : 0;
     a.x_units = tbs * a.x_strips;
-    a.vec_dy = rows_of_16(a.dy, a.lddy);
     const int64_t blocks = (a.dz_units + a.x_units + 3) / 4;
     if (!blocks) return hipSuccess;
     if (f16)
@@ -317,11 +322,11 @@ hipError_t launch_linear_grad(GradArgs a, int f16, hipStream_t st)
 
 hipError_t launch_bias_sum(const float* part, int64_t runs, int64_t N, void* out, int f16, hipStream_t st)
 {
-    const unsigned blocks = (unsigned)((N + 63) / 64);
+    const unsigned blocks = (unsigned)((N + 15) / 16);
     if (f16)
-        k_bias_sum<F16><<<blocks, 64, 0, st>>>(part, runs, N, (unsigned short*)out);
+        k_bias_sum<F16><<<blocks, 256, 0, st>>>(part, runs, N, (unsigned short*)out);
     else
-        k_bias_sum<BF16><<<blocks, 64, 0, st>>>(part, runs, N, (unsigned short*)out);
+        k_bias_sum<BF16><<<blocks, 256, 0, st>>>(part, runs, N, (unsigned short*)out);
     return hipGetLastError();
 }
 

@@ -237,4 +237,40 @@ inline int pick_ksplit(const KsplitShape& s)
     return plain >= 0 && ksplit_fits(plain, s) ? plain : -1;
 }
 
+// The forms of the ternary linear layer's product (linear.hip).  Few: weights straight into registers, up to kFewTokens
+// tokens.  Split: blocks of 32 x 32, 32 x 64 and 64 x 64 (tokens x outputs) whose 8 waves share the columns.  Tiles: of
+// 128 x 128 and 128 x 256, two blocks a CU.
+enum class LinearForm { kFew, kSplit32, kSplit32x64, kSplit64, kTile128, kTile256 };
+constexpr int kFewTokens = 4;
+
+// The least of the forms' times, each a line through measured ones, in us (bf16, no activation; k = K / 1024):
+//   rounds of 256 blocks: split 32 x 32  2 + r (1.9 + 1.2 k), 32 x 64  2 + r (2.2 + 1.45 k), 64 x 64  2 + r (4 + 2 k)
+//   tiles (blocks of one round share their CU's memory path): 128 x 128  3.5 + 6.9 k up to 128 blocks, 4 + 9.2 k up to 256, and
+//   128 x 256  4 + 10.3 k, 11.8 k and 15 k up to 64, 128 and 256 blocks; then rounds of 512 blocks of 3 + 16.5 k and 5 + 25.5 k
+// Measured, M x N x K: 32 x 32 / 32 x 64 / 64 x 64 / 128 x 128 / 128 x 256
+//     64 x 4096 x 4096    7.6 / 8.7 / 11.8 / 29.9 / 42.0      1024 x 4096 x 1024  46.7 / 32.0 / 26.2 / 13.4 / 18.0
+//     512 x 2048 x 2048  18.1 / 12.7 / 10.8 / 18.4 / 25.3     1024 x 8192 x 4096   186 / 124 / 102 / 67.0 / 60.6
+//     256 x 4096 x 4096  27.3 / 18.1 / 13.8 / 31.2 / 43.7     4096 x 4096 x 4096   363 / 239 / 199 / 124 / 108
+// A token count that kFew takes: 1 x 4096 x 4096 measured beside it at launch_linear.
+inline LinearForm linear_form(int64_t M, int64_t N, int64_t K, bool keeps_z)
+{
+    if (M <= kFewTokens && !keeps_z) return LinearForm::kFew;
+    auto blocks = [&](int64_t m, int64_t n) { return ((M + m - 1) / m) * ((N + n - 1) / n); };
+    const double k = (double)K / 1024;
+    auto split = [&](int64_t n, double base, double slope) { return 2 + (double)((n + 255) / 256) * (base + slope * k); };
+    auto tile = [&](int64_t n, double two_base, double two, double b0, double s0, double b1, double s1, double b2, double s2) {
+        if (n <= 64) return b0 + s0 * k;
+        if (n <= 128) return b1 + s1 * k;
+        if (n <= 256) return b2 + s2 * k;
+        return (double)((n + 511) / 512) * (two_base + two * k);
+    };
+    const double t[5] = {split(blocks(32, 32), 1.9, 1.2), split(blocks(32, 64), 2.2, 1.45), split(blocks(64, 64), 4, 2),
+                         tile(blocks(128, 128), 3, 16.5, 3.5, 6.9, 3.5, 6.9, 4, 9.2),
+                         tile(blocks(128, 256), 5, 25.5, 4, 10.3, 4, 11.8, 4, 15)};
+    int best = 4;
+    for (int i = 3; i >= 0; --i)
+        if (t[i] < t[best]) best = i;
+    return (LinearForm)((int)LinearForm::kSplit32 + best);
+}
+
 }  // namespace rtn

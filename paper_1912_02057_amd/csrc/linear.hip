@@ -24,48 +24,121 @@ struct LinParams {
     unsigned short* y;
     int8_t* zq;
     int act;
-    int vec_y, vec_r;       // rows of y / residual can be accessed 16 bytes at a time
 };
+
+// 16 bytes of a row wherever it starts (global accesses need no alignment on this target)
+__device__ __forceinline__ u32x4 load16(const void* p)
+{
+    u32x4 v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+__device__ __forceinline__ void store16(void* p, u32x4 v) { __builtin_memcpy(p, &v, 16); }
 
 // The parameters of 8 consecutive outputs (0 past the end).
 template <class T>
 __device__ __forceinline__ void load_affine(const LinParams& p, int n, float (&al)[8], float (&bi)[8])
 {
+    if (n + 8 <= p.N) {
+        if (p.alpha.ptr) {
+            __builtin_memcpy(al, p.alpha.ptr + n, 32);
+        } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const bool in = n + i < p.N;
-        al[i] = in ? 0.5f * (p.alpha.ptr ? p.alpha.ptr[n + i] : p.alpha.s) : 0.f;
-        bi[i] = in && p.bias ? T::to_float(p.bias[n + i]) : 0.f;
+            for (int i = 0; i < 8; ++i) al[i] = p.alpha.s;
+        }
+        u32x4 b = {0, 0, 0, 0};
+        if (p.bias) b = load16(p.bias + n);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) al[i] *= 0.5f, bi[i] = half_of<T>(b[i >> 1], i & 1);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bool in = n + i < p.N;
+            al[i] = in ? 0.5f * (p.alpha.ptr ? p.alpha.ptr[n + i] : p.alpha.s) : 0.f;
+            bi[i] = in && p.bias ? T::to_float(p.bias[n + i]) : 0.f;
+        }
     }
 }
 
-// act(z) + residual of row m, outputs n .. n + 7 -> y
-template <class T, int ACT>
+// act(z) + residual of outputs n .. n + 7 of row m -> y.  WHOLE: the row exists and so do all eight.
+template <class T, int ACT, bool WHOLE>
 __device__ __forceinline__ void finish_row(const LinParams& p, int m, int n, const float (&z)[8])
 {
-    if (m >= p.M || n >= p.N) return;
+    if (!WHOLE && (m >= p.M || n >= p.N)) return;
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = act_value<ACT>(z[i]);
-    const bool whole = n + 8 <= p.N;
-    if (p.res) {
-        const unsigned short* r = p.res + m * p.ldr + n;
-        if (p.vec_r && whole) {
-            const u32x4 q = *(const u32x4*)r;
+    unsigned short* y = p.y + m * p.ldy + n;
+    if (WHOLE || n + 8 <= p.N) {
+        if (p.res) {
+            const u32x4 q = load16(p.res + m * p.ldr + n);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += half_of<T>(q[i >> 1], i & 1);
-        } else {
-            for (int i = 0; i < 8; ++i)
-                if (n + i < p.N) v[i] += T::to_float(r[i]);
         }
-    }
-    unsigned short* y = p.y + m * p.ldy + n;
-    if (p.vec_y && whole) {
-        *(u32x4*)y = u32x4{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])};
+        store16(y, u32x4{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])});
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (n + i < p.N) y[i] = T::from_float(v[i]);
+            if (n + i < p.N) y[i] = T::from_float(p.res ? v[i] + T::to_float(p.res[m * p.ldr + n + i]) : v[i]);
+    }
+}
+
+template <class F>
+__device__ __forceinline__ void with_act(int act, F&& f)
+{
+    if (act == kActNone)
+        f(std::integral_constant<int, kActNone>{});
+    else if (act == kActRelu)
+        f(std::integral_constant<int, kActRelu>{});
+    else if (act == kActGelu)
+        f(std::integral_constant<int, kActGelu>{});
+    else
+        f(std::integral_constant<int, kActSilu>{});
+}
+
+// Scales of 8 channels from the largest magnitudes (as bits) of their groups
+template <class T>
+struct CkptScale {
+    unsigned ex[2] = {0, 0};
+    float inv[8];
+    bool clamp;
+    __device__ __forceinline__ CkptScale(const unsigned (&am)[8])
+    {
+        bool end = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int e = ckpt_exponent<T>(__uint_as_float(am[i]));
+            ex[i >> 2] |= (unsigned)e << (8 * (i & 3));
+            inv[i] = ckpt_inverse(e);
+            end |= e == T::kMostExp + 127;
+        }
+        clamp = __any(end);
+    }
+};
+template <class T>
+__device__ __forceinline__ void store_scales(const LinParams& p, int mt, int n, const CkptScale<T>& s)
+{
+    const CkptShape cs(p.M, p.N);
+    *(uint2*)(p.zq + cs.codes() + ((int64_t)(mt >> 5) * cs.cb + (n >> 3)) * 8) = make_uint2(s.ex[0], s.ex[1]);
+}
+// The codes of R tokens from mt + t0 on
+template <class T, int R>
+__device__ __forceinline__ void store_codes(const LinParams& p, int mt, int t0, int n, const float (&z)[R][8], const CkptScale<T>& s)
+{
+    const CkptShape cs(p.M, p.N);
+    int8_t* out = p.zq + ((int64_t)(mt >> 5) * cs.cb + (n >> 3)) * 256 + t0 * 8;
+    unsigned w[R * 2];
+#pragma unroll
+    for (int t = 0; t < R; ++t)
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            w[2 * t + q] = ckpt_codes(z[t][4 * q], z[t][4 * q + 1], z[t][4 * q + 2], z[t][4 * q + 3], s.inv[4 * q], s.inv[4 * q + 1],
+                                      s.inv[4 * q + 2], s.inv[4 * q + 3], s.clamp);
+    if constexpr (R > 1) {
+#pragma unroll
+        for (int i = 0; i < R; i += 2) *(uint4*)(out + 8 * i) = make_uint4(w[2 * i], w[2 * i + 1], w[2 * i + 2], w[2 * i + 3]);
+    } else {
+        *(uint2*)out = make_uint2(w[0], w[1]);
     }
 }
 
@@ -81,16 +154,17 @@ __device__ __forceinline__ u32x4 expand(uint2 word)
 template <int BM, int BN, int NS>
 struct LinTile {
     static constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32, NM = TM * TN;
-    static constexpr int ABYTES = BM * 128, STAGE = ABYTES + BN * 16, DPS = BM / 32 + 1;
+    static constexpr int ABYTES = BM * 128, STAGE = ABYTES + BN * 16, XDMA = BM / 32, DPS = XDMA + 1;
     static constexpr int ZPITCH = WN * 4 + 16, ZBYTES = 32 * ZPITCH;  // a wave's 32 rows of fp32 in the epilogue
     static constexpr int LDS = NS * STAGE > 4 * ZBYTES ? NS * STAGE : 4 * ZBYTES;
+    static constexpr int PER_CU = NM >= 16 ? 1 : 2;  // blocks that registers and LDS allow
 };
 
 // A block of 4 waves (2 x 2) owns BM tokens x BN outputs.  Ring of NS stages of 64 columns: x rows of 128 bytes, 16-byte
 // chunk c of row r at place c ^ (r >> 1 & 7), so that 16 rows' fragments hit all banks; then the weights' words.  One barrier per
 // step, before the last of its four 16-column slices, and fragments are read one slice ahead.
 template <class T, int BM, int BN, int NS>
-__global__ __launch_bounds__(256, BM * BN >= 256 * 256 ? 1 : 2) void k_linear(LinParams p)
+__global__ __launch_bounds__(256, (LinTile<BM, BN, NS>::PER_CU)) void k_linear(LinParams p)
 {
     using L = LinTile<BM, BN, NS>;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -109,10 +183,10 @@ __global__ __launch_bounds__(256, BM * BN >= 256 * 256 ? 1 : 2) void k_linear(Li
 
     // ---- direct loads of a stage
     const v4i xr = buffer_base(p.x + (int64_t)m0 * p.ldx * 2), wr = buffer_base(p.w + (int64_t)(n0 / 32) * nk * 512);
-    unsigned xoff[BM / 32];
+    unsigned xoff[L::XDMA];
 #pragma unroll
-    for (int i = 0; i < BM / 32; ++i) {
-        const int row = (wave * (BM / 32) + i) * 8 + (lane >> 3), last = p.M - 1 - m0;
+    for (int i = 0; i < L::XDMA; ++i) {
+        const int row = (wave * L::XDMA + i) * 8 + (lane >> 3), last = p.M - 1 - m0;
         xoff[i] = (unsigned)(row < last ? row : last) * (unsigned)(p.ldx * 2) + (unsigned)(((lane & 7) ^ ((row >> 1) & 7)) * 16);
     }
     unsigned woff;
@@ -121,21 +195,24 @@ __global__ __launch_bounds__(256, BM * BN >= 256 * 256 ? 1 : 2) void k_linear(Li
         woff = (unsigned)(r < last ? r : last) * (unsigned)(nk * 512) + (unsigned)(at & 511);
     }
     const int ktail = p.K & 63;
+    // load i of step `step`, into the stage at LDS address `base`; TAIL: it may be the last one, whose chunks past the rows' ends are zeros
+    auto load_one = [&](auto index, auto may_end, int step, unsigned base) {
+        constexpr int i = decltype(index)::value;
+        if constexpr (i < L::XDMA) {
+            unsigned v = xoff[i];
+            if constexpr (decltype(may_end)::value) {
+                const int row = (wave * L::XDMA + i) * 8 + (lane >> 3);
+                if (ktail && step == nk - 1 && ((lane & 7) ^ ((row >> 1) & 7)) * 8 >= ktail) v = kOutside;
+            }
+            dma_buf<i * 1024>(xr, v, (unsigned)step * 128u, base + (unsigned)(wave * L::XDMA * 1024));
+        } else {
+            if (lane < BN / 4) dma_buf<L::ABYTES>(wr, woff, (unsigned)step * 512u, base + (unsigned)(wave * BN * 4));
+        }
+    };
+    const std::true_type yes{};
+    const std::false_type no{};
     auto issue = [&](int step, int slot) {
-        const unsigned base = lds0 + (unsigned)(slot * L::STAGE), k2 = (unsigned)step * 128u;
-        const bool tail = ktail && step == nk - 1;
-        for_each_index(
-            [&](auto index) {
-                constexpr int i = decltype(index)::value;
-                unsigned v = xoff[i];
-                if (tail) {  // chunks past the row's end are zeros
-                    const int row = (wave * (BM / 32) + i) * 8 + (lane >> 3);
-                    if (((lane & 7) ^ ((row >> 1) & 7)) * 8 >= ktail) v = kOutside;
-                }
-                dma_buf<i * 1024, true>(xr, v, k2, base + (unsigned)(wave * (BM / 32) * 1024));
-            },
-            std::make_integer_sequence<int, BM / 32>{});
-        if (lane < BN / 4) dma_buf<L::ABYTES, true>(wr, woff, (unsigned)step * 512u, base + (unsigned)(wave * BN * 4));
+        for_each_index([&](auto index) { load_one(index, yes, step, lds0 + (unsigned)(slot * L::STAGE)); }, std::make_integer_sequence<int, L::DPS>{});
     };
 
     f32x16 acc[L::TN][L::TM];
@@ -150,9 +227,8 @@ __global__ __launch_bounds__(256, BM * BN >= 256 * 256 ? 1 : 2) void k_linear(Li
     uint2 words[L::TN];
     const int xbase = (wm * L::WM + l32) * 128 + ((h ^ ((l32 >> 1) & 7)) * 16), wbase = L::ABYTES + wn * L::TN * 512 + lane * 8;
 
-    int issued = 0;
-    for (; issued < NS - 1 && issued < nk; ++issued) issue(issued, issued);
-    wait_groups<L::DPS>(issued - 1);
+    for (int s = 0; s < NS - 1 && s < nk; ++s) issue(s, s);
+    wait_groups<L::DPS>((nk < NS - 1 ? nk : NS - 1) - 1);
     block_barrier();
     int slot = 0;  // of the current step
 #pragma unroll
@@ -162,46 +238,66 @@ __global__ __launch_bounds__(256, BM * BN >= 256 * 256 ? 1 : 2) void k_linear(Li
 #pragma unroll
     for (int i = 0; i < L::TN; ++i) wf[0][i] = expand<0>(words[i]);
 
-    for (int step = 0; step < nk; ++step) {
-        int next = slot + 1 == NS ? 0 : slot + 1;
+    // STEADY: at least NS steps follow, so one more is loaded and no count depends on the step
+    auto one_step = [&](auto steady, int step) {
+        constexpr bool STEADY = decltype(steady)::value;
+        const int next = slot + 1 == NS ? 0 : slot + 1;
+        const unsigned fill = lds0 + (unsigned)((slot == 0 ? NS - 1 : slot - 1) * L::STAGE);
         auto slice = [&](auto index) {
             constexpr int j = decltype(index)::value, cur = j & 1, nxt = cur ^ 1;
             if constexpr (j == 3) {
                 // step + 1 has landed for this wave, then for all; and all are done with step - 1, whose slot is filled again
-                const int later = nk - 2 - step;
-                wait_groups<L::DPS>(later < NS - 3 ? later : NS - 3);
-                block_barrier();
-                if (issued < nk) {
-                    issue(issued, slot == 0 ? NS - 1 : slot - 1);
-                    ++issued;
+                if constexpr (STEADY) {
+                    wait_vm<(NS - 3) * L::DPS>();
+                } else {
+                    const int later = nk - 2 - step;
+                    wait_groups<L::DPS>(later < NS - 3 ? later : NS - 3);
                 }
+                block_barrier();
+                if (!STEADY && step + NS - 1 < nk) issue(step + NS - 1, slot == 0 ? NS - 1 : slot - 1);
             }
             const char* stage = smem + (j == 3 ? next : slot) * L::STAGE;
             uint2 ahead[L::TN];
-            if constexpr (j == 3) {
+            constexpr int NF = (j == 3 ? L::TN : 0) + L::TM, FPER = (NF + L::NM - 1) / L::NM;  // fragment reads, front-loaded
+            constexpr int ND = j == 3 && STEADY ? L::DPS : 0, DPER = (ND + L::NM - 1) / L::NM;
+            auto read = [&](int f) {
+                if (j == 3 && f < L::TN)
+                    ahead[f < L::TN ? f : 0] = *(const uint2*)(stage + wbase + f * 512);
+                else {
+                    const int i = j == 3 ? f - L::TN : f;
+                    xf[nxt][i] = *(const u32x4*)(stage + (xbase ^ (32 * ((j + 1) & 3))) + i * 4096);
+                }
+            };
+            auto widen = [&](int e) {
+                wf[nxt][e] = expand<(j + 1) & 3>(j == 3 ? ahead[e] : words[e]);
 #pragma unroll
-                for (int i = 0; i < L::TN; ++i) ahead[i] = *(const uint2*)(stage + wbase + i * 512);
-            }
-#pragma unroll
-            for (int i = 0; i < L::TM; ++i) xf[nxt][i] = *(const u32x4*)(stage + (xbase ^ (32 * ((j + 1) & 3))) + i * 4096);
-            __builtin_amdgcn_sched_barrier(0);
+                for (int r = 0; r < 4; ++r) {  // here, not where they are used: they would all sit in front of the next slice
+                    unsigned u = wf[nxt][e][r];
+                    pin(u);
+                    wf[nxt][e][r] = u;
+                }
+            };
             for_each_index(
                 [&](auto mi) {
                     constexpr int n = decltype(mi)::value, i = n / L::TM, k = n % L::TM;
                     acc[i][k] = T::mfma(wf[cur][i], xf[cur][k], acc[i][k]);
+#pragma unroll
+                    for (int f = n * FPER; f < (n + 1) * FPER && f < NF; ++f) read(f);
+                    for_each_index(
+                        [&](auto di) {
+                            constexpr int d = n * DPER + decltype(di)::value;
+                            if constexpr (d < ND) load_one(std::integral_constant<int, d>{}, no, step + NS - 1, fill);
+                        },
+                        std::make_integer_sequence<int, DPER>{});
                     // the next slice's weights, in the second half of this one's products
-                    constexpr int first = L::NM / 2, per = (L::NM - first) / L::TN > 0 ? (L::NM - first) / L::TN : 1;
-                    if constexpr (n >= first && (n - first) % per == 0 && (n - first) / per < L::TN) {
-                        constexpr int e = (n - first) / per;
-                        wf[nxt][e] = expand<(j + 1) & 3>(j == 3 ? ahead[e] : words[e]);
+                    constexpr int first = L::NM / 2, left = L::NM - first, per = (L::TN + left - 1) / left, every = left / L::TN > 0 ? left / L::TN : 1;
+                    if constexpr (n >= first && (n - first) % every == 0) {
+#pragma unroll
+                        for (int e = (n - first) / every * per; e < ((n - first) / every + 1) * per && e < L::TN; ++e) widen(e);
                     }
-                    if constexpr (L::NM > 2) __builtin_amdgcn_sched_barrier(0);
+                    __builtin_amdgcn_sched_barrier(0);
                 },
                 std::make_integer_sequence<int, L::NM>{});
-            if constexpr (L::NM / 2 + L::TN > L::NM) {
-#pragma unroll
-                for (int e = 0; e < L::TN; ++e) wf[nxt][e] = expand<(j + 1) & 3>(j == 3 ? ahead[e] : words[e]);
-            }
             if constexpr (j == 3) {
 #pragma unroll
                 for (int i = 0; i < L::TN; ++i) words[i] = ahead[i];
@@ -212,7 +308,10 @@ __global__ __launch_bounds__(256, BM * BN >= 256 * 256 ? 1 : 2) void k_linear(Li
         slice(std::integral_constant<int, 2>{});
         slice(std::integral_constant<int, 3>{});
         slot = next;
-    }
+    };
+    int step = 0;
+    for (; step < nk - NS; ++step) one_step(yes, step);
+    for (; step < nk; ++step) one_step(no, step);
 
     // ---- epilogue: 32 tokens of the wave's tile at a time through LDS, after which a lane has 8 outputs of TPL tokens
     __syncthreads();
@@ -220,7 +319,7 @@ __global__ __launch_bounds__(256, BM * BN >= 256 * 256 ? 1 : 2) void k_linear(Li
     char* zs = smem + wave * L::ZBYTES;
     const int n8 = n0 + wn * L::WN + (lane % CL) * 8, t0 = (lane / CL) * TPL;
     float al[8], bi[8];
-    load_affine<T>(p, n8, al, bi);
+    if (n8 < p.N) load_affine<T>(p, n8, al, bi);
 #pragma unroll 1
     for (int k = 0; k < L::TM; ++k) {
         auto put = [&](auto index) {
@@ -235,127 +334,129 @@ __global__ __launch_bounds__(256, BM * BN >= 256 * 256 ? 1 : 2) void k_linear(Li
         };
         for_each_index(put, std::make_integer_sequence<int, L::TM>{});
         const int mt = m0 + wm * L::WM + k * 32;  // first token
-        float z[TPL][8];
+        if (mt >= p.M || n0 + wn * L::WN >= p.N) continue;
+        const bool whole = mt + 32 <= p.M && n0 + (wn + 1) * L::WN <= p.N;
         wait_lgkm0();
-#pragma unroll
-        for (int t = 0; t < TPL; ++t) {
+        auto row_z = [&](int t, float(&z)[8]) {
             const float* row = (const float*)(zs + (t0 + t) * L::ZPITCH + (lane % CL) * 32);
             const float4 a = *(const float4*)row, b = *(const float4*)(row + 4);
             const float s[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[t][i] = fmaf(s[i], al[i], bi[i]);
-        }
-        if (mt >= p.M || n0 + wn * L::WN >= p.N) continue;
+            for (int i = 0; i < 8; ++i) z[i] = fmaf(s[i], al[i], bi[i]);
+        };
+        // R rows at a time: more of them would not fit beside the accumulators of a tile that shares its CU
+        constexpr int R = TPL < 4 ? TPL : 4;
         if (p.zq) {
-            const CkptShape cs(p.M, p.N);
-            unsigned am[8];
+            unsigned am[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll 1
+            for (int r = 0; r < TPL; r += R)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                am[i] = 0;
+                for (int t = 0; t < R; ++t) {
+                    float z[8];
+                    row_z(r + t, z);
 #pragma unroll
-                for (int t = 0; t < TPL; ++t) {
-                    const unsigned u = mt + t0 + t < p.M ? __float_as_uint(z[t][i]) & 0x7fffffffu : 0u;
-                    am[i] = u > am[i] ? u : am[i];
+                    for (int i = 0; i < 8; ++i) {
+                        const unsigned u = mt + t0 + r + t < p.M ? __float_as_uint(z[i]) & 0x7fffffffu : 0u;
+                        am[i] = u > am[i] ? u : am[i];
+                    }
                 }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int d = CL; d < 64; d *= 2) {
                     const unsigned o = (unsigned)__shfl_xor((int)am[i], d);
                     am[i] = o > am[i] ? o : am[i];
                 }
-            }
-            unsigned char ex[8];
-            float inv[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int e = ckpt_exponent<T>(__uint_as_float(am[i]));
-                ex[i] = (unsigned char)e;
-                inv[i] = ckpt_inverse(e);
-            }
+            const CkptScale<T> scale(am);
             if (n8 < p.N) {
-                const int64_t blk = (int64_t)(mt >> 5) * cs.cb + (n8 >> 3);
-                int8_t* out = p.zq + blk * 256 + t0 * 8;
+                if (t0 == 0) store_scales(p, mt, n8, scale);
+#pragma unroll 1
+                for (int r = 0; r < TPL; r += R) {
+                    float z[R][8];
 #pragma unroll
-                for (int t = 0; t < TPL; ++t) {
-                    unsigned w[2] = {0, 0};
+                    for (int t = 0; t < R; ++t) {
+                        row_z(r + t, z[t]);
+                        if (mt + t0 + r + t >= p.M)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const unsigned q = mt + t0 + t < p.M ? ckpt_code(z[t][i], inv[i]) : 0u;
-                        w[i >> 2] |= q << (8 * (i & 3));
+                            for (int i = 0; i < 8; ++i) z[t][i] = 0.f;
                     }
-                    *(uint2*)(out + t * 8) = make_uint2(w[0], w[1]);
-                }
-                if (t0 == 0) {
-                    uint2 e2;
-                    e2.x = ex[0] | ex[1] << 8 | ex[2] << 16 | (unsigned)ex[3] << 24;
-                    e2.y = ex[4] | ex[5] << 8 | ex[6] << 16 | (unsigned)ex[7] << 24;
-                    *(uint2*)(p.zq + cs.codes() + blk * 8) = e2;
+                    store_codes<T, R>(p, mt, t0 + r, n8, z, scale);
                 }
             }
         }
-        auto rows = [&](auto which) {
+        if (whole)
+            with_act(p.act, [&](auto which) {
+#pragma unroll 1
+                for (int r = 0; r < TPL; r += R)
 #pragma unroll
-            for (int t = 0; t < TPL; ++t) finish_row<T, decltype(which)::value>(p, mt + t0 + t, n8, z[t]);
-        };
-        if (p.act == kActNone)
-            rows(std::integral_constant<int, kActNone>{});
-        else if (p.act == kActRelu)
-            rows(std::integral_constant<int, kActRelu>{});
-        else if (p.act == kActGelu)
-            rows(std::integral_constant<int, kActGelu>{});
+                    for (int t = 0; t < R; ++t) {
+                        float z[8];
+                        row_z(r + t, z);
+                        finish_row<T, decltype(which)::value, true>(p, mt + t0 + r + t, n8, z);
+                    }
+            });
         else
-            rows(std::integral_constant<int, kActSilu>{});
+            with_act(p.act, [&](auto which) {
+#pragma unroll 1
+                for (int t = 0; t < TPL; ++t) {
+                    float z[8];
+                    row_z(t, z);
+                    finish_row<T, decltype(which)::value, false>(p, mt + t0 + t, n8, z);
+                }
+            });
         // (the next round's writes to `zs` are this wave's own and come after its reads)
     }
 }
 
-// Few tokens (at most 32 TT): a block has 32 outputs, its waves share the columns, the weights are read once and straight into
-// registers.  Bound by the weights' bytes and, for small layers, by the latency of one load after the launch.
-template <class T, int TT, int WAVES, bool VEC>
+// A few tokens: a block has 32 outputs, its waves share the columns, the weights are read once and x and weights go
+// straight into registers, BATCH steps' loads in flight at a time.  A load of x touches a cache line per token.
+template <class T, int WAVES, int BATCH, bool ROW16>
 __global__ __launch_bounds__(WAVES * 64) void k_linear_few(LinParams p)
 {
-    __shared__ float part[WAVES][TT][32][33];
+    __shared__ float part[WAVES][kFewTokens][36];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, h = lane >> 5;
     const int rb = blockIdx.x, n0 = rb * 32;
-    f32x16 acc[TT];
+    f32x16 acc;
 #pragma unroll
-    for (int t = 0; t < TT; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[t][r] = 0.f;
+    for (int r = 0; r < 16; ++r) acc[r] = 0.f;
     const uint2* w = (const uint2*)p.w + (int64_t)rb * p.nk * 64 + lane;
-    const unsigned short* xrow[TT];
+    const unsigned short* xrow = (const unsigned short*)p.x + (int64_t)l32 * p.ldx;
+    const bool mine = l32 < p.M;
+    auto load_x = [&](int k) {
+        u32x4 v = {0, 0, 0, 0};
+        if (mine) {
+            if (ROW16 ? k < p.K : k + 8 <= p.K) {
+                v = load16(xrow + k);
+            } else if (!ROW16) {
 #pragma unroll
-    for (int t = 0; t < TT; ++t) xrow[t] = (const unsigned short*)p.x + (int64_t)(t * 32 + l32) * p.ldx;
-    for (int step = wave; step < p.nk; step += WAVES) {
-        const uint2 word = w[(int64_t)step * 64];
-        auto slice = [&](auto index) {
-            constexpr int j = decltype(index)::value;
-            const int k = step * 64 + 16 * j + 8 * h;
-            const u32x4 wf = expand<j>(word);
-#pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                u32x4 xf = {0, 0, 0, 0};
-                if (t * 32 + l32 < p.M) {
-                    if constexpr (VEC) {
-                        if (k < p.K) xf = *(const u32x4*)(xrow[t] + k);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (k + i < p.K) xf[i >> 1] |= (unsigned)xrow[t][k + i] << (16 * (i & 1));
-                    }
-                }
-                acc[t] = T::mfma(wf, xf, acc[t]);
+                for (int i = 0; i < 8; ++i)
+                    if (k + i < p.K) v[i >> 1] |= (unsigned)xrow[k + i] << (16 * (i & 1));
             }
-        };
-        slice(std::integral_constant<int, 0>{});
-        slice(std::integral_constant<int, 1>{});
-        slice(std::integral_constant<int, 2>{});
-        slice(std::integral_constant<int, 3>{});
+        }
+        return v;
+    };
+    for (int s0 = wave; s0 < p.nk; s0 += WAVES * BATCH) {
+        uint2 word[BATCH];
+        u32x4 xf[BATCH][4];
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+            const int step = s0 + b * WAVES;
+            word[b] = step < p.nk ? w[(int64_t)step * 64] : make_uint2(0, 0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) xf[b][j] = load_x(step * 64 + 16 * j + 8 * h);  // (zeros from step nk on)
+        }
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+            acc = T::mfma(expand<0>(word[b]), xf[b][0], acc);
+            acc = T::mfma(expand<1>(word[b]), xf[b][1], acc);
+            acc = T::mfma(expand<2>(word[b]), xf[b][2], acc);
+            acc = T::mfma(expand<3>(word[b]), xf[b][3], acc);
+        }
     }
+    if (mine && l32 < kFewTokens)
 #pragma unroll
-    for (int t = 0; t < TT; ++t)
-        if (t * 32 + l32 < p.M)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) part[wave][t][l32][8 * (r >> 2) + 4 * h + (r & 3)] = acc[t][r];
+        for (int q = 0; q < 4; ++q)
+            *(float4*)&part[wave][l32][8 * q + 4 * h] = make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
     __syncthreads();
     for (int o = tid; o < p.M * 4; o += WAVES * 64) {  // 8 outputs of a token each
         const int m = o >> 2, c = (o & 3) * 8, n = n0 + c;
@@ -365,17 +466,151 @@ __global__ __launch_bounds__(WAVES * 64) void k_linear_few(LinParams p)
         for (int i = 0; i < 8; ++i) {
             float s = 0.f;
 #pragma unroll
-            for (int v = 0; v < WAVES; ++v) s += part[v][m >> 5][m & 31][c + i];
+            for (int v = 0; v < WAVES; ++v) s += part[v][m][c + i];
             z[i] = fmaf(s, al[i], bi[i]);
         }
-        if (p.act == kActNone)
-            finish_row<T, kActNone>(p, m, n, z);
-        else if (p.act == kActRelu)
-            finish_row<T, kActRelu>(p, m, n, z);
-        else if (p.act == kActGelu)
-            finish_row<T, kActGelu>(p, m, n, z);
-        else
-            finish_row<T, kActSilu>(p, m, n, z);
+        with_act(p.act, [&](auto which) { finish_row<T, decltype(which)::value, false>(p, m, n, z); });
+    }
+}
+
+template <int TT, int RB, int WAVES, int D>
+struct SplitTile {
+    static constexpr int XBYTES = TT * 4096, STAGE = XBYTES + RB * 512, DPS = TT * 4 + 1;
+    static constexpr int ZPITCH = RB * 128 + 16, ZBYTES = TT * 32 * ZPITCH;
+    static constexpr int WAVE = D * STAGE > ZBYTES ? D * STAGE : ZBYTES;
+    static constexpr int LDS = WAVES * WAVE + TT * RB * 128;
+};
+
+// Small grids: a block has 32 TT tokens x 32 RB outputs and its waves share the columns, every WAVES-th step each, with rings
+// of their own in LDS (D stages) and no barrier until their sums are added up in LDS.
+template <class T, int TT, int RB, int WAVES, int D>
+__global__ __launch_bounds__(WAVES * 64) void k_linear_split(LinParams p)
+{
+    using L = SplitTile<TT, RB, WAVES, D>;
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, h = lane >> 5;
+    const int nk = p.nk, tn = (int)blockIdx.x / p.tilesM, tm = (int)blockIdx.x - tn * p.tilesM;
+    const int m0 = tm * 32 * TT, n0 = tn * 32 * RB;
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem + (unsigned)(wave * L::WAVE);
+    char* ring = smem + wave * L::WAVE;
+    unsigned* amax = (unsigned*)(smem + WAVES * L::WAVE);  // [TT][32 RB]
+    if (tid < TT * RB * 32) amax[tid] = 0;
+
+    const v4i xr = buffer_base(p.x + (int64_t)m0 * p.ldx * 2), wr = buffer_base(p.w + (int64_t)(n0 / 32) * nk * 512);
+    unsigned xoff[TT * 4];
+#pragma unroll
+    for (int i = 0; i < TT * 4; ++i) {
+        const int row = i * 8 + (lane >> 3), last = p.M - 1 - m0;
+        xoff[i] = (unsigned)(row < last ? row : last) * (unsigned)(p.ldx * 2) + (unsigned)(((lane & 7) ^ ((row >> 1) & 7)) * 16);
+    }
+    unsigned woff;
+    {
+        const int last = p.rb - 1 - n0 / 32, r = lane >> 5;
+        woff = (unsigned)(r < last ? r : last) * (unsigned)(nk * 512) + (unsigned)((lane & 31) * 16);
+    }
+    const int ktail = p.K & 63;
+    auto issue = [&](int step, int slot) {
+        const unsigned base = lds0 + (unsigned)(slot * L::STAGE);
+        const bool end = ktail && step == nk - 1;  // chunks past the rows' ends are zeros
+        for_each_index(
+            [&](auto index) {
+                constexpr int i = decltype(index)::value;
+                const int row = i * 8 + (lane >> 3);
+                const unsigned v = end && ((lane & 7) ^ ((row >> 1) & 7)) * 8 >= ktail ? kOutside : xoff[i];
+                dma_buf<i * 1024>(xr, v, (unsigned)step * 128u, base);
+            },
+            std::make_integer_sequence<int, TT * 4>{});
+        if (lane < RB * 32) dma_buf<L::XBYTES>(wr, woff, (unsigned)step * 512u, base);
+    };
+
+    f32x16 acc[RB][TT];
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < TT; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    const int xbase = l32 * 128 + ((h ^ ((l32 >> 1) & 7)) * 16), wbase = L::XBYTES + lane * 8;
+    const int count = wave < nk ? (nk - wave + WAVES - 1) / WAVES : 0;
+    for (int i = 0; i < D && i < count; ++i) issue(wave + i * WAVES, i);
+    int slot = 0;
+    for (int i = 0; i < count; ++i) {
+        wait_groups<L::DPS>(count - 1 - i < D - 1 ? count - 1 - i : D - 1);
+        const char* stage = ring + slot * L::STAGE;
+        uint2 words[RB];
+        u32x4 xf[4][TT];
+#pragma unroll
+        for (int r = 0; r < RB; ++r) words[r] = *(const uint2*)(stage + wbase + r * 512);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int t = 0; t < TT; ++t) xf[j][t] = *(const u32x4*)(stage + (xbase ^ (32 * j)) + t * 4096);
+        wait_lgkm0();
+        if (i + D < count) issue(wave + (i + D) * WAVES, slot);
+        for_each_index(
+            [&](auto index) {
+                constexpr int j = decltype(index)::value;
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    const u32x4 wf = expand<j>(words[r]);
+#pragma unroll
+                    for (int t = 0; t < TT; ++t) acc[r][t] = T::mfma(wf, xf[j][t], acc[r][t]);
+                }
+            },
+            std::make_integer_sequence<int, 4>{});
+        slot = slot + 1 == D ? 0 : slot + 1;
+    }
+    // (this wave's ring is its own, and all of it has been read)
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *(float4*)(ring + (t * 32 + l32) * L::ZPITCH + (r * 32 + q * 8 + h * 4) * 4) =
+                    make_float4(acc[r][t][4 * q], acc[r][t][4 * q + 1], acc[r][t][4 * q + 2], acc[r][t][4 * q + 3]);
+    __syncthreads();
+    constexpr int GROUPS = RB * 4, ITEMS = TT * 32 * GROUPS, PER = (ITEMS + WAVES * 64 - 1) / (WAVES * 64);
+    float z[PER][8];
+#pragma unroll
+    for (int o = 0; o < PER; ++o) {
+        const int item = tid + o * WAVES * 64, g = item % GROUPS, t = item / GROUPS, n = n0 + g * 8;
+        if (item >= ITEMS) break;
+        float al[8], bi[8], s[8];
+        load_affine<T>(p, n, al, bi);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int v = 0; v < WAVES; ++v) {
+            const float* row = (const float*)(smem + v * L::WAVE + t * L::ZPITCH + g * 32);
+            const float4 a = *(const float4*)row, b = *(const float4*)(row + 4);
+            s[0] += a.x, s[1] += a.y, s[2] += a.z, s[3] += a.w, s[4] += b.x, s[5] += b.y, s[6] += b.z, s[7] += b.w;
+        }
+        const bool in = m0 + t < p.M;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[o][i] = in ? fmaf(s[i], al[i], bi[i]) : 0.f;
+        with_act(p.act, [&](auto which) { finish_row<T, decltype(which)::value, false>(p, m0 + t, n, z[o]); });
+        if (p.zq)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) atomicMax(&amax[(t >> 5) * (32 * RB) + g * 8 + i], __float_as_uint(z[o][i]) & 0x7fffffffu);
+    }
+    if (!p.zq) return;
+    __syncthreads();
+#pragma unroll
+    for (int o = 0; o < PER; ++o) {
+        const int item = tid + o * WAVES * 64, g = item % GROUPS, t = item / GROUPS, n = n0 + g * 8;
+        if (item >= ITEMS) break;
+        const int mt = m0 + (t & ~31);
+        unsigned am[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) am[i] = amax[(t >> 5) * (32 * RB) + g * 8 + i];
+        float zz[1][8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) zz[0][i] = z[o][i];
+        const CkptScale<T> scale(am);
+        if (mt >= p.M || n >= p.N) continue;
+        store_codes<T, 1>(p, mt, t & 31, n, zz, scale);
+        if ((t & 31) == 0) store_scales(p, mt, n, scale);
     }
 }
 
@@ -387,9 +622,13 @@ __global__ __launch_bounds__(256) void k_copy_rows(const unsigned short* x, int6
         const int64_t m = i / per, k = (i - m * per) * 8;
         const unsigned short* r = x + m * ldx + k;
         u32x4 v = {0, 0, 0, 0};
+        if (k + 8 <= K) {
+            v = load16(r);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (k + j < K) v[j >> 1] |= (unsigned)r[j] << (16 * (j & 1));
+            for (int j = 0; j < 8; ++j)
+                if (k + j < K) v[j >> 1] |= (unsigned)r[j] << (16 * (j & 1));
+        }
         *(u32x4*)(out + m * ld + k) = v;
     }
 }
@@ -413,14 +652,29 @@ hipError_t run_tile(LinParams& p, hipStream_t st)
     return hipGetLastError();
 }
 
-template <class T, int TT, int WAVES>
-hipError_t run_few(const LinParams& p, bool vec, hipStream_t st)
+template <class T, int WAVES, int BATCH>
+hipError_t run_few(const LinParams& p, hipStream_t st)
 {
     const unsigned grid = (unsigned)((p.N + 31) / 32);
-    if (vec)
-        k_linear_few<T, TT, WAVES, true><<<grid, WAVES * 64, 0, st>>>(p);
+    if (p.K % 8 == 0)
+        k_linear_few<T, WAVES, BATCH, true><<<grid, WAVES * 64, 0, st>>>(p);
     else
-        k_linear_few<T, TT, WAVES, false><<<grid, WAVES * 64, 0, st>>>(p);
+        k_linear_few<T, WAVES, BATCH, false><<<grid, WAVES * 64, 0, st>>>(p);
+    return hipGetLastError();
+}
+
+template <class T, int TT, int RB, int WAVES, int D>
+hipError_t run_split(LinParams& p, hipStream_t st)
+{
+    using L = SplitTile<TT, RB, WAVES, D>;
+    static_assert(L::LDS <= 160 * 1024, "");
+    p.tilesM = (p.M + 32 * TT - 1) / (32 * TT);
+    const int64_t nt = (int64_t)p.tilesM * ((p.N + 32 * RB - 1) / (32 * RB));
+    if (nt > 0x7fffff00) return hipErrorInvalidValue;
+    static LdsLimit limit;
+    const hipError_t e = limit.raise((const void*)&k_linear_split<T, TT, RB, WAVES, D>, L::LDS);
+    if (e != hipSuccess) return e;
+    k_linear_split<T, TT, RB, WAVES, D><<<(unsigned)nt, WAVES * 64, L::LDS, st>>>(p);
     return hipGetLastError();
 }
 
@@ -429,8 +683,8 @@ bool rows_of_16(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && 
 template <class T>
 hipError_t run(const LinearArgs& a, LinParams p, hipStream_t st)
 {
-    const bool vec = rows_of_16(a.x, a.ldx) && a.K % 8 == 0;
-    if (a.M <= kFewTokens && !a.zq) return p.nk >= 16 ? run_few<T, 1, 16>(p, vec, st) : run_few<T, 1, 4>(p, vec, st);
+    const LinearForm form = linear_form(a.M, a.N, a.K, a.zq != nullptr);
+    if (form == LinearForm::kFew) return p.nk >= 16 ? run_few<T, 16, 4>(p, st) : run_few<T, 4, 4>(p, st);
     if (linear_copies_x(a)) {
         const int64_t ld = (a.K + 63) / 64 * 64, blocks = (a.M * ld / 8 + 255) / 256;
         k_copy_rows<<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, st>>>((const unsigned short*)a.x, a.ldx, a.M, a.K, ld, (unsigned short*)a.workspace);
@@ -440,17 +694,20 @@ hipError_t run(const LinearArgs& a, LinParams p, hipStream_t st)
         p.ldx = ld;
         p.K = (int)ld;
     }
-    const int64_t t256 = ((a.M + 255) / 256) * ((a.N + 255) / 256), t128 = ((a.M + 127) / 128) * ((a.N + 127) / 128);
-    if (t256 >= 192) return run_tile<T, 256, 256, 4>(p, st);
-    if (t128 >= 192) return run_tile<T, 128, 128, 4>(p, st);
-    return run_tile<T, 64, 64, 4>(p, st);
+    switch (form) {
+        case LinearForm::kSplit32: return run_split<T, 1, 1, 8, 4>(p, st);
+        case LinearForm::kSplit32x64: return run_split<T, 1, 2, 8, 3>(p, st);
+        case LinearForm::kSplit64: return run_split<T, 2, 2, 8, 2>(p, st);
+        case LinearForm::kTile128: return run_tile<T, 128, 128, 4>(p, st);
+        default: return run_tile<T, 128, 256, 4>(p, st);
+    }
 }
 
 }  // namespace
 
 bool linear_copies_x(const LinearArgs& a)
 {
-    if (a.M <= kFewTokens && !a.zq) return false;
+    if (linear_form(a.M, a.N, a.K, a.zq != nullptr) == LinearForm::kFew) return false;
     return !rows_of_16(a.x, a.ldx) || a.K % 8 != 0 || 256 * a.ldx * 2 + a.K * 2 >= (int64_t)kOutside;
 }
 
@@ -467,7 +724,6 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t st)
     p.y = (unsigned short*)a.y;
     p.zq = a.zq;
     p.act = a.act;
-    p.vec_y = rows_of_16(a.y, a.ldy), p.vec_r = rows_of_16(a.res, a.ldr);
     return a.f16 ? run<F16>(a, p, st) : run<BF16>(a, p, st);
 }
 

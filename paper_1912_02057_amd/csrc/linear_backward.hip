@@ -14,28 +14,28 @@ namespace {
 
 struct WgParams {
     const char *x, *d;  // x^ and dz in operand order
-    int N, K, nk;       // nk: blocks of 32 tokens
+    int N, K, nk;       // nk: steps of 64 tokens
     int64_t xpitch, dpitch;  // bytes from one block of tokens to the next
     int tilesN, ntiles, band_tiles;
     FastDiv div_band, div_lastband;
     void* dw;
-    int vec;
 };
 
-template <int BN, int BK, int NS>
+template <int BN, int BK>
 struct WgTile {
     static constexpr int WN = BN / 2, WK = BK / 2, TN = WN / 32, TK = WK / 32, NM = TN * TK;
-    static constexpr int XBYTES = BK * 64, STAGE = XBYTES + BN * 64, XDMA = BK / 64, DDMA = BN / 64, DPS = XDMA + DDMA;  // 1 KiB / wave
+    // a stage: two blocks of 32 tokens, x^ before dz in each; a wave's loads of 1 KiB
+    static constexpr int XBYTES = BK * 64, HALF = XBYTES + BN * 64, STAGE = 2 * HALF, XDMA = BK / 64, DDMA = BN / 64, DPS = 2 * (XDMA + DDMA);
     static constexpr int ZPITCH = WK * 4 + 16, ZBYTES = 32 * ZPITCH;
-    static constexpr int LDS = NS * STAGE > 4 * ZBYTES ? NS * STAGE : 4 * ZBYTES;
+    static constexpr int LDS = 2 * STAGE > 4 * ZBYTES ? 2 * STAGE : 4 * ZBYTES;
 };
 
-// A block of 4 waves (2 x 2) owns BN x BK of dw; a ring of NS stages of 32 tokens, a barrier per stage before the second
-// of its two 16-token slices, fragments read one slice ahead.
-template <class T, int BN, int BK, int NS, bool F32>
+// A block of 4 waves (2 x 2) owns BN x BK of dw.  Two stages of 64 tokens; fragments are read one 16-token slice ahead, so that
+// before the last slice of a step nothing is left to read of its stage: behind the one barrier there it is filled again.
+template <class T, int BN, int BK, bool F32>
 __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgParams p)
 {
-    using L = WgTile<BN, BK, NS>;
+    using L = WgTile<BN, BK>;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wn = wave >> 1, wk = wave & 1, l32 = lane & 31, h = lane >> 5;
@@ -50,23 +50,19 @@ __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgP
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
     const char* xg = p.x + (int64_t)(k0 / 32) * 2048 + wave * L::XDMA * 1024;
     const char* dg = p.d + (int64_t)(n0 / 32) * 2048 + wave * L::DDMA * 1024;
+    // load i of a step whose operands start at xs, ds; the second 32 tokens lie a pitch (below 2^32 bytes) further on
+    const unsigned voff = (unsigned)lane * 16u;
+    auto load_one = [&](auto index, const int8_t* xs, const int8_t* ds, unsigned base) {
+        constexpr int i = decltype(index)::value, half = i / (L::XDMA + L::DDMA), j = i % (L::XDMA + L::DDMA);
+        if constexpr (j < L::XDMA)
+            dma16_base<half * L::HALF + j * 1024>(xs + (half ? p.xpitch : 0), voff + j * 1024, base + (unsigned)(wave * L::XDMA * 1024));
+        else
+            dma16_base<half * L::HALF + L::XBYTES + (j - L::XDMA) * 1024>(ds + (half ? p.dpitch : 0), voff + (j - L::XDMA) * 1024,
+                                                                          base + (unsigned)(wave * L::DDMA * 1024));
+    };
     auto issue = [&](int step, int slot) {
-        const unsigned base = lds0 + (unsigned)(slot * L::STAGE);
-        const int8_t* xs = uniform_ptr((const int8_t*)xg + step * p.xpitch);
-        const int8_t* ds = uniform_ptr((const int8_t*)dg + step * p.dpitch);
-        asm volatile("s_nop 4" : "+s"(xs), "+s"(ds));  // five wait states: they may just have left vector registers
-        for_each_index(
-            [&](auto index) {
-                constexpr int i = decltype(index)::value;
-                dma16_base<i * 1024>(xs, (unsigned)(lane * 16 + i * 1024), base + (unsigned)(wave * L::XDMA * 1024));
-            },
-            std::make_integer_sequence<int, L::XDMA>{});
-        for_each_index(
-            [&](auto index) {
-                constexpr int i = decltype(index)::value;
-                dma16_base<L::XBYTES + i * 1024>(ds, (unsigned)(lane * 16 + i * 1024), base + (unsigned)(wave * L::DDMA * 1024));
-            },
-            std::make_integer_sequence<int, L::DDMA>{});
+        const int8_t *xs = (const int8_t*)xg + step * (2 * p.xpitch), *ds = (const int8_t*)dg + step * (2 * p.dpitch);
+        for_each_index([&](auto index) { load_one(index, xs, ds, lds0 + (unsigned)(slot * L::STAGE)); }, std::make_integer_sequence<int, L::DPS>{});
     };
 
     f32x16 acc[L::TK][L::TN];
@@ -79,52 +75,69 @@ __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgP
     u32x4 xf[2][L::TK], df[2][L::TN];
     const int xbase = wk * L::TK * 2048 + lane * 16, dbase = L::XBYTES + wn * L::TN * 2048 + lane * 16;
 
-    int issued = 0;
-    for (; issued < NS - 1 && issued < nk; ++issued) issue(issued, issued);
-    wait_groups<L::DPS>(issued - 1);
+    if (nk > 0) issue(0, 0);
+    if (nk > 1) issue(1, 1);
+    if (nk > 1)
+        wait_vm<L::DPS>();
+    else
+        wait_vm<0>();
     block_barrier();
-    int slot = 0;
 #pragma unroll
     for (int i = 0; i < L::TK; ++i) xf[0][i] = *(const u32x4*)(smem + xbase + i * 2048);
 #pragma unroll
     for (int i = 0; i < L::TN; ++i) df[0][i] = *(const u32x4*)(smem + dbase + i * 2048);
 
-    for (int step = 0; step < nk; ++step) {
-        const int next = slot + 1 == NS ? 0 : slot + 1;
+    const std::true_type yes{};
+    const std::false_type no{};
+    int slot = 0;
+    // MORE: two steps follow, the later of which is loaded
+    auto one_step = [&](auto more, int step) {
+        constexpr bool MORE = decltype(more)::value;
+        const int8_t *xs = (const int8_t*)xg + (step + 2) * (2 * p.xpitch), *ds = (const int8_t*)dg + (step + 2) * (2 * p.dpitch);
+        const unsigned fill = lds0 + (unsigned)(slot * L::STAGE);
         auto slice = [&](auto index) {
-            constexpr int j = decltype(index)::value, cur = j, nxt = j ^ 1;
-            if constexpr (j == 1) {
-                // step + 1 has landed for this wave, then for all; and all are done with step - 1, whose slot is filled again
-                const int later = nk - 2 - step;
-                wait_groups<L::DPS>(later < NS - 3 ? later : NS - 3);
+            constexpr int j = decltype(index)::value, cur = j & 1, nxt = cur ^ 1;
+            if constexpr (j == 3) {
+                wait_vm<0>();   // the next step has landed,
+                wait_lgkm0();   // and this wave has read all of the present one
                 block_barrier();
-                if (issued < nk) {
-                    issue(issued, slot == 0 ? NS - 1 : slot - 1);
-                    ++issued;
-                }
             }
-            const char* stage = smem + (j == 1 ? next : slot) * L::STAGE + (j == 0 ? 1024 : 0);
+            const char* stage = smem + (j == 3 ? slot ^ 1 : slot) * L::STAGE + ((j + 1) & 2 ? L::HALF : 0) + ((j + 1) & 1) * 1024;
             for_each_index(
                 [&](auto mi) {
                     constexpr int n = decltype(mi)::value, i = n / L::TN, k = n % L::TN;
+                    acc[i][k] = T::mfma(xf[cur][i], df[cur][k], acc[i][k]);
                     // the next slice's fragments, early in this one's products
                     constexpr int NF = L::TK + L::TN, PER = (NF + L::NM - 1) / L::NM;
 #pragma unroll
                     for (int f = n * PER; f < (n + 1) * PER && f < NF; ++f) {
                         if (f < L::TK)
-                            xf[nxt][f] = *(const u32x4*)(stage + xbase + f * 2048);
+                            xf[nxt][f < L::TK ? f : 0] = *(const u32x4*)(stage + xbase + f * 2048);
                         else
-                            df[nxt][f - L::TK] = *(const u32x4*)(stage + dbase + (f - L::TK) * 2048);
+                            df[nxt][f < L::TK ? 0 : f - L::TK] = *(const u32x4*)(stage + dbase + (f - L::TK) * 2048);
                     }
-                    acc[i][k] = T::mfma(xf[cur][i], df[cur][k], acc[i][k]);
-                    if constexpr (L::NM > 2) __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (j == 3 && MORE) {
+                        constexpr int DPER = (L::DPS + L::NM - 1) / L::NM;
+                        for_each_index(
+                            [&](auto di) {
+                                constexpr int d = n * DPER + decltype(di)::value;
+                                if constexpr (d < L::DPS) load_one(std::integral_constant<int, d>{}, xs, ds, fill);
+                            },
+                            std::make_integer_sequence<int, DPER>{});
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 },
                 std::make_integer_sequence<int, L::NM>{});
         };
         slice(std::integral_constant<int, 0>{});
         slice(std::integral_constant<int, 1>{});
-        slot = next;
-    }
+        slice(std::integral_constant<int, 2>{});
+        slice(std::integral_constant<int, 3>{});
+        slot ^= 1;
+    };
+    int step = 0;
+    for (; step < nk - 2; ++step) one_step(yes, step);
+    for (; step < nk; ++step) one_step(no, step);
 
     __syncthreads();
     constexpr int CL = L::WK / 8, TPL = CL / 2;
@@ -155,9 +168,8 @@ __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgP
             const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
             if constexpr (F32) {
                 float* o = (float*)p.dw + (int64_t)n * p.K + k8;
-                if (p.vec && k8 + 8 <= p.K) {
-                    *(float4*)o = a;
-                    *(float4*)(o + 4) = b;
+                if (k8 + 8 <= p.K) {
+                    __builtin_memcpy(o, v, 32);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
@@ -165,8 +177,9 @@ __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgP
                 }
             } else {
                 unsigned short* o = (unsigned short*)p.dw + (int64_t)n * p.K + k8;
-                if (p.vec && k8 + 8 <= p.K) {
-                    *(u32x4*)o = u32x4{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])};
+                if (k8 + 8 <= p.K) {
+                    const u32x4 q = {pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])};
+                    __builtin_memcpy(o, &q, 16);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
@@ -177,10 +190,10 @@ __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgP
     }
 }
 
-template <class T, int BN, int BK, int NS, bool F32>
+template <class T, int BN, int BK, bool F32>
 hipError_t run_tile(WgParams& p, hipStream_t st)
 {
-    using L = WgTile<BN, BK, NS>;
+    using L = WgTile<BN, BK>;
     p.tilesN = (p.N + BN - 1) / BN;
     const int tilesK = (p.K + BK - 1) / BK;
     const int64_t nt = (int64_t)p.tilesN * tilesK;
@@ -190,9 +203,9 @@ hipError_t run_tile(WgParams& p, hipStream_t st)
     p.div_band = make_fastdiv((uint32_t)p.band_tiles);
     p.div_lastband = make_fastdiv((uint32_t)(p.tilesN % 8 ? p.tilesN % 8 : 8));
     static LdsLimit limit;
-    const hipError_t e = limit.raise((const void*)&k_wgrad<T, BN, BK, NS, F32>, L::LDS);
+    const hipError_t e = limit.raise((const void*)&k_wgrad<T, BN, BK, F32>, L::LDS);
     if (e != hipSuccess) return e;
-    k_wgrad<T, BN, BK, NS, F32><<<(unsigned)((nt + 7) / 8 * 8), 256, L::LDS, st>>>(p);
+    k_wgrad<T, BN, BK, F32><<<(unsigned)((nt + 7) / 8 * 8), 256, L::LDS, st>>>(p);
     return hipGetLastError();
 }
 
@@ -200,9 +213,9 @@ template <class T, bool F32>
 hipError_t run(WgParams& p, hipStream_t st)
 {
     const int64_t t256 = (int64_t)((p.N + 255) / 256) * ((p.K + 255) / 256), t128 = (int64_t)((p.N + 127) / 128) * ((p.K + 127) / 128);
-    if (t256 >= 192) return run_tile<T, 256, 256, 4, F32>(p, st);
-    if (t128 >= 192) return run_tile<T, 128, 128, 4, F32>(p, st);
-    return run_tile<T, 64, 64, 4, F32>(p, st);
+    if (t256 >= 192) return run_tile<T, 256, 256, F32>(p, st);
+    if (t128 >= 192) return run_tile<T, 128, 128, F32>(p, st);
+    return run_tile<T, 64, 64, F32>(p, st);
 }
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
@@ -210,7 +223,7 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 // Runs of token blocks whose sums of dz are kept apart: few for a long batch, one block each while there are few waves.
 int64_t blocks_per_run(int64_t M, int64_t N)
 {
-    const int64_t units = (M + 31) / 32 * ((N + 127) / 128);
+    const int64_t units = operand_blocks(M) * ((N + 127) / 128);
     return units >= 8 * 4096 ? 8 : units >= 2 * 4096 ? 2 : 1;
 }
 
@@ -222,7 +235,7 @@ struct BwdWork {
         dzt = dza + round_up(M * round_up(N, 64) * 2, 256);
         xt = dzt + operand_bytes(M, N);
         part = xt + operand_bytes(M, K);
-        const int64_t tb = (M + 31) / 32, per = blocks_per_run(M, N);
+        const int64_t tb = operand_blocks(M), per = blocks_per_run(M, N);
         total = part + round_up((tb + per - 1) / per * N * 4, 256);
     }
 };
@@ -233,10 +246,9 @@ hipError_t launch_linear_wgrad(const WgradArgs& a, hipStream_t st)
 {
     WgParams p = {};
     p.x = a.xt, p.d = a.dzt;
-    p.N = (int)a.N, p.K = (int)a.K, p.nk = (int)((a.M + 31) / 32);
+    p.N = (int)a.N, p.K = (int)a.K, p.nk = (int)((a.M + 63) / 64);
     p.xpitch = (a.K + 31) / 32 * 2048, p.dpitch = (a.N + 31) / 32 * 2048;
     p.dw = a.dw;
-    p.vec = ((uintptr_t)a.dw & 15) == 0 && a.K % 8 == 0;
     if (a.f16) return a.dw_f32 ? run<F16, true>(p, st) : run<F16, false>(p, st);
     return a.dw_f32 ? run<BF16, true>(p, st) : run<BF16, false>(p, st);
 }
@@ -276,7 +288,7 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t st)
         if ((e = launch_linear_wgrad(d, st)) != hipSuccess) return e;
     }
     if (a.dbias) {
-        const int64_t tb = (a.M + 31) / 32;
+        const int64_t tb = operand_blocks(a.M);
         if ((e = launch_bias_sum(g.part, (tb + g.per - 1) / g.per, a.N, a.dbias, a.f16, st)) != hipSuccess) return e;
     }
     return hipSuccess;

@@ -701,7 +701,7 @@ size_t rtn_linear_workspace_bytes(const void* x, int64_t ldx, int64_t M, int64_t
 {
     if (!linear_dims(1, K) || M <= 0 || M > kMaxDim || ldx < K) return 0;
     rtn::LinearArgs a = {};
-    a.x = x, a.M = M, a.K = K, a.ldx = ldx;
+    a.x = x, a.M = M, a.N = 1, a.K = K, a.ldx = ldx;  // (what is asked here does not depend on N)
     a.zq = keeps_z ? (int8_t*)16 : nullptr;
     return rtn::linear_copies_x(a) ? (size_t)M * (size_t)((K + 63) / 64 * 128) : 0;
 }

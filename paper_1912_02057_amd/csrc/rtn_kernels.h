@@ -276,7 +276,6 @@ struct GradArgs {
     int64_t per;
     // set by launch_linear_grad
     int64_t dz_strips, dz_units, x_strips, x_units;
-    int vec_dy;
 };
 hipError_t launch_linear_grad(GradArgs a, int f16, hipStream_t st);
 hipError_t launch_bias_sum(const float* part, int64_t runs, int64_t N, void* out, int f16, hipStream_t st);

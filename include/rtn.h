@@ -444,8 +444,8 @@ int rtn_epilogue_reparam_conv2d(const int32_t *acc, int64_t Nb, int64_t C, int64
  * act: RTN_ACT_NONE, RTN_ACT_RELU, RTN_ACT_GELU (z times the normal distribution function), RTN_ACT_SILU (z / (1 + exp(-z))).
  * M = 0 is a call with nothing to do.  N, K <= 2^21, pitches <= 2^31, 2-byte aligned; rows of 16-byte units
  * (pointer 16-byte aligned, pitch and row length multiples of 8 elements) are read and written fastest.
- * workspace: rtn_linear_workspace_bytes() of the same x, ldx, M, K and z_ckpt != NULL, 0 wherever rows can be read where they
- * lie; 16-byte aligned.
+ * workspace: rtn_linear_workspace_bytes() of the same x, ldx, M, N, K and z_ckpt != NULL, 0 wherever rows can be read where
+ * they lie; 16-byte aligned.
  * z_ckpt (nullable): receives the 8-bit checkpoint (below) of z, for rtn_linear_backward: rtn_checkpoint_bytes(M, N) bytes. */
 typedef enum { RTN_BF16 = 0, RTN_F16 = 1, RTN_F32 = 2 } rtn_dtype;
 typedef enum { RTN_ACT_NONE = 0, RTN_ACT_RELU = 1, RTN_ACT_GELU = 2, RTN_ACT_SILU = 3 } rtn_act;
@@ -458,7 +458,7 @@ typedef enum { RTN_ACT_NONE = 0, RTN_ACT_RELU = 1, RTN_ACT_GELU = 2, RTN_ACT_SIL
 size_t rtn_linear_prepared_bytes(int64_t N, int64_t K);
 int rtn_linear_prepare(rtn_code_format fmt, const void *w_codes, int64_t N, int64_t K, void *prepared,
                        size_t prepared_bytes, void *prepared_t, size_t prepared_t_bytes, void *stream);
-size_t rtn_linear_workspace_bytes(const void *x, int64_t ldx, int64_t M, int64_t K, int keeps_z);
+size_t rtn_linear_workspace_bytes(const void *x, int64_t ldx, int64_t M, int64_t N, int64_t K, int keeps_z);
 int rtn_linear(rtn_dtype dt, const void *x, int64_t ldx, const void *prepared, int64_t M, int64_t N, int64_t K,
                const float *alpha_w, rtn_gran gran_w, const void *bias, rtn_act act, const void *residual, int64_t ldr,
                void *y, int64_t ldy, void *z_ckpt, size_t z_ckpt_bytes, void *workspace, size_t workspace_bytes,

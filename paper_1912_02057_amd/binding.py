@@ -144,7 +144,7 @@ def lib():
         L.rtn_linear_prepare.restype = ci
         L.rtn_linear_prepare.argtypes = [ci, vp, i64, i64, vp, sz, vp, sz, vp]
         L.rtn_linear_workspace_bytes.restype = sz
-        L.rtn_linear_workspace_bytes.argtypes = [vp, i64, i64, i64, ci]
+        L.rtn_linear_workspace_bytes.argtypes = [vp, i64, i64, i64, i64, ci]
         L.rtn_linear.restype = ci
         L.rtn_linear.argtypes = [ci, vp, i64, vp, i64, i64, i64, vp, ci, vp, ci, vp, i64, vp, i64, vp, sz, vp, sz, vp]
         L.rtn_checkpoint_bytes.restype = sz
@@ -531,33 +531,25 @@ def ternary_depthwise_conv2d(a_codes, w_codes, Nb, Cc, H, W, KH, KW, stride, pad
     return acc_out, y_out
 
 
+def _made(r, where):
+    """The outputs of a native call that allocates them, which returns the status where there are none."""
+    if type(r) is int:
+        _check(r, where)
+    return r
+
+
 def linear_prepare(w_codes, N, K, fmt=RTN_CODE_I8, backward=False):
     """Weights of the ternary linear layer from codes [N, Kpad] in format fmt (as ternarize_pack returns them), in the order
     its products take: the buffer linear() reads, and with backward=True also the one linear_backward() reads."""
-    _check_codes(w_codes, N, K, fmt, "w_codes")
-    dev = w_codes.device
-    w = torch.empty(lib().rtn_linear_prepared_bytes(N, K), dtype=torch.uint8, device=dev)
-    wt = torch.empty(lib().rtn_linear_prepared_bytes(K, N), dtype=torch.uint8, device=dev) if backward else None
-    rc = lib().rtn_linear_prepare(fmt, w_codes.data_ptr(), N, K, w.data_ptr(), w.numel(), None if wt is None else wt.data_ptr(),
-                                  0 if wt is None else wt.numel(), _stream())
-    _check(rc, "rtn_linear_prepare")
-    return (w, wt) if backward else w
+    r = _made(_native().linear_prepare(w_codes, N, K, fmt, backward), "rtn_linear_prepare")
+    return r if backward else r[0]
 
 
 def linear(x, prepared, N, alpha_w, bias=None, act=RTN_ACT_NONE, residual=None, y_out=None, z_ckpt=None, workspace=None):
     """y = act(alpha_w * (x t^T) + bias) + residual: x cuda bfloat16 / float16 [M, K] (rows may lie apart), prepared from
     linear_prepare(), alpha_w a python float or cuda float32 [N], bias [N] and residual [M, N] in x's type.  z_ckpt, from
     checkpoint_empty(M, N), receives the 8-bit checkpoint of the value before the activation.  Returns y [M, N]."""
-    M, K = x.shape
-    if y_out is None:
-        y_out = torch.empty((M, N), dtype=x.dtype, device=x.device)
-    if workspace is None:
-        need = lib().rtn_linear_workspace_bytes(x.data_ptr(), x.stride(0) if M > 1 else K, M, K, z_ckpt is not None)
-        if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
-    rc = _native().linear(x, prepared, M, N, K, alpha_w, bias, act, residual, y_out, z_ckpt, workspace)
-    _check(rc, "rtn_linear")
-    return y_out
+    return _made(_native().linear(x, prepared, N, alpha_w, bias, act, residual, y_out, z_ckpt, workspace), "rtn_linear")
 
 
 def checkpoint_empty(M, Cc, device="cuda"):
@@ -567,18 +559,15 @@ def checkpoint_empty(M, Cc, device="cuda"):
 
 def checkpoint_pack(x, ckpt=None):
     """8-bit checkpoint of x, cuda bfloat16 / float16 [M, C] (rows may lie apart)."""
-    if ckpt is None:
-        ckpt = checkpoint_empty(x.shape[0], x.shape[1], x.device)
-    _check(_native().checkpoint(x, ckpt, True), "rtn_checkpoint_pack")
-    return ckpt
+    return _made(_native().checkpoint_pack(x, ckpt), "rtn_checkpoint_pack")
 
 
 def checkpoint_unpack(ckpt, M, Cc, dtype, out=None):
     """What the checkpoint of an [M, Cc] tensor stands for, in bfloat16 or float16."""
     if out is None:
         out = torch.empty((M, Cc), dtype=dtype, device=ckpt.device)
-    _check(_native().checkpoint(out, ckpt, False), "rtn_checkpoint_unpack")
-    return out
+    assert tuple(out.shape) == (M, Cc) and out.dtype == dtype
+    return _made(_native().checkpoint_unpack(ckpt, out), "rtn_checkpoint_unpack")
 
 
 def linear_backward(dy, prepared_t, K, alpha_w, x_ckpt, act=RTN_ACT_NONE, z_ckpt=None, want_dx=True, want_dw=True, want_dbias=True,
@@ -586,16 +575,6 @@ def linear_backward(dy, prepared_t, K, alpha_w, x_ckpt, act=RTN_ACT_NONE, z_ckpt
     """Gradients of linear() from dy [M, N] (rows may lie apart) and the checkpoints of its input and, unless act is
     RTN_ACT_NONE, of its value before the activation.  Returns (dx [M, K], dw [N, K], dbias [N]) or None in the place of
     what is not wanted; dw, the gradient of alpha_w * t, is of dy's type or dw_dtype=torch.float32."""
-    M, N = dy.shape
-    dev = dy.device
-    if want_dx and dx is None:
-        dx = torch.empty((M, K), dtype=dy.dtype, device=dev)
-    if want_dw and dw is None:
-        dw = torch.empty((N, K), dtype=dw_dtype or dy.dtype, device=dev)
-    if want_dbias and dbias is None:
-        dbias = torch.empty(N, dtype=dy.dtype, device=dev)
-    if workspace is None:
-        workspace = torch.empty(lib().rtn_linear_backward_workspace_bytes(M, N, K), dtype=torch.uint8, device=dev)
-    rc = _native().linear_backward(dy, x_ckpt, z_ckpt, act, prepared_t, M, N, K, alpha_w, dx, dw, dbias, workspace)
-    _check(rc, "rtn_linear_backward")
-    return dx, dw, dbias
+    assert dw_dtype in (None, dy.dtype, torch.float32)
+    return _made(_native().linear_backward(dy, prepared_t, K, alpha_w, x_ckpt, act, z_ckpt, want_dx, want_dw, want_dbias,
+                                           dw_dtype is torch.float32, dx, dw, dbias, workspace), "rtn_linear_backward")

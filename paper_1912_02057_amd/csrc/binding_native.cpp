@@ -7,7 +7,8 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
-#include <ATen/core/TensorBase.h>
+#include <ATen/core/Tensor.h>
+#include <ATen/ops/empty.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -317,17 +318,45 @@ PyObject* weight_backward(PyObject*, Args a, Py_ssize_t n)
     });
 }
 
-// Row pitch of a [rows][len] device tensor of type `type` whose rows are dense; its data pointer.  None -> NULL.
-void* rows2d(PyObject* o, c10::ScalarType type, int64_t rows, int64_t len, const char* what, int64_t& ld)
+// Bytes or a matrix on the device of `like`.
+at::Tensor make_bytes(size_t n, const at::Tensor& like) { return at::empty({(int64_t)n}, like.options().dtype(c10::kByte)); }
+at::Tensor make_rows(int64_t rows, int64_t cols, c10::ScalarType type, const at::Tensor& like)
 {
-    ld = len;
-    if (o == Py_None) return nullptr;
-    const at::Tensor& t = tensor(o, what);
+    return at::empty({rows, cols}, like.options().dtype(type));
+}
+// `given`, or what `make` allocates where it is None
+template <class F>
+at::Tensor given_or(PyObject* given, const char* what, F make)
+{
+    return given == Py_None ? make() : tensor(given, what);
+}
+void* rows2d(const at::Tensor& t, c10::ScalarType type, int64_t rows, int64_t len, const char* what, int64_t& ld)
+{
     if (!t.is_cuda() || t.scalar_type() != type || t.dim() != 2 || t.size(0) != rows || t.size(1) != len ||
         (len > 1 && t.stride(1) != 1))
         fail(PyExc_AssertionError, "%s: a device tensor of the documented type and shape, its rows dense, is required", what);
-    if (rows > 1) ld = t.stride(0);
+    ld = rows > 1 ? t.stride(0) : len;
     return t.data_ptr();
+}
+void* bytes_of(const at::Tensor& t, size_t need, const char* what)
+{
+    if (!(t.is_cuda() && t.is_contiguous() && t.nbytes() >= need)) {
+        PyErr_Format(PyExc_ValueError, "%s: a device buffer of %zu bytes is required", what, need);
+        throw PyError();
+    }
+    return t.data_ptr();
+}
+void* rows2d(PyObject* o, c10::ScalarType type, int64_t rows, int64_t len, const char* what, int64_t& ld)
+{
+    ld = len;
+    return o == Py_None ? nullptr : rows2d(tensor(o, what), type, rows, len, what, ld);
+}
+void* bytes_of(PyObject* o, size_t need, const char* what) { return o == Py_None ? nullptr : bytes_of(tensor(o, what), need, what); }
+void* vector_of(PyObject* o, c10::ScalarType type, int64_t n, const char* what)
+{
+    void* p = dev(o, type, what);
+    if (p && tensor(o, what).numel() != n) fail(PyExc_AssertionError, "%s: one entry per output is required", what);
+    return p;
 }
 rtn_dtype dtype(c10::ScalarType t, const char* what, bool f32 = false)
 {
@@ -336,94 +365,153 @@ rtn_dtype dtype(c10::ScalarType t, const char* what, bool f32 = false)
     if (!f32 || t != c10::kFloat) fail(PyExc_AssertionError, "%s: bfloat16 or float16 is required", what);
     return RTN_F32;
 }
-// A buffer of bytes on the device that holds at least `need`.
-void* bytes_of(PyObject* o, size_t need, const char* what)
+const at::Tensor& matrix(PyObject* o, const char* what)
 {
-    if (o == Py_None) return nullptr;
     const at::Tensor& t = tensor(o, what);
-    if (!(t.is_cuda() && t.is_contiguous() && t.nbytes() >= need)) {
-        PyErr_Format(PyExc_ValueError, "%s: a device buffer of %zu bytes is required", what, need);
-        throw PyError();
+    if (!t.is_cuda() || t.dim() != 2) fail(PyExc_AssertionError, "%s: a matrix on the device is required", what);
+    return t;
+}
+struct AlphaN : Gran {
+    AlphaN(PyObject* o, int64_t n) : Gran(o, "alpha_w")
+    {
+        if (gran == RTN_VECTOR && tensor(o, "alpha_w").numel() != n) fail(PyExc_AssertionError, "%s: one entry per output is required", "alpha_w");
     }
-    return t.data_ptr();
+};
+
+// Runs `f`, which returns a status and leaves its outputs; on RTN_OK the outputs are the result (one, or a tuple with None for
+// what is undefined), else the status.
+template <int N, class F>
+PyObject* call_for(Py_ssize_t want, Py_ssize_t n, F f)
+{
+    at::Tensor out[N];
+    PyObject* status = call(want, n, [&] { return f(out); });
+    if (!status || PyLong_AsLong(status) != RTN_OK) return status;
+    Py_DECREF(status);
+    auto wrap = [](at::Tensor& t) -> PyObject* { return t.defined() ? THPVariable_Wrap(std::move(t)) : Py_NewRef(Py_None); };
+    if (N == 1) return wrap(out[0]);
+    PyObject* tuple = PyTuple_New(N);
+    for (int i = 0; tuple && i < N; ++i) PyTuple_SET_ITEM(tuple, i, wrap(out[i]));
+    return tuple;
 }
 
-// x, prepared, M, N, K, alpha_w, bias, act, residual, y, z_ckpt, workspace
+// w_codes, N, K, fmt, backward
+PyObject* linear_prepare(PyObject*, Args a, Py_ssize_t n)
+{
+    return call_for<2>(5, n, [&](at::Tensor* out) {
+        const int64_t N = integer(a[1]), K = integer(a[2]);
+        const rtn_code_format fmt = (rtn_code_format)integer(a[3]);
+        const void* w = codes(a[0], N, K, fmt, "w_codes");
+        const at::Tensor& like = tensor(a[0], "w_codes");
+        const size_t b = rtn_linear_prepared_bytes(N, K), bt = truth(a[4]) ? rtn_linear_prepared_bytes(K, N) : 0;
+        out[0] = make_bytes(b, like);
+        if (bt) out[1] = make_bytes(bt, like);
+        void *p = out[0].data_ptr(), *pt = bt ? out[1].data_ptr() : nullptr, *st = stream();
+        const Unlocked u;
+        return rtn_linear_prepare(fmt, w, N, K, p, b, pt, bt, st);
+    });
+}
+
+// x, prepared, N, alpha_w, bias, act, residual, y_out, z_ckpt, workspace
 PyObject* linear(PyObject*, Args a, Py_ssize_t n)
 {
-    return call(12, n, [&] {
-        const c10::ScalarType type = tensor(a[0], "x").scalar_type();
+    return call_for<1>(10, n, [&](at::Tensor* out) {
+        const at::Tensor& xt = matrix(a[0], "x");
+        const c10::ScalarType type = xt.scalar_type();
         const rtn_dtype dt = dtype(type, "x");
-        const int64_t M = integer(a[2]), N = integer(a[3]), K = integer(a[4]);
+        const int64_t M = xt.size(0), K = xt.size(1), N = integer(a[2]);
         int64_t ldx, ldr, ldy;
-        const void* x = rows2d(a[0], type, M, K, "x", ldx);
+        const void* x = rows2d(xt, type, M, K, "x", ldx);
         const void* w = bytes_of(a[1], rtn_linear_prepared_bytes(N, K), "prepared");
-        const Gran al(a[5], "alpha_w");
-        if (al.gran == RTN_VECTOR && tensor(a[5], "alpha_w").numel() != N) fail(PyExc_AssertionError, "%s: one entry per output is required", "alpha_w");
-        const void* bias = dev(a[6], type, "bias");
-        if (bias && tensor(a[6], "bias").numel() != N) fail(PyExc_AssertionError, "%s: one entry per output is required", "bias");
-        const rtn_act act = (rtn_act)integer(a[7]);
-        const void* res = rows2d(a[8], type, M, N, "residual", ldr);
-        void* y = rows2d(a[9], type, M, N, "y_out", ldy);
-        void* z = bytes_of(a[10], rtn_checkpoint_bytes(M, N), "z_ckpt");
-        const size_t zb = raw_bytes(a[10], "z_ckpt");
-        void* ws = raw(a[11], "workspace");
-        const size_t wsb = raw_bytes(a[11], "workspace");
-        void* st = stream();
+        const AlphaN al(a[3], N);
+        const void* bias = vector_of(a[4], type, N, "bias");
+        const rtn_act act = (rtn_act)integer(a[5]);
+        const void* res = rows2d(a[6], type, M, N, "residual", ldr);
+        out[0] = given_or(a[7], "y_out", [&] { return make_rows(M, N, type, xt); });
+        void* y = rows2d(out[0], type, M, N, "y_out", ldy);
+        void* z = bytes_of(a[8], rtn_checkpoint_bytes(M, N), "z_ckpt");
+        const size_t zb = raw_bytes(a[8], "z_ckpt"), need = rtn_linear_workspace_bytes(x, ldx, M, N, K, z != nullptr);
+        at::Tensor work;
+        if (need) work = given_or(a[9], "workspace", [&] { return make_bytes(need, xt); });
+        void *ws = need ? work.data_ptr() : nullptr, *st = stream();
+        const size_t wsb = need ? work.nbytes() : 0;
         const Unlocked u;
         return rtn_linear(dt, x, ldx, w, M, N, K, al.ptr, al.gran, bias, act, res, ldr, y, ldy, z, zb, ws, wsb, st);
     });
 }
 
-// x, ckpt, pack (else unpack)
-PyObject* checkpoint(PyObject*, Args a, Py_ssize_t n)
+// x, ckpt
+PyObject* checkpoint_pack(PyObject*, Args a, Py_ssize_t n)
 {
-    return call(3, n, [&] {
-        const at::Tensor& t = tensor(a[0], "x");
+    return call_for<1>(2, n, [&](at::Tensor* out) {
+        const at::Tensor& t = matrix(a[0], "x");
         const rtn_dtype dt = dtype(t.scalar_type(), "x");
-        if (t.dim() != 2) fail(PyExc_AssertionError, "%s: a matrix is required", "x");
         const int64_t M = t.size(0), C = t.size(1);
         int64_t ld;
-        void* x = rows2d(a[0], t.scalar_type(), M, C, "x", ld);
-        void* k = bytes_of(a[1], rtn_checkpoint_bytes(M, C), "ckpt");
-        const size_t kb = raw_bytes(a[1], "ckpt");
-        const int pack = truth(a[2]);
-        void* st = stream();
+        const void* x = rows2d(t, t.scalar_type(), M, C, "x", ld);
+        const size_t need = rtn_checkpoint_bytes(M, C);
+        out[0] = given_or(a[1], "ckpt", [&] { return make_bytes(need, t); });
+        void *k = bytes_of(out[0], need, "ckpt"), *st = stream();
+        const size_t kb = out[0].nbytes();
         const Unlocked u;
-        return pack ? rtn_checkpoint_pack(dt, x, ld, M, C, k, kb, st) : rtn_checkpoint_unpack(dt, k, kb, M, C, x, ld, st);
+        return rtn_checkpoint_pack(dt, x, ld, M, C, k, kb, st);
     });
 }
 
-// dy, x_ckpt, z_ckpt, act, prepared_t, M, N, K, alpha_w, dx, dw, dbias, workspace
+// ckpt, out
+PyObject* checkpoint_unpack(PyObject*, Args a, Py_ssize_t n)
+{
+    return call_for<1>(2, n, [&](at::Tensor* out) {
+        const at::Tensor& t = matrix(a[1], "out");
+        const rtn_dtype dt = dtype(t.scalar_type(), "out");
+        const int64_t M = t.size(0), C = t.size(1);
+        int64_t ld;
+        void* y = rows2d(t, t.scalar_type(), M, C, "out", ld);
+        const void* k = bytes_of(a[0], rtn_checkpoint_bytes(M, C), "ckpt");
+        const size_t kb = raw_bytes(a[0], "ckpt");
+        out[0] = t;
+        void* st = stream();
+        const Unlocked u;
+        return rtn_checkpoint_unpack(dt, k, kb, M, C, y, ld, st);
+    });
+}
+
+// dy, prepared_t, K, alpha_w, x_ckpt, act, z_ckpt, want_dx, want_dw, want_dbias, dw in fp32, dx, dw, dbias, workspace
 PyObject* linear_backward(PyObject*, Args a, Py_ssize_t n)
 {
-    return call(13, n, [&] {
-        const c10::ScalarType type = tensor(a[0], "dy").scalar_type();
+    return call_for<3>(15, n, [&](at::Tensor* out) {
+        const at::Tensor& t = matrix(a[0], "dy");
+        const c10::ScalarType type = t.scalar_type();
         const rtn_dtype dt = dtype(type, "dy");
-        const int64_t M = integer(a[5]), N = integer(a[6]), K = integer(a[7]);
-        int64_t lddy, lddx, lddw;
-        const void* dy = rows2d(a[0], type, M, N, "dy", lddy);
-        const void* x = bytes_of(a[1], rtn_checkpoint_bytes(M, K), "x_ckpt");
-        const void* z = bytes_of(a[2], rtn_checkpoint_bytes(M, N), "z_ckpt");
-        const size_t xb = raw_bytes(a[1], "x_ckpt"), zb = raw_bytes(a[2], "z_ckpt");
-        const rtn_act act = (rtn_act)integer(a[3]);
-        const void* w = bytes_of(a[4], rtn_linear_prepared_bytes(K, N), "prepared_t");
-        const Gran al(a[8], "alpha_w");
-        if (al.gran == RTN_VECTOR && tensor(a[8], "alpha_w").numel() != N) fail(PyExc_AssertionError, "%s: one entry per output is required", "alpha_w");
-        void* dx = rows2d(a[9], type, M, K, "dx", lddx);
-        void* dw = nullptr;
+        const int64_t M = t.size(0), N = t.size(1), K = integer(a[2]);
+        int64_t lddy, lddx = K, lddw;
+        const void* dy = rows2d(t, type, M, N, "dy", lddy);
+        const void* w = bytes_of(a[1], rtn_linear_prepared_bytes(K, N), "prepared_t");
+        const AlphaN al(a[3], N);
+        const void* x = bytes_of(a[4], rtn_checkpoint_bytes(M, K), "x_ckpt");
+        const rtn_act act = (rtn_act)integer(a[5]);
+        const void* z = bytes_of(a[6], rtn_checkpoint_bytes(M, N), "z_ckpt");
+        const size_t xb = raw_bytes(a[4], "x_ckpt"), zb = raw_bytes(a[6], "z_ckpt");
+        void *dx = nullptr, *dw = nullptr, *db = nullptr;
         rtn_dtype dwt = dt;
-        if (a[10] != Py_None) {
-            const c10::ScalarType t = tensor(a[10], "dw").scalar_type();
-            dwt = dtype(t, "dw", true);
-            dw = rows2d(a[10], t, N, K, "dw", lddw);
+        if (truth(a[7])) {
+            out[0] = given_or(a[11], "dx", [&] { return make_rows(M, K, type, t); });
+            dx = rows2d(out[0], type, M, K, "dx", lddx);
+        }
+        if (truth(a[8])) {
+            out[1] = given_or(a[12], "dw", [&] { return make_rows(N, K, truth(a[10]) ? c10::kFloat : type, t); });
+            dwt = dtype(out[1].scalar_type(), "dw", true);
+            dw = rows2d(out[1], out[1].scalar_type(), N, K, "dw", lddw);
             if (lddw != K) fail(PyExc_AssertionError, "%s: a contiguous tensor is required", "dw");
         }
-        void* db = dev(a[11], type, "dbias");
-        if (db && tensor(a[11], "dbias").numel() != N) fail(PyExc_AssertionError, "%s: one entry per output is required", "dbias");
-        void* ws = raw(a[12], "workspace");
-        const size_t wsb = raw_bytes(a[12], "workspace");
-        void* st = stream();
+        if (truth(a[9])) {
+            out[2] = given_or(a[13], "dbias", [&] { return at::empty({N}, t.options()); });
+            if (!out[2].is_cuda() || out[2].scalar_type() != type || !out[2].is_contiguous() || out[2].numel() != N)
+                fail(PyExc_AssertionError, "%s: a contiguous device tensor of dy's type, one entry per output, is required", "dbias");
+            db = out[2].data_ptr();
+        }
+        const at::Tensor work = given_or(a[14], "workspace", [&] { return make_bytes(rtn_linear_backward_workspace_bytes(M, N, K), t); });
+        void *ws = work.data_ptr(), *st = stream();
+        const size_t wsb = work.nbytes();
         const Unlocked u;
         return rtn_linear_backward(dt, dy, lddy, x, xb, z, zb, act, w, M, N, K, al.ptr, al.gran, dx, lddx, dw, dwt, db, ws, wsb, st);
     });
@@ -432,7 +520,7 @@ PyObject* linear_backward(PyObject*, Args a, Py_ssize_t n)
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(pack), FAST(gemm), FAST(conv2d), FAST(conv2d_ternarize), FAST(depthwise), FAST(weight_gemm),
                          FAST(weight_conv2d_prepared), FAST(activation_backward), FAST(weight_backward),
-                         FAST(linear), FAST(checkpoint), FAST(linear_backward), {nullptr, nullptr, 0, nullptr}};
+                         FAST(linear_prepare), FAST(linear), FAST(checkpoint_pack), FAST(checkpoint_unpack), FAST(linear_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

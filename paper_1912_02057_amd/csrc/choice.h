@@ -241,7 +241,7 @@ inline int pick_ksplit(const KsplitShape& s)
 // tokens.  Split: blocks of 32 x 32, 32 x 64 and 64 x 64 (tokens x outputs) whose 8 waves share the columns.  Tiles: of
 // 128 x 128 and 128 x 256, two blocks a CU.
 enum class LinearForm { kFew, kSplit32, kSplit32x64, kSplit64, kTile128, kTile256 };
-constexpr int kFewTokens = 4;
+constexpr int kFewTokens = 16, kFewOutputs = 4096;
 
 // The least of the forms' times, each a line through measured ones, in us (bf16, no activation; k = K / 1024):
 //   rounds of 256 blocks: split 32 x 32  2 + r (1.9 + 1.2 k), 32 x 64  2 + r (2.2 + 1.45 k), 64 x 64  2 + r (4 + 2 k)
@@ -251,10 +251,15 @@ constexpr int kFewTokens = 4;
 //     64 x 4096 x 4096    7.6 / 8.7 / 11.8 / 29.9 / 42.0      1024 x 4096 x 1024  46.7 / 32.0 / 26.2 / 13.4 / 18.0
 //     512 x 2048 x 2048  18.1 / 12.7 / 10.8 / 18.4 / 25.3     1024 x 8192 x 4096   186 / 124 / 102 / 67.0 / 60.6
 //     256 x 4096 x 4096  27.3 / 18.1 / 13.8 / 31.2 / 43.7     4096 x 4096 x 4096   363 / 239 / 199 / 124 / 108
-// A token count that kFew takes: 1 x 4096 x 4096 measured beside it at launch_linear.
+// kFew, blocks of 16 outputs up to kFewOutputs of them (a block per CU), of 32 beyond, where x is loaded half as often (us):
+//     tokens                          1      4      8     16     (32 x 32 split)
+//     4096 x 4096, blocks of 16      3.5    4.2           6.0     6.8
+//                            32      4.0    4.6           6.7
+//     8192 x 8192, blocks of 16      8.1   10.4   12.9   18.2     9.8
+//                            32      6.9    8.0    9.0   11.4
 inline LinearForm linear_form(int64_t M, int64_t N, int64_t K, bool keeps_z)
 {
-    if (M <= kFewTokens && !keeps_z) return LinearForm::kFew;
+    if (M <= (N > kFewOutputs ? kFewTokens / 2 : kFewTokens) && !keeps_z) return LinearForm::kFew;
     auto blocks = [&](int64_t m, int64_t n) { return ((M + m - 1) / m) * ((N + n - 1) / n); };
     const double k = (double)K / 1024;
     auto split = [&](int64_t n, double base, double slope) { return 2 + (double)((n + 255) / 256) * (base + slope * k); };

@@ -408,68 +408,114 @@ __global__ __launch_bounds__(256, (LinTile<BM, BN, NS>::PER_CU)) void k_linear(L
     }
 }
 
-// A few tokens: a block has 32 outputs, its waves share the columns, the weights are read once and x and weights go
-// straight into registers, BATCH steps' loads in flight at a time.  A load of x touches a cache line per token.
-template <class T, int WAVES, int BATCH, bool ROW16>
+// A few tokens (at most 16): a block has 16 RB outputs, its waves share the columns, the weights are read once and x and weights
+// go straight into registers.  v_mfma 16x16x32 takes row l & 15, columns 8 (l >> 4) .. + 7 from lane l, which lane
+// (l & 15) + 16 half + 32 (l >> 4 & 1) of the 32-row order has, in the word's first four registers (slice 2 s) or its last.
+// Bound by the widening of the weights, two vector operations for two of them, and for small layers by the latency of a load
+// after the launch.
+template <class T, int RB, int WAVES, int BATCH, bool ROW16>
 __global__ __launch_bounds__(WAVES * 64) void k_linear_few(LinParams p)
 {
-    __shared__ float part[WAVES][kFewTokens][36];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, h = lane >> 5;
-    const int rb = blockIdx.x, n0 = rb * 32;
-    f32x16 acc;
+    __shared__ float part[WAVES][kFewTokens][RB * 16 + 4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, c = lane >> 4;
+    const int n0 = blockIdx.x * 16 * RB;
+    f32x4 acc[RB][2];  // the instruction's result is late for the next one on the same registers
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[r] = 0.f;
-    const uint2* w = (const uint2*)p.w + (int64_t)rb * p.nk * 64 + lane;
-    const unsigned short* xrow = (const unsigned short*)p.x + (int64_t)l32 * p.ldx;
-    const bool mine = l32 < p.M;
-    auto load_x = [&](int k) {
-        u32x4 v = {0, 0, 0, 0};
-        if (mine) {
-            if (ROW16 ? k < p.K : k + 8 <= p.K) {
+    for (int r = 0; r < RB; ++r) acc[r][0] = acc[r][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const bool mine = l16 < p.M;  // the other lanes' columns of the result are not looked at, whatever they hold
+    const int ktail = p.K & 63;
+    const auto xr = __builtin_amdgcn_make_buffer_rsrc((void*)p.x, 0, (int)(((p.M - 1) * p.ldx + p.K) * 2), 0x00020000);
+    const int xoff = (int)(l16 * p.ldx * 2) + c * 16;
+    int woff[RB];
+    const int rb0 = (int)(blockIdx.x * RB) >> 1, rbs = p.rb - rb0;  // (a block of 32 rows holds two of 16)
+    const auto wr = __builtin_amdgcn_make_buffer_rsrc((void*)(p.w + (int64_t)rb0 * p.nk * 512), 0, rbs < (RB + 1) / 2 ? rbs * p.nk * 512 : (RB + 1) / 2 * p.nk * 512, 0x00020000);
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        const int r16 = (int)(blockIdx.x * RB) + r;  // (rows of no block read as zeros)
+        woff[r] = ((r16 >> 1) - rb0) * p.nk * 512 + (l16 + 16 * (r16 & 1) + 32 * (c & 1)) * 8;
+    }
+    const int up = c & 2 ? 8 : 0;
+    const unsigned short* xrow = (const unsigned short*)p.x + (int64_t)l16 * p.ldx;
+    auto load_x = [&](int step, int s) {
+        if constexpr (ROW16) {
+            return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xr, xoff, step * 128 + 64 * s, 0));
+        } else {
+            const int k = step * 64 + 32 * s + 8 * c;
+            u32x4 v = {0, 0, 0, 0};
+            if (k + 8 <= p.K) {
                 v = load16(xrow + k);
-            } else if (!ROW16) {
+            } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     if (k + i < p.K) v[i >> 1] |= (unsigned)xrow[k + i] << (16 * (i & 1));
             }
+            return v;
         }
-        return v;
     };
+    // what the outputs need beside the sums, fetched with the first weights: thread 16 RB m + i has output i of token m
+    constexpr int OUTS = 16 * RB, PER = (kFewTokens * OUTS + WAVES * 64 - 1) / (WAVES * 64);
+    float al[PER], bi[PER], re[PER];
+#pragma unroll
+    for (int o = 0; o < PER; ++o) {
+        const int at = tid + o * WAVES * 64, om = at / OUTS, on = n0 + at % OUTS;
+        al[o] = bi[o] = re[o] = 0.f;
+        if (om >= p.M || on >= p.N) continue;
+        al[o] = 0.5f * (p.alpha.ptr ? p.alpha.ptr[on] : p.alpha.s);
+        if (p.bias) bi[o] = T::to_float(p.bias[on]);
+        if (p.res) re[o] = T::to_float(p.res[om * p.ldr + on]);
+    }
     for (int s0 = wave; s0 < p.nk; s0 += WAVES * BATCH) {
-        uint2 word[BATCH];
-        u32x4 xf[BATCH][4];
+        uint2 word[BATCH][RB];
+        u32x4 xf[BATCH][2];
+        // past the last step: that one again, with weights of zero
+        auto step_at = [&](int b) {
+            const int step = s0 + b * WAVES;
+            return step < p.nk ? step : p.nk - 1;
+        };
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b)
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+                word[b][r] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(wr, woff[r], step_at(b) * 512, 0));
+        if (mine)
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) xf[b][s] = load_x(step_at(b), s);
 #pragma unroll
         for (int b = 0; b < BATCH; ++b) {
             const int step = s0 + b * WAVES;
-            word[b] = step < p.nk ? w[(int64_t)step * 64] : make_uint2(0, 0);
+            const unsigned real = step < p.nk ? ~0u : 0u;
+            if (ROW16 && ktail && step >= p.nk - 1) {  // columns past K
 #pragma unroll
-            for (int j = 0; j < 4; ++j) xf[b][j] = load_x(step * 64 + 16 * j + 8 * h);  // (zeros from step nk on)
-        }
+                for (int s = 0; s < 2; ++s)
+                    if (32 * s + 8 * c >= ktail) xf[b][s] = u32x4{0, 0, 0, 0};
+            }
 #pragma unroll
-        for (int b = 0; b < BATCH; ++b) {
-            acc = T::mfma(expand<0>(word[b]), xf[b][0], acc);
-            acc = T::mfma(expand<1>(word[b]), xf[b][1], acc);
-            acc = T::mfma(expand<2>(word[b]), xf[b][2], acc);
-            acc = T::mfma(expand<3>(word[b]), xf[b][3], acc);
+            for (int r = 0; r < RB; ++r) {
+                const uint2 w2 = make_uint2((word[b][r].x & real) << up, (word[b][r].y & real) << up);
+                acc[r][0] = T::mfma16(expand<0>(w2), xf[b][0], acc[r][0]);
+                acc[r][1] = T::mfma16(expand<2>(w2), xf[b][1], acc[r][1]);
+            }
         }
     }
-    if (mine && l32 < kFewTokens)
+    if (mine)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            *(float4*)&part[wave][l32][8 * q + 4 * h] = make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
+        for (int r = 0; r < RB; ++r)
+            *(float4*)&part[wave][l16][r * 16 + 4 * c] = make_float4(acc[r][0][0] + acc[r][1][0], acc[r][0][1] + acc[r][1][1],
+                                                                     acc[r][0][2] + acc[r][1][2], acc[r][0][3] + acc[r][1][3]);
     __syncthreads();
-    for (int o = tid; o < p.M * 4; o += WAVES * 64) {  // 8 outputs of a token each
-        const int m = o >> 2, c = (o & 3) * 8, n = n0 + c;
-        float al[8], bi[8], z[8];
-        load_affine<T>(p, n, al, bi);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float s = 0.f;
+    for (int o = 0; o < PER; ++o) {
+        const int at = tid + o * WAVES * 64, om = at / OUTS, i = at % OUTS;
+        if (om >= p.M || n0 + i >= p.N) continue;
+        float s = 0.f;
 #pragma unroll
-            for (int v = 0; v < WAVES; ++v) s += part[v][m][c + i];
-            z[i] = fmaf(s, al[i], bi[i]);
-        }
-        with_act(p.act, [&](auto which) { finish_row<T, decltype(which)::value, false>(p, m, n, z); });
+        for (int v = 0; v < WAVES; ++v) s += part[v][om][i];
+        const float z = fmaf(s, al[o], bi[o]);
+        with_act(p.act, [&](auto which) {
+            p.y[om * p.ldy + n0 + i] = T::from_float(act_value<decltype(which)::value>(z) + re[o]);
+        });
     }
 }
 
@@ -652,14 +698,16 @@ hipError_t run_tile(LinParams& p, hipStream_t st)
     return hipGetLastError();
 }
 
-template <class T, int WAVES, int BATCH>
+bool rows_of_16(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
+
+template <class T, int RB, int WAVES, int BATCH>
 hipError_t run_few(const LinParams& p, hipStream_t st)
 {
-    const unsigned grid = (unsigned)((p.N + 31) / 32);
-    if (p.K % 8 == 0)
-        k_linear_few<T, WAVES, BATCH, true><<<grid, WAVES * 64, 0, st>>>(p);
+    const unsigned grid = (unsigned)((p.N + 16 * RB - 1) / (16 * RB));
+    if (p.K % 8 == 0 && rows_of_16(p.x, p.ldx) && (p.M * p.ldx + p.K) * 2 < (int64_t)kOutside)
+        k_linear_few<T, RB, WAVES, BATCH, true><<<grid, WAVES * 64, 0, st>>>(p);
     else
-        k_linear_few<T, WAVES, BATCH, false><<<grid, WAVES * 64, 0, st>>>(p);
+        k_linear_few<T, RB, WAVES, BATCH, false><<<grid, WAVES * 64, 0, st>>>(p);
     return hipGetLastError();
 }
 
@@ -678,13 +726,11 @@ hipError_t run_split(LinParams& p, hipStream_t st)
     return hipGetLastError();
 }
 
-bool rows_of_16(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
-
 template <class T>
 hipError_t run(const LinearArgs& a, LinParams p, hipStream_t st)
 {
     const LinearForm form = linear_form(a.M, a.N, a.K, a.zq != nullptr);
-    if (form == LinearForm::kFew) return p.nk >= 16 ? run_few<T, 16, 4>(p, st) : run_few<T, 4, 4>(p, st);
+    if (form == LinearForm::kFew) return a.N > kFewOutputs ? run_few<T, 2, 16, 2>(p, st) : run_few<T, 1, 16, 2>(p, st);
     if (linear_copies_x(a)) {
         const int64_t ld = (a.K + 63) / 64 * 64, blocks = (a.M * ld / 8 + 255) / 256;
         k_copy_rows<<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, st>>>((const unsigned short*)a.x, a.ldx, a.M, a.K, ld, (unsigned short*)a.workspace);

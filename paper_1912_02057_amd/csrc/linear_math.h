@@ -52,9 +52,14 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 struct BF16 {
+    static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
     // of a checkpoint's scale: 2^-126 is the least normal; 127 x 2^121 is finite, 64 x 2^122 is not
     static constexpr int kLeastExp = -126, kMostExp = 121;
     static __device__ __forceinline__ float to_float(unsigned short v) { return __uint_as_float((unsigned)v << 16); }
@@ -72,6 +77,10 @@ struct BF16 {
     }
 };
 struct F16 {
+    static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
     // every float16 is a multiple of 2^-24, and so is what a checkpoint gives back; 64 x 2^10 is infinite
     static constexpr int kLeastExp = -24, kMostExp = 9;
     static __device__ __forceinline__ float to_float(unsigned short v) { return (float)__builtin_bit_cast(_Float16, v); }

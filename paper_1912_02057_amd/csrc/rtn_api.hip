@@ -697,11 +697,11 @@ int rtn_linear_prepare(rtn_code_format fmt, const void* w_codes, int64_t N, int6
     return e == hipSuccess ? RTN_OK : hip_fail(e);
 }
 
-size_t rtn_linear_workspace_bytes(const void* x, int64_t ldx, int64_t M, int64_t K, int keeps_z)
+size_t rtn_linear_workspace_bytes(const void* x, int64_t ldx, int64_t M, int64_t N, int64_t K, int keeps_z)
 {
-    if (!linear_dims(1, K) || M <= 0 || M > kMaxDim || ldx < K) return 0;
+    if (!linear_dims(N, K) || M <= 0 || M > kMaxDim || ldx < K) return 0;
     rtn::LinearArgs a = {};
-    a.x = x, a.M = M, a.N = 1, a.K = K, a.ldx = ldx;  // (what is asked here does not depend on N)
+    a.x = x, a.M = M, a.N = N, a.K = K, a.ldx = ldx;
     a.zq = keeps_z ? (int8_t*)16 : nullptr;
     return rtn::linear_copies_x(a) ? (size_t)M * (size_t)((K + 63) / 64 * 128) : 0;
 }
@@ -723,7 +723,7 @@ int rtn_linear(rtn_dtype dt, const void* x, int64_t ldx, const void* prepared, i
     if (rc != RTN_OK) return rc;
     if (z_ckpt && z_ckpt_bytes < rtn_checkpoint_bytes(M, N)) return RTN_ERR_WORKSPACE;
     if (M == 0) return RTN_OK;
-    const size_t need = rtn_linear_workspace_bytes(x, ldx, M, K, z_ckpt != nullptr);
+    const size_t need = rtn_linear_workspace_bytes(x, ldx, M, N, K, z_ckpt != nullptr);
     if (need && (!workspace || workspace_bytes < need)) return RTN_ERR_WORKSPACE;
     if (need && !aligned(workspace, 16)) return RTN_ERR_ALIGN;
     a.x = x, a.w = prepared;

@@ -42,12 +42,12 @@ def test_sizes(L):
     assert L.rtn_checkpoint_bytes(33, 9) == 4 * 264
     assert L.rtn_checkpoint_bytes(0, 9) == 0 and L.rtn_checkpoint_bytes(5, -1) == 0
     # rows of whole 16 bytes are read where they lie, others are copied; a few tokens never are
-    assert L.rtn_linear_workspace_bytes(FAKE, 128, 500, 128, 0) == 0
-    assert L.rtn_linear_workspace_bytes(FAKE, 131, 500, 128, 0) == 500 * 128 * 2
-    assert L.rtn_linear_workspace_bytes(FAKE, 136, 500, 130, 0) == 500 * 192 * 2
-    assert L.rtn_linear_workspace_bytes(HALF, 128, 500, 128, 0) == 500 * 128 * 2
-    assert L.rtn_linear_workspace_bytes(HALF, 131, 1, 130, 0) == 0
-    assert L.rtn_linear_workspace_bytes(FAKE, 100, 500, 128, 0) == 0          # a pitch below the row's length
+    assert L.rtn_linear_workspace_bytes(FAKE, 128, 500, 300, 128, 0) == 0
+    assert L.rtn_linear_workspace_bytes(FAKE, 131, 500, 300, 128, 0) == 500 * 128 * 2
+    assert L.rtn_linear_workspace_bytes(FAKE, 136, 500, 300, 130, 0) == 500 * 192 * 2
+    assert L.rtn_linear_workspace_bytes(HALF, 128, 500, 300, 128, 0) == 500 * 128 * 2
+    assert L.rtn_linear_workspace_bytes(HALF, 131, 1, 300, 130, 0) == 0
+    assert L.rtn_linear_workspace_bytes(FAKE, 100, 500, 300, 128, 0) == 0          # a pitch below the row's length
     assert L.rtn_linear_backward_workspace_bytes(100, 64, 0) == 0
     assert L.rtn_linear_backward_workspace_bytes(100, 64, 64) > 100 * 64 * 4
 

@@ -23,15 +23,17 @@ struct WgParams {
 
 template <int BN, int BK>
 struct WgTile {
-    static constexpr int WN = BN / 2, WK = BK / 2, TN = WN / 32, TK = WK / 32, NM = TN * TK;
-    // a stage: two blocks of 32 tokens, x^ before dz in each; a wave's loads of 1 KiB
-    static constexpr int XBYTES = BK * 64, HALF = XBYTES + BN * 64, STAGE = 2 * HALF, XDMA = BK / 64, DDMA = BN / 64, DPS = 2 * (XDMA + DDMA);
+    static constexpr int WN = BN / 2, WK = BK / 2, TN = WN / 32, TK = WK / 32, NM = TN * TK, SLOTS = 5;
+    // a slot: a block of 32 tokens, x^ before dz; a wave's loads of 1 KiB
+    static constexpr int XBYTES = BK * 64, SLOT = XBYTES + BN * 64, XDMA = BK / 64, DDMA = BN / 64, DPS = XDMA + DDMA;
     static constexpr int ZPITCH = WK * 4 + 16, ZBYTES = 32 * ZPITCH;
-    static constexpr int LDS = 2 * STAGE > 4 * ZBYTES ? 2 * STAGE : 4 * ZBYTES;
+    static constexpr int LDS = SLOTS * SLOT > 4 * ZBYTES ? SLOTS * SLOT : 4 * ZBYTES;
 };
 
-// A block of 4 waves (2 x 2) owns BN x BK of dw.  Two stages of 64 tokens; fragments are read one 16-token slice ahead, so that
-// before the last slice of a step nothing is left to read of its stage: behind the one barrier there it is filled again.
+// A block of 4 waves (2 x 2) owns BN x BK of dw.  A step is 64 tokens, two slots of a ring of five; fragments are read one
+// 16-token slice ahead, so that before the last slice of a step nothing is left to read of its slots.  Behind the one barrier
+// there they are filled again, over the next four slices: first with the second half of the step after next, which then has half
+// a step to land, then with the first half of the one after that.
 template <class T, int BN, int BK, bool F32>
 __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgParams p)
 {
@@ -46,24 +48,20 @@ __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgP
         band_tile(bid, p.tilesN, p.band_tiles, [&](int n) { return (int)fastdiv((uint32_t)n, p.div_band); },
                   [&](int n) { return (int)fastdiv((uint32_t)n, p.div_lastband); }, tn, tk);
     }
-    const int n0 = tn * BN, k0 = tk * BK, nk = p.nk;
+    const int n0 = tn * BN, k0 = tk * BK, nk = p.nk, nh = 2 * nk;
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-    const char* xg = p.x + (int64_t)(k0 / 32) * 2048 + wave * L::XDMA * 1024;
-    const char* dg = p.d + (int64_t)(n0 / 32) * 2048 + wave * L::DDMA * 1024;
-    // load i of a step whose operands start at xs, ds; the second 32 tokens lie a pitch (below 2^32 bytes) further on
+    const int8_t* xg = (const int8_t*)p.x + (int64_t)(k0 / 32) * 2048 + wave * L::XDMA * 1024;
+    const int8_t* dg = (const int8_t*)p.d + (int64_t)(n0 / 32) * 2048 + wave * L::DDMA * 1024;
     const unsigned voff = (unsigned)lane * 16u;
-    auto load_one = [&](auto index, const int8_t* xs, const int8_t* ds, unsigned base) {
-        constexpr int i = decltype(index)::value, half = i / (L::XDMA + L::DDMA), j = i % (L::XDMA + L::DDMA);
-        if constexpr (j < L::XDMA)
-            dma16_base<half * L::HALF + j * 1024>(xs + (half ? p.xpitch : 0), voff + j * 1024, base + (unsigned)(wave * L::XDMA * 1024));
+    // load i of token block q into its slot at LDS address `base`
+    auto load_one = [&](auto index, int q, unsigned base) {
+        constexpr int i = decltype(index)::value;
+        if constexpr (i < L::XDMA)
+            dma16_base<i * 1024>(xg + q * p.xpitch, voff + i * 1024, base + (unsigned)(wave * L::XDMA * 1024));
         else
-            dma16_base<half * L::HALF + L::XBYTES + (j - L::XDMA) * 1024>(ds + (half ? p.dpitch : 0), voff + (j - L::XDMA) * 1024,
-                                                                          base + (unsigned)(wave * L::DDMA * 1024));
+            dma16_base<L::XBYTES + (i - L::XDMA) * 1024>(dg + q * p.dpitch, voff + (i - L::XDMA) * 1024, base + (unsigned)(wave * L::DDMA * 1024));
     };
-    auto issue = [&](int step, int slot) {
-        const int8_t *xs = (const int8_t*)xg + step * (2 * p.xpitch), *ds = (const int8_t*)dg + step * (2 * p.dpitch);
-        for_each_index([&](auto index) { load_one(index, xs, ds, lds0 + (unsigned)(slot * L::STAGE)); }, std::make_integer_sequence<int, L::DPS>{});
-    };
+    auto slot_of = [&](int q) { return q >= 2 * L::SLOTS ? q - 2 * L::SLOTS : q >= L::SLOTS ? q - L::SLOTS : q; };
 
     f32x16 acc[L::TK][L::TN];
 #pragma unroll
@@ -75,12 +73,11 @@ __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgP
     u32x4 xf[2][L::TK], df[2][L::TN];
     const int xbase = wk * L::TK * 2048 + lane * 16, dbase = L::XBYTES + wn * L::TN * 2048 + lane * 16;
 
-    if (nk > 0) issue(0, 0);
-    if (nk > 1) issue(1, 1);
-    if (nk > 1)
-        wait_vm<L::DPS>();
-    else
-        wait_vm<0>();
+    // blocks 0 .. 4, of which the first step's two are waited for
+    const int first = nh < L::SLOTS ? nh : L::SLOTS;
+    for (int q = 0; q < first; ++q)
+        for_each_index([&](auto index) { load_one(index, q, lds0 + (unsigned)(q * L::SLOT)); }, std::make_integer_sequence<int, L::DPS>{});
+    wait_groups<L::DPS>(first - 2);
     block_barrier();
 #pragma unroll
     for (int i = 0; i < L::TK; ++i) xf[0][i] = *(const u32x4*)(smem + xbase + i * 2048);
@@ -89,20 +86,28 @@ __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgP
 
     const std::true_type yes{};
     const std::false_type no{};
-    int slot = 0;
-    // MORE: two steps follow, the later of which is loaded
-    auto one_step = [&](auto more, int step) {
-        constexpr bool MORE = decltype(more)::value;
-        const int8_t *xs = (const int8_t*)xg + (step + 2) * (2 * p.xpitch), *ds = (const int8_t*)dg + (step + 2) * (2 * p.dpitch);
-        const unsigned fill = lds0 + (unsigned)(slot * L::STAGE);
+    int s0 = 0;  // slot of the step's first block
+    // Whether slice 0, slices 1 and 2, and slice 3 load anything: the rest of block 2 step + 3, block 2 step + 4, the first half of
+    // block 2 step + 5.
+    auto one_step = [&](auto fill0, auto fill12, auto fill3, int step) {
         auto slice = [&](auto index) {
             constexpr int j = decltype(index)::value, cur = j & 1, nxt = cur ^ 1;
+            constexpr bool FILL = j == 0 ? decltype(fill0)::value : j == 3 ? decltype(fill3)::value : decltype(fill12)::value;
             if constexpr (j == 3) {
-                wait_vm<0>();   // the next step has landed,
-                wait_lgkm0();   // and this wave has read all of the present one
+                // the next step has landed, but for the first half of the one behind it; this wave has read all of the present one
+                if constexpr (FILL)
+                    wait_vm<L::DPS>();
+                else
+                    wait_vm<0>();
+                wait_lgkm0();
                 block_barrier();
             }
-            const char* stage = smem + (j == 3 ? slot ^ 1 : slot) * L::STAGE + ((j + 1) & 2 ? L::HALF : 0) + ((j + 1) & 1) * 1024;
+            // the slot the next slice is read from
+            const char* stage = smem + slot_of(s0 + (j == 0 ? 0 : j == 3 ? 2 : 1)) * L::SLOT + ((j + 1) & 1) * 1024;
+            // the loads of four slices from a barrier on: part 0 (slice 3) to 3 (slice 2 of the next step), two of a block
+            constexpr int part = (j + 1) & 3, DN = L::DPS / 2;
+            const int q = 2 * step + (j == 3 ? 5 : 3) + (part >> 1);
+            const unsigned base = lds0 + (unsigned)(slot_of(s0 + (j == 3 ? 0 : 3) + (part >> 1)) * L::SLOT);
             for_each_index(
                 [&](auto mi) {
                     constexpr int n = decltype(mi)::value, i = n / L::TN, k = n % L::TN;
@@ -116,14 +121,15 @@ __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgP
                         else
                             df[nxt][f < L::TK ? 0 : f - L::TK] = *(const u32x4*)(stage + dbase + (f - L::TK) * 2048);
                     }
-                    if constexpr (j == 3 && MORE) {
-                        constexpr int DPER = (L::DPS + L::NM - 1) / L::NM;
-                        for_each_index(
-                            [&](auto di) {
-                                constexpr int d = n * DPER + decltype(di)::value;
-                                if constexpr (d < L::DPS) load_one(std::integral_constant<int, d>{}, xs, ds, fill);
-                            },
-                            std::make_integer_sequence<int, DPER>{});
+                    if constexpr (FILL) {
+                        constexpr int EVERY = L::NM / DN > 0 ? L::NM / DN : 1, DPER = (DN + L::NM - 1) / L::NM;
+                        if constexpr (n % EVERY == EVERY - 1)
+                            for_each_index(
+                                [&](auto di) {
+                                    constexpr int d = n / EVERY * DPER + decltype(di)::value;
+                                    if constexpr (d < DN) load_one(std::integral_constant<int, (part & 1) * DN + d>{}, q, base);
+                                },
+                                std::make_integer_sequence<int, DPER>{});
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 },
@@ -133,11 +139,16 @@ __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgP
         slice(std::integral_constant<int, 1>{});
         slice(std::integral_constant<int, 2>{});
         slice(std::integral_constant<int, 3>{});
-        slot ^= 1;
+        s0 = slot_of(s0 + 2);
     };
+    // (the first step finds blocks 3 and 4 loaded; the last block is 2 nk - 1)
     int step = 0;
-    for (; step < nk - 2; ++step) one_step(yes, step);
-    for (; step < nk; ++step) one_step(no, step);
+    if (nk > 2) {
+        one_step(no, no, yes, step++);
+        for (; step < nk - 2; ++step) one_step(yes, yes, yes, step);
+        one_step(yes, no, no, step++);
+    }
+    for (; step < nk; ++step) one_step(no, no, no, step);
 
     __syncthreads();
     constexpr int CL = L::WK / 8, TPL = CL / 2;

@@ -1,8 +1,9 @@
 // Activations kept in 8 bits between the forward and the backward pass (CkptShape): into 8 bits, back, and into the operand
 // order of the weight gradient's product, there together with the gradient that it meets.
 //
-// All of them are one pass over memory.  A lane has 8 tokens of 8 channels: 8 rows of 16 bytes of a 16-bit tensor (16 lanes
-// beside each other read 256 bytes of a row), 64 bytes in a row of a checkpoint, and 16 bytes per channel of an operand.
+// All of them are one pass over memory.  A wave has 32 tokens x 64 channels, a lane 4 tokens of 8 channels: 4 rows of 16 bytes
+// of a 16-bit tensor (8 lanes beside each other read 128 bytes of a row), 32 bytes in a row of a checkpoint.  (8 tokens a lane need
+// twice the registers: the gradient's pass over 16384 x 8192 took 282 us with 190 of them, 368 with 128 and spills, and takes GRADT.)
 #include "linear_math.h"
 #include "rtn_kernels.h"
 
@@ -10,15 +11,16 @@ namespace rtn {
 
 namespace {
 
+constexpr int kTok = 4, kStrip = 64;  // tokens of a lane; channels of a wave
+
 struct Micro {  // what a lane owns
     int64_t mb, c;  // block of 32 tokens; its first channel
-    int t0;         // first of its 8 tokens in the block
+    int t0;         // first of its tokens in the block
 };
-// Wave `unit` of a tensor of cb blocks of 8 channels: 32 tokens x 128 channels.
 __device__ __forceinline__ Micro micro_of(int64_t mb, int64_t strip)
 {
     const int lane = threadIdx.x & 63;
-    return {mb, (strip * 16 + (lane & 15)) * 8, (lane >> 4) * 8};
+    return {mb, strip * kStrip + (lane & 7) * 8, (lane >> 3) * kTok};
 }
 
 // 8 channels of a row as they are; zeros past the end
@@ -45,9 +47,9 @@ __global__ __launch_bounds__(256) void k_ckpt_pack(CkptArgs a, int strips)
     if (unit >= cs.tb * strips) return;
     const int64_t mb = unit / strips;
     const Micro u = micro_of(mb, unit - mb * strips);
-    u32x4 v[8];
+    u32x4 v[kTok];
 #pragma unroll
-    for (int t = 0; t < 8; ++t)
+    for (int t = 0; t < kTok; ++t)
         v[t] = load_row((const unsigned short*)a.x, a.ld, mb * 32 + u.t0 + t, a.M, u.c, a.C);
     unsigned ex[2] = {0, 0};
     float inv[8];
@@ -56,12 +58,12 @@ __global__ __launch_bounds__(256) void k_ckpt_pack(CkptArgs a, int strips)
     for (int i = 0; i < 8; ++i) {
         unsigned am = 0;  // as bits: a NaN is larger than an infinity, and that than any number
 #pragma unroll
-        for (int t = 0; t < 8; ++t) {
+        for (int t = 0; t < kTok; ++t) {
             const unsigned b = (v[t][i >> 1] >> (16 * (i & 1))) & 0x7fffu;
             am = b > am ? b : am;
         }
 #pragma unroll
-        for (int d = 16; d < 64; d *= 2) {
+        for (int d = 8; d < 64; d *= 2) {
             const unsigned o = (unsigned)__shfl_xor((int)am, d);
             am = o > am ? o : am;
         }
@@ -73,35 +75,35 @@ __global__ __launch_bounds__(256) void k_ckpt_pack(CkptArgs a, int strips)
     const bool clamp = __any(end);
     if (u.c >= a.C) return;
     const int64_t blk = mb * cs.cb + (u.c >> 3);
-    unsigned w[16];
+    unsigned w[2 * kTok];
 #pragma unroll
-    for (int t = 0; t < 8; ++t)
+    for (int t = 0; t < kTok; ++t)
 #pragma unroll
         for (int q = 0; q < 2; ++q)
             w[t * 2 + q] = ckpt_codes(half_of<T>(v[t][2 * q], 0), half_of<T>(v[t][2 * q], 1), half_of<T>(v[t][2 * q + 1], 0),
                                       half_of<T>(v[t][2 * q + 1], 1), inv[4 * q], inv[4 * q + 1], inv[4 * q + 2], inv[4 * q + 3], clamp);
     uint4* out = (uint4*)(a.ckpt + blk * 256 + u.t0 * 8);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    for (int i = 0; i < kTok / 2; ++i) out[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
     if (u.t0 == 0) *(uint2*)(a.ckpt + cs.codes() + blk * 8) = make_uint2(ex[0], ex[1]);
 }
 
-// The 8 tokens x 8 channels of a lane of a checkpoint: codes and scales.
+// The tokens and channels of a lane of a checkpoint: codes and scales.
 struct MicroCkpt {
-    uint4 q[4];
+    uint4 q[kTok / 2];
     uint2 e;
     __device__ __forceinline__ void load(const int8_t* ckpt, const CkptShape& cs, const Micro& u)
     {
         const int64_t blk = u.mb * cs.cb + (u.c >> 3);
         const uint4* p = (const uint4*)(ckpt + blk * 256 + u.t0 * 8);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = p[i];
+        for (int i = 0; i < kTok / 2; ++i) q[i] = p[i];
         e = *(const uint2*)(ckpt + cs.codes() + blk * 8);
     }
     __device__ __forceinline__ void zero()
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < kTok / 2; ++i) q[i] = make_uint4(0, 0, 0, 0);
         e = make_uint2(0, 0);
     }
     __device__ __forceinline__ float scale(int i) const { return ckpt_scale((int)((i < 4 ? e.x : e.y) >> (8 * (i & 3)) & 255)); }
@@ -129,7 +131,7 @@ __global__ __launch_bounds__(256) void k_ckpt_unpack(CkptArgs a, int strips)
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[i] = k.scale(i);
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
+    for (int t = 0; t < kTok; ++t) {
         const int64_t m = mb * 32 + u.t0 + t;
         if (m >= a.M) break;
         float v[8];
@@ -147,16 +149,26 @@ __global__ __launch_bounds__(256) void k_ckpt_unpack(CkptArgs a, int strips)
     }
 }
 
-// 8 tokens x 8 channels (values of type T in v[channel][token pair]) -> the operand order of the weight gradient.
-__device__ __forceinline__ void store_operand(char* out, int64_t blocks, const Micro& u, const u32x4 (&v)[8])
+// A wave's 32 tokens x 64 channels (v[channel][token pair] of each lane) -> the operand order of the weight gradient.  Through
+// LDS, so that every store of the wave is 1 KiB in a row.  16-byte piece p of the wave's 4 KiB is kept at p ^ (p / 8 ^ p / 64) % 8,
+// which spreads the writes over the banks.
+__device__ __forceinline__ void store_operand(char* out, int64_t blocks, const Micro& u, const uint2 (&v)[8], char* lds)
 {
-    char* p = out + operand_offset(u.mb, u.c >> 5, blocks) + (u.t0 >> 4) * 1024 + ((u.t0 >> 3 & 1) * 32 + (int)(u.c & 31)) * 16;
+    const int lane = threadIdx.x & 63;
+    auto at = [&](int p) { return lds + 16 * (p ^ (((p >> 3) ^ (p >> 6)) & 7)); };
+    const int c = (lane & 7) * 8, p0 = (c >> 5) * 128 + (u.t0 >> 3) * 32 + (c & 31), half = u.t0 & 4;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) *(u32x4*)(p + i * 16) = v[i];
+    for (int i = 0; i < 8; ++i) *(uint2*)(at(p0 + i) + half * 2) = v[i];
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    const int64_t cb = (u.c - c) >> 5;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        if (cb + (r >> 1) < blocks) *(u32x4*)(out + operand_offset(u.mb, cb, blocks) + r * 1024 + lane * 16) = *(const u32x4*)at(r * 64 + lane);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
 template <class T, int ACT>
-__device__ __forceinline__ void grad_unit(const GradArgs& a, int64_t tb0, int64_t strip)
+__device__ __forceinline__ void grad_unit(const GradArgs& a, int64_t tb0, int64_t strip, char* lds)
 {
     const int64_t nb = (a.N + 31) / 32, tbs = operand_blocks(a.M);
     const CkptShape cs(a.M, a.N);
@@ -169,9 +181,9 @@ __device__ __forceinline__ void grad_unit(const GradArgs& a, int64_t tb0, int64_
     }
     for (int64_t mb = tb0; mb < tb0 + a.per && mb < tbs; ++mb) {
         const Micro u = micro_of(mb, strip);
-        u32x4 v[8];
+        u32x4 v[kTok];
 #pragma unroll
-        for (int t = 0; t < 8; ++t) v[t] = load_row((const unsigned short*)a.dy, a.lddy, mb * 32 + u.t0 + t, a.M, u.c, a.N);
+        for (int t = 0; t < kTok; ++t) v[t] = load_row((const unsigned short*)a.dy, a.lddy, mb * 32 + u.t0 + t, a.M, u.c, a.N);
         MicroCkpt k;
         if constexpr (ACT != kActNone) {
             if (u.c < a.N && mb < cs.tb)
@@ -179,9 +191,9 @@ __device__ __forceinline__ void grad_unit(const GradArgs& a, int64_t tb0, int64_
             else
                 k.zero();
         }
-        u32x4 o[8];
+        unsigned o[8][kTok / 2];
 #pragma unroll
-        for (int t = 0; t < 8; ++t) {
+        for (int t = 0; t < kTok; ++t) {
             float d[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -204,16 +216,22 @@ __device__ __forceinline__ void grad_unit(const GradArgs& a, int64_t tb0, int64_
                     u32x4{pack2<T>(d[0] * al[0], d[1] * al[1]), pack2<T>(d[2] * al[2], d[3] * al[3]), pack2<T>(d[4] * al[4], d[5] * al[5]),
                           pack2<T>(d[6] * al[6], d[7] * al[7])};
         }
-        if (a.dzt && u.c < nb * 32) store_operand(a.dzt, nb, u, o);
+        if (a.dzt) {
+            uint2 w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = make_uint2(o[i][0], o[i][1]);
+            store_operand(a.dzt, nb, u, w, lds);
+        }
     }
     if (!a.part) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
+        sum[i] += __shfl_xor(sum[i], 8);
         sum[i] += __shfl_xor(sum[i], 16);
         sum[i] += __shfl_xor(sum[i], 32);
     }
     const int64_t row = tb0 / a.per;
-    if ((threadIdx.x & 63) < 16)
+    if ((threadIdx.x & 63) < 8)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (c + i < a.N) a.part[row * a.N + c + i] = sum[i];
@@ -224,17 +242,19 @@ __device__ __forceinline__ void grad_unit(const GradArgs& a, int64_t tb0, int64_
 template <class T>
 __global__ __launch_bounds__(256) void k_linear_grad(GradArgs a)
 {
+    __shared__ __attribute__((aligned(16))) char smem[4 * 4096];
+    char* lds = smem + (threadIdx.x >> 6) * 4096;  // of this wave
     int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (unit < a.dz_units) {
         const int64_t run = unit / a.dz_strips, strip = unit - run * a.dz_strips, tb0 = run * a.per;
         if (a.act == kActNone)
-            grad_unit<T, kActNone>(a, tb0, strip);
+            grad_unit<T, kActNone>(a, tb0, strip, lds);
         else if (a.act == kActRelu)
-            grad_unit<T, kActRelu>(a, tb0, strip);
+            grad_unit<T, kActRelu>(a, tb0, strip, lds);
         else if (a.act == kActGelu)
-            grad_unit<T, kActGelu>(a, tb0, strip);
+            grad_unit<T, kActGelu>(a, tb0, strip, lds);
         else
-            grad_unit<T, kActSilu>(a, tb0, strip);
+            grad_unit<T, kActSilu>(a, tb0, strip, lds);
         return;
     }
     unit -= a.dz_units;
@@ -242,24 +262,25 @@ __global__ __launch_bounds__(256) void k_linear_grad(GradArgs a)
     const int64_t mb = unit / a.x_strips;
     const Micro u = micro_of(mb, unit - mb * a.x_strips);
     const int64_t kb = (a.K + 31) / 32;
-    if (u.c >= kb * 32) return;
     const CkptShape cs(a.M, a.K);
     MicroCkpt k;
     if (u.c < a.K && mb < cs.tb)
         k.load(a.xq, cs, u);
     else
         k.zero();
-    u32x4 o[8];
+    uint2 o[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float s = k.scale(i);
+        unsigned w[2];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int t = 0; t < 2; ++t) {
             const int64_t m = mb * 32 + u.t0 + 2 * t;
-            o[i][t] = pack2<T>(m < a.M ? k.code(2 * t, i) * s : 0.f, m + 1 < a.M ? k.code(2 * t + 1, i) * s : 0.f);
+            w[t] = pack2<T>(m < a.M ? k.code(2 * t, i) * s : 0.f, m + 1 < a.M ? k.code(2 * t + 1, i) * s : 0.f);
         }
+        o[i] = make_uint2(w[0], w[1]);
     }
-    store_operand(a.xt, kb, u, o);
+    store_operand(a.xt, kb, u, o, lds);
 }
 
 // dbias[n] = sum of the runs' partial sums: 16 strands of every 16th run, each in order, then the strands in order
@@ -286,7 +307,7 @@ __global__ __launch_bounds__(256) void k_bias_sum(const float* part, int64_t run
 
 hipError_t launch_checkpoint_pack(const CkptArgs& a, hipStream_t st)
 {
-    const int64_t strips = (a.C + 127) / 128, blocks = ((a.M + 31) / 32 * strips + 3) / 4;
+    const int64_t strips = (a.C + kStrip - 1) / kStrip, blocks = ((a.M + 31) / 32 * strips + 3) / 4;
     if (a.f16)
         k_ckpt_pack<F16><<<(unsigned)blocks, 256, 0, st>>>(a, (int)strips);
     else
@@ -296,7 +317,7 @@ hipError_t launch_checkpoint_pack(const CkptArgs& a, hipStream_t st)
 
 hipError_t launch_checkpoint_unpack(const CkptArgs& a, hipStream_t st)
 {
-    const int64_t strips = (a.C + 127) / 128, blocks = ((a.M + 31) / 32 * strips + 3) / 4;
+    const int64_t strips = (a.C + kStrip - 1) / kStrip, blocks = ((a.M + 31) / 32 * strips + 3) / 4;
     if (a.f16)
         k_ckpt_unpack<F16><<<(unsigned)blocks, 256, 0, st>>>(a, (int)strips);
     else
@@ -307,9 +328,9 @@ hipError_t launch_checkpoint_unpack(const CkptArgs& a, hipStream_t st)
 hipError_t launch_linear_grad(GradArgs a, int f16, hipStream_t st)
 {
     const int64_t tbs = operand_blocks(a.M);
-    a.dz_strips = a.dzt || a.dza || a.part ? (a.N + 127) / 128 : 0;
+    a.dz_strips = a.dzt || a.dza || a.part ? (a.N + kStrip - 1) / kStrip : 0;
     a.dz_units = (tbs + a.per - 1) / a.per * a.dz_strips;
-    a.x_strips = a.xt ? (a.K + 127) / 128 : 0;
+    a.x_strips = a.xt ? (a.K + kStrip - 1) / kStrip : 0;
     a.x_units = tbs * a.x_strips;
     const int64_t blocks = (a.dz_units + a.x_units + 3) / 4;
     if (!blocks) return hipSuccess;

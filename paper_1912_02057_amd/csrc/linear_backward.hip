@@ -234,8 +234,8 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 // Runs of token blocks whose sums of dz are kept apart: few for a long batch, one block each while there are few waves.
 int64_t blocks_per_run(int64_t M, int64_t N)
 {
-    const int64_t units = operand_blocks(M) * ((N + 127) / 128);
-    return units >= 8 * 4096 ? 8 : units >= 2 * 4096 ? 2 : 1;
+    const int64_t units = operand_blocks(M) * ((N + 63) / 64);
+    return units >= 8 * 8192 ? 8 : units >= 2 * 8192 ? 2 : 1;
 }
 
 struct BwdWork {

@@ -95,7 +95,7 @@ int make_geom(int64_t Nb, int64_t C, int64_t H, int64_t W, int64_t O, int KH, in
 constexpr int64_t kMaxFeatures = 1LL << 21;
 bool linear_dims(int64_t N, int64_t K) { return N > 0 && K > 0 && N <= kMaxFeatures && K <= kMaxFeatures; }
 bool linear_rows(int64_t M, int64_t len, int64_t ld) { return M >= 0 && M <= kMaxDim && ld >= len && ld <= (1LL << 31); }
-bool ckpt_units(int64_t M, int64_t C) { return (double)((M + 31) / 32) * (double)((C + 127) / 128) < (double)(1LL << 31); }
+bool ckpt_units(int64_t M, int64_t C) { return (double)((M + 63) / 32) * (double)((C + 63) / 64) < (double)(1LL << 31); }
 bool known_act(rtn_act act) { return act >= RTN_ACT_NONE && act <= RTN_ACT_SILU; }
 
 }  // namespace

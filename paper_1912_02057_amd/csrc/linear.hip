@@ -153,23 +153,25 @@ __device__ __forceinline__ u32x4 expand(uint2 word)
 
 template <int BM, int BN, int NS>
 struct LinTile {
-    static constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32, NM = TM * TN;
+    static constexpr int WN = BN / 4, TM = BM / 32, TN = WN / 32, NM = TM * TN;
     static constexpr int ABYTES = BM * 128, STAGE = ABYTES + BN * 16, XDMA = BM / 32, DPS = XDMA + 1;
     static constexpr int ZPITCH = WN * 4 + 16, ZBYTES = 32 * ZPITCH;  // a wave's 32 rows of fp32 in the epilogue
     static constexpr int LDS = NS * STAGE > 4 * ZBYTES ? NS * STAGE : 4 * ZBYTES;
-    static constexpr int PER_CU = NM >= 16 ? 1 : 2;  // blocks that registers and LDS allow
 };
 
-// A block of 4 waves (2 x 2) owns BM tokens x BN outputs.  Ring of NS stages of 64 columns: x rows of 128 bytes, 16-byte
+// A block of 4 waves owns BM tokens x BN outputs, a wave all the tokens of a quarter of the outputs, so that no weight is widened
+// twice: large products are bound by the power limit (clock 1.7 GHz while the matrix cores are busy 84 % of it), and with the waves 2 x
+// 2 instead the redundant vector operations cost 3 to 4 %: 16384 x 8192 x 8192 1540 us against 1490.  Two blocks share a CU, so one's
+// epilogue passes beside the other's products (one block of 256 x 256: 1660 us).  Ring of NS stages of 64 columns: x rows of 128 bytes, 16-byte
 // chunk c of row r at place c ^ (r >> 1 & 7), so that 16 rows' fragments hit all banks; then the weights' words.  One barrier per
 // step, before the last of its four 16-column slices, and fragments are read one slice ahead.
 template <class T, int BM, int BN, int NS>
-__global__ __launch_bounds__(256, (LinTile<BM, BN, NS>::PER_CU)) void k_linear(LinParams p)
+__global__ __launch_bounds__(256, 2) void k_linear(LinParams p)
 {
     using L = LinTile<BM, BN, NS>;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave >> 1, wn = wave & 1, l32 = lane & 31, h = lane >> 5;
+    const int l32 = lane & 31, h = lane >> 5;
 
     int tm, tn;
     {
@@ -225,7 +227,7 @@ __global__ __launch_bounds__(256, (LinTile<BM, BN, NS>::PER_CU)) void k_linear(L
 
     u32x4 xf[2][L::TM], wf[2][L::TN];
     uint2 words[L::TN];
-    const int xbase = (wm * L::WM + l32) * 128 + ((h ^ ((l32 >> 1) & 7)) * 16), wbase = L::ABYTES + wn * L::TN * 512 + lane * 8;
+    const int xbase = l32 * 128 + ((h ^ ((l32 >> 1) & 7)) * 16), wbase = L::ABYTES + wave * L::TN * 512 + lane * 8;
 
     for (int s = 0; s < NS - 1 && s < nk; ++s) issue(s, s);
     wait_groups<L::DPS>((nk < NS - 1 ? nk : NS - 1) - 1);
@@ -317,7 +319,7 @@ __global__ __launch_bounds__(256, (LinTile<BM, BN, NS>::PER_CU)) void k_linear(L
     __syncthreads();
     constexpr int CL = L::WN / 8, TPL = CL / 2;
     char* zs = smem + wave * L::ZBYTES;
-    const int n8 = n0 + wn * L::WN + (lane % CL) * 8, t0 = (lane / CL) * TPL;
+    const int n8 = n0 + wave * L::WN + (lane % CL) * 8, t0 = (lane / CL) * TPL;
     float al[8], bi[8];
     if (n8 < p.N) load_affine<T>(p, n8, al, bi);
 #pragma unroll 1
@@ -333,9 +335,9 @@ __global__ __launch_bounds__(256, (LinTile<BM, BN, NS>::PER_CU)) void k_linear(L
                         make_float4(acc[i][kk][4 * q], acc[i][kk][4 * q + 1], acc[i][kk][4 * q + 2], acc[i][kk][4 * q + 3]);
         };
         for_each_index(put, std::make_integer_sequence<int, L::TM>{});
-        const int mt = m0 + wm * L::WM + k * 32;  // first token
-        if (mt >= p.M || n0 + wn * L::WN >= p.N) continue;
-        const bool whole = mt + 32 <= p.M && n0 + (wn + 1) * L::WN <= p.N;
+        const int mt = m0 + k * 32;  // first token
+        if (mt >= p.M || n0 + wave * L::WN >= p.N) continue;
+        const bool whole = mt + 32 <= p.M && n0 + (wave + 1) * L::WN <= p.N;
         wait_lgkm0();
         auto row_z = [&](int t, float(&z)[8]) {
             const float* row = (const float*)(zs + (t0 + t) * L::ZPITCH + (lane % CL) * 32);

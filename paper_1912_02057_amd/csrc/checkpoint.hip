@@ -283,26 +283,6 @@ __global__ __launch_bounds__(256) void k_linear_grad(GradArgs a)
     store_operand(a.xt, kb, u, o, lds);
 }
 
-// dbias[n] = sum of the runs' partial sums: 16 strands of every 16th run, each in order, then the strands in order
-template <class T>
-__global__ __launch_bounds__(256) void k_bias_sum(const float* part, int64_t runs, int64_t N, unsigned short* out)
-{
-    __shared__ float sums[16][16];
-    const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
-    const int64_t n = (int64_t)blockIdx.x * 16 + c;
-    float s = 0.f;
-    if (n < N) {
-#pragma unroll 4
-        for (int64_t r = g; r < runs; r += 16) s += part[r * N + n];
-    }
-    sums[g][c] = s;
-    __syncthreads();
-    if (g || n >= N) return;
-#pragma unroll
-    for (int i = 1; i < 16; ++i) s += sums[i][c];
-    out[n] = T::from_float(s);
-}
-
 }  // namespace
 
 hipError_t launch_checkpoint_pack(const CkptArgs& a, hipStream_t st)
@@ -338,16 +318,6 @@ hipError_t launch_linear_grad(GradArgs a, int f16, hipStream_t st)
         k_linear_grad<F16><<<(unsigned)blocks, 256, 0, st>>>(a);
     else
         k_linear_grad<BF16><<<(unsigned)blocks, 256, 0, st>>>(a);
-    return hipGetLastError();
-}
-
-hipError_t launch_bias_sum(const float* part, int64_t runs, int64_t N, void* out, int f16, hipStream_t st)
-{
-    const unsigned blocks = (unsigned)((N + 15) / 16);
-    if (f16)
-        k_bias_sum<F16><<<blocks, 256, 0, st>>>(part, runs, N, (unsigned short*)out);
-    else
-        k_bias_sum<BF16><<<blocks, 256, 0, st>>>(part, runs, N, (unsigned short*)out);
     return hipGetLastError();
 }
 

@@ -12,6 +12,28 @@ namespace rtn {
 
 namespace {
 
+// dbias[n] = sum of the runs' partial sums: four strands of every fourth run, each in order, then the strands in order.  A block of
+// 256 threads has 64 outputs; `sums` 256 floats of LDS.
+__host__ __device__ inline int bias_blocks(const BiasSum& b) { return b.out ? (int)((b.N + 63) / 64) : 0; }
+template <class T>
+__device__ __forceinline__ void bias_sum(const BiasSum& b, int block, float* sums)
+{
+    if (block >= bias_blocks(b)) return;
+    const int c = threadIdx.x & 63, g = threadIdx.x >> 6;
+    const int64_t n = (int64_t)block * 64 + c;
+    float s = 0.f;
+    if (n < b.N) {
+#pragma unroll 8
+        for (int64_t r = g; r < b.runs; r += 4) s += b.part[r * b.N + n];
+    }
+    sums[g * 64 + c] = s;
+    __syncthreads();
+    if (g || n >= b.N) return;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) s += sums[i * 64 + c];
+    ((unsigned short*)b.out)[n] = T::from_float(s);
+}
+
 struct WgParams {
     const char *x, *d;  // x^ and dz in operand order
     int N, K, nk;       // nk: steps of 64 tokens
@@ -19,6 +41,7 @@ struct WgParams {
     int tilesN, ntiles, band_tiles;
     FastDiv div_band, div_lastband;
     void* dw;
+    BiasSum bias;       // blocks behind the tiles'
 };
 
 template <int BN, int BK>
@@ -29,6 +52,13 @@ struct WgTile {
     static constexpr int ZPITCH = WK * 4 + 16, ZBYTES = 32 * ZPITCH;
     static constexpr int LDS = SLOTS * SLOT > 4 * ZBYTES ? SLOTS * SLOT : 4 * ZBYTES;
 };
+
+template <class T>
+__global__ __launch_bounds__(256) void k_bias_sum(BiasSum b)
+{
+    __shared__ float sums[256];
+    bias_sum<T>(b, blockIdx.x, sums);
+}
 
 // A block of 4 waves (2 x 2) owns BN x BK of dw.  A step is 64 tokens, two slots of a ring of five; fragments are read one
 // 16-token slice ahead, so that before the last slice of a step nothing is left to read of its slots.  Behind the one barrier
@@ -43,7 +73,12 @@ __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgP
     const int wn = wave >> 1, wk = wave & 1, l32 = lane & 31, h = lane >> 5;
     int tn, tk;
     {
-        const int chunk = (int)(gridDim.x >> 3), bid = (int)(blockIdx.x & 7) * chunk + (int)(blockIdx.x >> 3);
+        // each XCD has a run of the tiles, then of the sums
+        const int chunk = (p.ntiles + 7) >> 3, at = (int)(blockIdx.x >> 3), bid = (int)(blockIdx.x & 7) * chunk + at;
+        if (at >= chunk) {
+            bias_sum<T>(p.bias, (at - chunk) * 8 + (int)(blockIdx.x & 7), (float*)smem);
+            return;
+        }
         if (bid >= p.ntiles) return;
         band_tile(bid, p.tilesN, p.band_tiles, [&](int n) { return (int)fastdiv((uint32_t)n, p.div_band); },
                   [&](int n) { return (int)fastdiv((uint32_t)n, p.div_lastband); }, tn, tk);
@@ -208,7 +243,8 @@ hipError_t run_tile(WgParams& p, hipStream_t st)
     p.tilesN = (p.N + BN - 1) / BN;
     const int tilesK = (p.K + BK - 1) / BK;
     const int64_t nt = (int64_t)p.tilesN * tilesK;
-    if (nt > 0x7fffff00) return hipErrorInvalidValue;
+    const int64_t blocks = (nt + 7) / 8 * 8 + bias_blocks(p.bias);
+    if (blocks > 0x7fffff00) return hipErrorInvalidValue;
     p.ntiles = (int)nt;
     p.band_tiles = 8 * tilesK;
     p.div_band = make_fastdiv((uint32_t)p.band_tiles);
@@ -216,7 +252,7 @@ hipError_t run_tile(WgParams& p, hipStream_t st)
     static LdsLimit limit;
     const hipError_t e = limit.raise((const void*)&k_wgrad<T, BN, BK, F32>, L::LDS);
     if (e != hipSuccess) return e;
-    k_wgrad<T, BN, BK, F32><<<(unsigned)((nt + 7) / 8 * 8), 256, L::LDS, st>>>(p);
+    k_wgrad<T, BN, BK, F32><<<(unsigned)((blocks + 7) / 8 * 8), 256, L::LDS, st>>>(p);
     return hipGetLastError();
 }
 
@@ -251,6 +287,15 @@ struct BwdWork {
     }
 };
 
+hipError_t launch_bias_sum(const BiasSum& b, int f16, hipStream_t st)
+{
+    if (f16)
+        k_bias_sum<F16><<<(unsigned)bias_blocks(b), 256, 0, st>>>(b);
+    else
+        k_bias_sum<BF16><<<(unsigned)bias_blocks(b), 256, 0, st>>>(b);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_linear_wgrad(const WgradArgs& a, hipStream_t st)
@@ -260,6 +305,7 @@ hipError_t launch_linear_wgrad(const WgradArgs& a, hipStream_t st)
     p.N = (int)a.N, p.K = (int)a.K, p.nk = (int)((a.M + 63) / 64);
     p.xpitch = (a.K + 31) / 32 * 2048, p.dpitch = (a.N + 31) / 32 * 2048;
     p.dw = a.dw;
+    p.bias = a.bias;
     if (a.f16) return a.dw_f32 ? run<F16, true>(p, st) : run<F16, false>(p, st);
     return a.dw_f32 ? run<BF16, true>(p, st) : run<BF16, false>(p, st);
 }
@@ -294,15 +340,10 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t st)
         l.workspace = a.workspace + w.dza;
         if ((e = launch_linear(l, st)) != hipSuccess) return e;
     }
-    if (a.dw) {
-        WgradArgs d = {g.dzt, g.xt, a.M, a.N, a.K, a.dw, a.f16, a.dw_f32};
-        if ((e = launch_linear_wgrad(d, st)) != hipSuccess) return e;
-    }
-    if (a.dbias) {
-        const int64_t tb = operand_blocks(a.M);
-        if ((e = launch_bias_sum(g.part, (tb + g.per - 1) / g.per, a.N, a.dbias, a.f16, st)) != hipSuccess) return e;
-    }
-    return hipSuccess;
+    BiasSum bias = {};
+    if (a.dbias) bias = {g.part, (operand_blocks(a.M) + g.per - 1) / g.per, a.N, a.dbias};
+    if (a.dw) return launch_linear_wgrad(WgradArgs{g.dzt, g.xt, a.M, a.N, a.K, a.dw, a.f16, a.dw_f32, bias}, st);
+    return a.dbias ? launch_bias_sum(bias, a.f16, st) : hipSuccess;
 }
 
 }  // namespace rtn

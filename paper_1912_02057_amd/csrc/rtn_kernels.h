@@ -278,7 +278,12 @@ struct GradArgs {
     int64_t dz_strips, dz_units, x_strips, x_units;
 };
 hipError_t launch_linear_grad(GradArgs a, int f16, hipStream_t st);
-hipError_t launch_bias_sum(const float* part, int64_t runs, int64_t N, void* out, int f16, hipStream_t st);
+// out[n] = sum over r of part[r][n], 16 bit; out NULL: nothing
+struct BiasSum {
+    const float* part;
+    int64_t runs, N;
+    void* out;
+};
 
 // dw[n][k] = sum_m dz[m][n] x^[m][k], both operands in operand order
 struct WgradArgs {
@@ -286,6 +291,7 @@ struct WgradArgs {
     int64_t M, N, K;
     void* dw;  // [N][K]
     int f16, dw_f32;
+    BiasSum bias;  // in the same launch
 };
 hipError_t launch_linear_wgrad(const WgradArgs& a, hipStream_t st);
 

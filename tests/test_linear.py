@@ -12,7 +12,8 @@ pytestmark = pytest.mark.gpu
 # one token, a few, the edges of the kernels' token counts and tiles (32, 64, 128, 256), odd sizes, rows that are no whole
 # 16 bytes, columns that end inside a 64-step, and enough tiles for each tile size
 SIZES = [(1, 64, 64), (1, 4096, 1024), (2, 33, 70), (7, 100, 1000), (31, 250, 264), (32, 96, 2187), (33, 256, 256), (64, 65, 1),
-         (65, 1, 130), (100, 31, 63), (129, 300, 200), (257, 515, 1027), (700, 1100, 328), (1800, 1800, 72), (3700, 3700, 40)]
+         (65, 1, 130), (100, 31, 63), (129, 300, 200), (257, 515, 1027), (700, 1100, 328), (1800, 1800, 72), (3700, 3700, 40),
+         (9, 4160, 520), (16, 100, 520), (300, 900, 1000), (500, 1500, 2187), (1100, 1000, 2000)]
 
 
 def run(L, name, w, **kw):
@@ -301,3 +302,18 @@ def test_offsets_beyond_32_bits():
     (dxs, ex), (dws, ew), _ = L.grads64("none", T.f64(back[-96:]), None)
     T.assert_within(dx[-96:], dxs, L.rounded(dxs, ex), "dx")
     T.assert_within(dw, dws, ew, "dw")                       # only the last rows of x are not zero
+
+
+def test_feed_forward_block_trains_and_answers():
+    """The example: the loss against a teacher falls, and one token alone is answered as among others (the forms add in other
+    orders, and h is rounded to 16 bits in between: two roundings of y and one of h of an ulp each)."""
+    from paper_1912_02057_amd import ternary_mlp as E
+    block, losses = E.train(steps=40, tokens=256, width=128, hidden=320)
+    assert losses[-1] < 0.75 * losses[0], losses
+    block.freeze()
+    x = torch.randn((40, 128), device=T.DEV).to(torch.bfloat16)
+    y, one = T.f64(block(x)), np.concatenate([T.f64(block(x[i:i + 1])) for i in range(40)])
+    h = T.f64(block.up(x, T.ACTS["gelu"]))
+    t2 = np.abs(T.f64(block.down.w)) > E.THRESHOLD
+    bound = 2 * T.U["bf16"] * np.maximum(np.abs(y), np.abs(one)) + 2 * T.U["bf16"] * (np.abs(h) @ t2.T) * T.f64(block.down.alpha)
+    T.assert_within(one, y, bound, "one token")

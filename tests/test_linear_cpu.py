@@ -1,12 +1,14 @@
 """What the entry points of the ternary linear layer and of the 8-bit checkpoints refuse, on a host without a GPU: every
-check comes before any launch."""
+check comes before any launch.  And the rule that picks the product's form, compiled for the host."""
 import ctypes as C
 import os
+import subprocess
 
 import pytest
 import torch
 
 from paper_1912_02057_amd import binding as B
+from test_linear import SIZES
 
 FAKE, OTHER = C.c_void_p(0x10000), C.c_void_p(0x20000)   # never dereferenced: validation fails first
 ODD, HALF = C.c_void_p(0x10001), C.c_void_p(0x10002)
@@ -119,3 +121,39 @@ def test_binding_refuses_tensors_it_cannot_pass_on():
         B.linear_backward(x, w, 64, 1.0, w)
     with pytest.raises(ValueError):
         B.linear_prepare(torch.zeros((64, 64), dtype=torch.int8), 64, 64)
+
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_1912_02057_amd", "csrc")
+
+
+@pytest.fixture(scope="module")
+def form(tmp_path_factory):
+    d = tmp_path_factory.mktemp("form")
+    (d / "f.cpp").write_text("""#include "choice.h"
+extern "C" int form(int64_t M, int64_t N, int64_t K, int z) { return (int)rtn::linear_form(M, N, K, z != 0); }
+""")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I" + CSRC, str(d / "f.cpp"), "-o", str(d / "f.so")], check=True)
+    f = C.CDLL(str(d / "f.so")).form
+    f.argtypes = [C.c_int64, C.c_int64, C.c_int64, C.c_int]
+    return f
+
+
+def test_forms_follow_the_sizes(form):
+    few, split32, split32x64, split64, tile128, tile256 = range(6)
+    assert form(1, 4096, 4096, 0) == few and form(16, 4096, 4096, 0) == few and form(16, 8192, 8192, 0) == split32
+    assert form(1, 4096, 4096, 1) != few                      # a checkpoint's groups need all tokens of 32
+    assert form(64, 4096, 4096, 0) == split32 and form(512, 2048, 2048, 0) == split64
+    assert form(1024, 4096, 1024, 0) == tile128 and form(2048, 2048, 2048, 0) == tile128
+    assert form(4096, 4096, 4096, 0) == tile256 and form(16384, 8192, 8192, 0) == tile256
+    # large sizes do not overflow on the way, and every size has a form
+    assert form(0x7fffffff - 1024, 1 << 21, 1 << 21, 0) == tile256
+    for M in (1, 17, 100, 5000):
+        for N in (1, 100, 5000):
+            for K in (1, 100, 5000):
+                assert few <= form(M, N, K, 0) <= tile256
+
+
+def test_parity_sizes_reach_every_form(form):
+    """With and without a checkpoint; dx is the same kernels on the transposed weights."""
+    assert {form(M, N, K, 0) for M, N, K in SIZES} == set(range(6))
+    assert {form(M, N, K, 1) for M, N, K in SIZES} == set(range(1, 6))

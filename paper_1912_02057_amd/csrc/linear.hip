@@ -282,7 +282,7 @@ __global__ __launch_bounds__(256, 2) void k_linear(LinParams p)
             for_each_index(
                 [&](auto mi) {
                     constexpr int n = decltype(mi)::value, i = n / L::TM, k = n % L::TM;
-                    acc[i][k] = T::mfma(wf[cur][i], xf[cur][k], acc[i][k]);
+                    acc[i][k] = T::mfma(xf[cur][k], wf[cur][i], acc[i][k]);
 #pragma unroll
                     for (int f = n * FPER; f < (n + 1) * FPER && f < NF; ++f) read(f);
                     for_each_index(
@@ -330,9 +330,8 @@ __global__ __launch_bounds__(256, 2) void k_linear(LinParams p)
 #pragma unroll
             for (int i = 0; i < L::TN; ++i)
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    *(float4*)(zs + l32 * L::ZPITCH + (i * 32 + q * 8 + h * 4) * 4) =
-                        make_float4(acc[i][kk][4 * q], acc[i][kk][4 * q + 1], acc[i][kk][4 * q + 2], acc[i][kk][4 * q + 3]);
+                for (int r = 0; r < 16; ++r)  // row 8 (r / 4) + 4 h + r % 4, column l32
+                    *(float*)(zs + (8 * (r >> 2) + 4 * h + (r & 3)) * L::ZPITCH + (i * 32 + l32) * 4) = acc[i][kk][r];
         };
         for_each_index(put, std::make_integer_sequence<int, L::TM>{});
         const int mt = m0 + k * 32;  // first token

@@ -26,17 +26,7 @@ __device__ __forceinline__ Micro micro_of(int64_t mb, int64_t strip)
 // 8 channels of a row as they are; zeros past the end
 __device__ __forceinline__ u32x4 load_row(const unsigned short* x, int64_t ld, int64_t m, int64_t M, int64_t c, int64_t C)
 {
-    u32x4 v = {0, 0, 0, 0};
-    if (m >= M) return v;
-    const unsigned short* r = x + m * ld + c;
-    if (c + 8 <= C) {  // wherever the row starts: global accesses need no alignment on this target
-        __builtin_memcpy(&v, r, 16);
-        return v;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (c + i < C) v[i >> 1] |= (unsigned)r[i] << (16 * (i & 1));
-    return v;
+    return m < M ? load_row8(x + m * ld, c, C) : u32x4{0, 0, 0, 0};
 }
 
 template <class T>

@@ -26,15 +26,6 @@ struct LinParams {
     int act;
 };
 
-// 16 bytes of a row wherever it starts (global accesses need no alignment on this target)
-__device__ __forceinline__ u32x4 load16(const void* p)
-{
-    u32x4 v;
-    __builtin_memcpy(&v, p, 16);
-    return v;
-}
-__device__ __forceinline__ void store16(void* p, u32x4 v) { __builtin_memcpy(p, &v, 16); }
-
 // The parameters of 8 consecutive outputs (0 past the end).
 template <class T>
 __device__ __forceinline__ void load_affine(const LinParams& p, int n, float (&al)[8], float (&bi)[8])
@@ -68,18 +59,18 @@ __device__ __forceinline__ void finish_row(const LinParams& p, int m, int n, con
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = act_value<ACT>(z[i]);
+    if (p.res) {
+        const u32x4 q = WHOLE ? load16(p.res + m * p.ldr + n) : load_row8(p.res + m * p.ldr, n, p.N);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += half_of<T>(q[i >> 1], i & 1);
+    }
     unsigned short* y = p.y + m * p.ldy + n;
     if (WHOLE || n + 8 <= p.N) {
-        if (p.res) {
-            const u32x4 q = load16(p.res + m * p.ldr + n);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += half_of<T>(q[i >> 1], i & 1);
-        }
         store16(y, u32x4{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])});
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (n + i < p.N) y[i] = T::from_float(p.res ? v[i] + T::to_float(p.res[m * p.ldr + n + i]) : v[i]);
+            if (n + i < p.N) y[i] = T::from_float(v[i]);
     }
 }
 
@@ -281,7 +272,7 @@ __global__ __launch_bounds__(256, 2) void k_linear(LinParams p)
             };
             for_each_index(
                 [&](auto mi) {
-                    constexpr int n = decltype(mi)::value, i = n / L::TM, k = n % L::TM;
+                    constexpr int n = decltype(mi)::value, i = n / L::TM, k = i & 1 ? L::TM - 1 - n % L::TM : n % L::TM;  // one operand changes at a time
                     acc[i][k] = T::mfma(xf[cur][k], wf[cur][i], acc[i][k]);
 #pragma unroll
                     for (int f = n * FPER; f < (n + 1) * FPER && f < NF; ++f) read(f);
@@ -441,16 +432,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_linear_few(LinParams p)
         if constexpr (ROW16) {
             return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xr, xoff, step * 128 + 64 * s, 0));
         } else {
-            const int k = step * 64 + 32 * s + 8 * c;
-            u32x4 v = {0, 0, 0, 0};
-            if (k + 8 <= p.K) {
-                v = load16(xrow + k);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (k + i < p.K) v[i >> 1] |= (unsigned)xrow[k + i] << (16 * (i & 1));
-            }
-            return v;
+            return load_row8(xrow, step * 64 + 32 * s + 8 * c, p.K);
         }
     };
     // what the outputs need beside the sums, fetched with the first weights: thread 16 RB m + i has output i of token m
@@ -529,8 +511,10 @@ struct SplitTile {
 };
 
 // Small grids: a block has 32 TT tokens x 32 RB outputs and its waves share the columns, every WAVES-th step each, with rings
-// of their own in LDS (D stages) and no barrier until their sums are added up in LDS.
-template <class T, int TT, int RB, int WAVES, int D>
+// of their own in LDS (D stages) and no barrier until their sums are added up in LDS.  ROW16: rows of whole 16-byte units, which
+// direct loads bring there; any others come through registers, a step ahead (1000 x 1003 x 2187: COPYT us where rows copied into
+// such units first take 15.5).
+template <class T, int TT, int RB, int WAVES, int D, bool ROW16>
 __global__ __launch_bounds__(WAVES * 64) void k_linear_split(LinParams p)
 {
     using L = SplitTile<TT, RB, WAVES, D>;
@@ -579,21 +563,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_linear_split(LinParams p)
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
     const int xbase = l32 * 128 + ((h ^ ((l32 >> 1) & 7)) * 16), wbase = L::XBYTES + lane * 8;
     const int count = wave < nk ? (nk - wave + WAVES - 1) / WAVES : 0;
-    for (int i = 0; i < D && i < count; ++i) issue(wave + i * WAVES, i);
-    int slot = 0;
-    for (int i = 0; i < count; ++i) {
-        wait_groups<L::DPS>(count - 1 - i < D - 1 ? count - 1 - i : D - 1);
-        const char* stage = ring + slot * L::STAGE;
-        uint2 words[RB];
-        u32x4 xf[4][TT];
-#pragma unroll
-        for (int r = 0; r < RB; ++r) words[r] = *(const uint2*)(stage + wbase + r * 512);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int t = 0; t < TT; ++t) xf[j][t] = *(const u32x4*)(stage + (xbase ^ (32 * j)) + t * 4096);
-        wait_lgkm0();
-        if (i + D < count) issue(wave + (i + D) * WAVES, slot);
+    auto products = [&](const u32x4(&xf)[4][TT], const uint2(&words)[RB]) {
         for_each_index(
             [&](auto index) {
                 constexpr int j = decltype(index)::value;
@@ -605,7 +575,69 @@ __global__ __launch_bounds__(WAVES * 64) void k_linear_split(LinParams p)
                 }
             },
             std::make_integer_sequence<int, 4>{});
-        slot = slot + 1 == D ? 0 : slot + 1;
+    };
+    auto read_x = [&](const char* stage, u32x4(&xf)[4][TT]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int t = 0; t < TT; ++t) xf[j][t] = *(const u32x4*)(stage + (xbase ^ (32 * j)) + t * 4096);
+    };
+    if constexpr (ROW16) {
+        for (int i = 0; i < D && i < count; ++i) issue(wave + i * WAVES, i);
+        int slot = 0;
+        for (int i = 0; i < count; ++i) {
+            wait_groups<L::DPS>(count - 1 - i < D - 1 ? count - 1 - i : D - 1);
+            const char* stage = ring + slot * L::STAGE;
+            uint2 words[RB];
+            u32x4 xf[4][TT];
+#pragma unroll
+            for (int r = 0; r < RB; ++r) words[r] = *(const uint2*)(stage + wbase + r * 512);
+            read_x(stage, xf);
+            wait_lgkm0();
+            if (i + D < count) issue(wave + (i + D) * WAVES, slot);
+            products(xf, words);
+            slot = slot + 1 == D ? 0 : slot + 1;
+        }
+    } else {
+        constexpr int AHEAD = 2;  // steps
+        u32x4 next[AHEAD][TT * 4];
+        uint2 ahead[AHEAD][RB];
+        auto load = [&](auto set, int step) {
+            constexpr int a = decltype(set)::value;
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                const int last = p.rb - 1 - n0 / 32;
+                ahead[a][r] = *((const uint2*)p.w + ((int64_t)(n0 / 32 + (r < last ? r : last)) * nk + step) * 64 + lane);
+            }
+#pragma unroll
+            for (int i = 0; i < TT * 4; ++i) {
+                const int row = i * 8 + (lane >> 3), last = p.M - 1 - m0, k = step * 64 + ((lane & 7) ^ ((row >> 1) & 7)) * 8;
+                next[a][i] = load_row8((const unsigned short*)p.x + (int64_t)(m0 + (row < last ? row : last)) * p.ldx, k, p.K);
+            }
+        };
+        auto one = [&](auto set, int i) {
+            constexpr int a = decltype(set)::value;
+            if (i >= count) return;
+            uint2 words[RB];
+            u32x4 xf[4][TT];
+#pragma unroll
+            for (int r = 0; r < RB; ++r) words[r] = ahead[a][r];
+#pragma unroll
+            for (int f = 0; f < TT * 4; ++f) *(u32x4*)(ring + f * 1024 + lane * 16) = next[a][f];
+            if (i + AHEAD < count) load(set, wave + (i + AHEAD) * WAVES);
+            wait_lgkm0();
+            read_x(ring, xf);
+            products(xf, words);
+        };
+        const std::integral_constant<int, 0> even{};
+        const std::integral_constant<int, 1> odd{};
+        if (count > 0) load(even, wave);
+        if (count > 1) load(odd, wave + WAVES);
+        for (int i = 0; i < count; i += AHEAD) {
+            one(even, i);
+            one(odd, i + 1);
+        }
+        wait_lgkm0();
     }
     // (this wave's ring is its own, and all of it has been read)
 #pragma unroll
@@ -667,16 +699,7 @@ __global__ __launch_bounds__(256) void k_copy_rows(const unsigned short* x, int6
     const int64_t per = ld / 8, n = M * per;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
         const int64_t m = i / per, k = (i - m * per) * 8;
-        const unsigned short* r = x + m * ldx + k;
-        u32x4 v = {0, 0, 0, 0};
-        if (k + 8 <= K) {
-            v = load16(r);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (k + j < K) v[j >> 1] |= (unsigned)r[j] << (16 * (j & 1));
-        }
-        *(u32x4*)(out + m * ld + k) = v;
+        *(u32x4*)(out + m * ld + k) = load_row8(x + m * ldx, k, K);
     }
 }
 
@@ -700,6 +723,8 @@ hipError_t run_tile(LinParams& p, hipStream_t st)
 }
 
 bool rows_of_16(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
+// Whether a tile's rows can be loaded straight into LDS: whole 16-byte units within the 32-bit offsets of up to 128 rows.
+bool direct_rows(const void* x, int64_t ldx, int64_t K) { return rows_of_16(x, ldx) && K % 8 == 0 && 128 * ldx * 2 + K * 2 < (int64_t)kOutside; }
 
 template <class T, int RB, int WAVES, int BATCH>
 hipError_t run_few(const LinParams& p, hipStream_t st)
@@ -712,8 +737,8 @@ hipError_t run_few(const LinParams& p, hipStream_t st)
     return hipGetLastError();
 }
 
-template <class T, int TT, int RB, int WAVES, int D>
-hipError_t run_split(LinParams& p, hipStream_t st)
+template <class T, int TT, int RB, int WAVES, int D, bool ROW16>
+hipError_t run_split_rows(LinParams& p, hipStream_t st)
 {
     using L = SplitTile<TT, RB, WAVES, D>;
     static_assert(L::LDS <= 160 * 1024, "");
@@ -721,10 +746,16 @@ hipError_t run_split(LinParams& p, hipStream_t st)
     const int64_t nt = (int64_t)p.tilesM * ((p.N + 32 * RB - 1) / (32 * RB));
     if (nt > 0x7fffff00) return hipErrorInvalidValue;
     static LdsLimit limit;
-    const hipError_t e = limit.raise((const void*)&k_linear_split<T, TT, RB, WAVES, D>, L::LDS);
+    const hipError_t e = limit.raise((const void*)&k_linear_split<T, TT, RB, WAVES, D, ROW16>, L::LDS);
     if (e != hipSuccess) return e;
-    k_linear_split<T, TT, RB, WAVES, D><<<(unsigned)nt, WAVES * 64, L::LDS, st>>>(p);
+    k_linear_split<T, TT, RB, WAVES, D, ROW16><<<(unsigned)nt, WAVES * 64, L::LDS, st>>>(p);
     return hipGetLastError();
+}
+
+template <class T, int TT, int RB, int WAVES, int D>
+hipError_t run_split(LinParams& p, hipStream_t st)
+{
+    return direct_rows(p.x, p.ldx, p.K) ? run_split_rows<T, TT, RB, WAVES, D, true>(p, st) : run_split_rows<T, TT, RB, WAVES, D, false>(p, st);
 }
 
 template <class T>
@@ -754,8 +785,8 @@ hipError_t run(const LinearArgs& a, LinParams p, hipStream_t st)
 
 bool linear_copies_x(const LinearArgs& a)
 {
-    if (linear_form(a.M, a.N, a.K, a.zq != nullptr) == LinearForm::kFew) return false;
-    return !rows_of_16(a.x, a.ldx) || a.K % 8 != 0 || 256 * a.ldx * 2 + a.K * 2 >= (int64_t)kOutside;
+    const LinearForm form = linear_form(a.M, a.N, a.K, a.zq != nullptr);
+    return (form == LinearForm::kTile128 || form == LinearForm::kTile256) && !direct_rows(a.x, a.ldx, a.K);
 }
 
 hipError_t launch_linear(const LinearArgs& a, hipStream_t st)

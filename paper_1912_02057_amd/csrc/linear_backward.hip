@@ -145,7 +145,7 @@ __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgP
             const unsigned base = lds0 + (unsigned)(slot_of(s0 + (j == 3 ? 0 : 3) + (part >> 1)) * L::SLOT);
             for_each_index(
                 [&](auto mi) {
-                    constexpr int n = decltype(mi)::value, i = n / L::TN, k = n % L::TN;
+                    constexpr int n = decltype(mi)::value, i = n / L::TN, k = i & 1 ? L::TN - 1 - n % L::TN : n % L::TN;  // one operand changes at a time
                     acc[i][k] = T::mfma(xf[cur][i], df[cur][k], acc[i][k]);
                     // the next slice's fragments, early in this one's products
                     constexpr int NF = L::TK + L::TN, PER = (NF + L::NM - 1) / L::NM;

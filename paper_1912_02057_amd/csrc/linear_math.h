@@ -120,6 +120,33 @@ __device__ __forceinline__ float normal_tail(float z, float& e)
     const float p = fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f) * 0.5f;
     return p * t * e;
 }
+// 16 bytes wherever they start (global accesses need no alignment on this target)
+__device__ __forceinline__ u32x4 load16(const void* p)
+{
+    u32x4 v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+__device__ __forceinline__ void store16(void* p, u32x4 v) { __builtin_memcpy(p, &v, 16); }
+// Elements k .. k + 7 of a row of `len`, zeros past its end: the row's last 16 bytes, shifted, where they do not all exist.  (One
+// load; eight conditional ones wait for each other.)
+__device__ __forceinline__ u32x4 load_row8(const unsigned short* row, int64_t k, int64_t len)
+{
+    if (k + 8 <= len) return load16(row + k);
+    if (k >= len) return u32x4{0, 0, 0, 0};
+    if (len < 8) {
+        u32x4 v = {0, 0, 0, 0};
+        for (int i = 0; i < 7; ++i)
+            if (k + i < len) v[i >> 1] |= (unsigned)row[k + i] << (16 * (i & 1));
+        return v;
+    }
+    const u32x4 t = load16(row + len - 8);
+    const int s = (int)(k + 8 - len) * 16;  // 16 .. 112
+    const uint64_t lo = t[0] | (uint64_t)t[1] << 32, hi = t[2] | (uint64_t)t[3] << 32;
+    const uint64_t l = s < 64 ? lo >> s | hi << (64 - s) : hi >> (s - 64), u = s < 64 ? hi >> s : 0;
+    return u32x4{(unsigned)l, (unsigned)(l >> 32), (unsigned)u, (unsigned)(u >> 32)};
+}
+
 // phi(z) in fp32.  gelu is z Phi(z) = max(z, 0) - |z| Q(|z|), Phi the normal distribution; silu z / (1 + exp(-z)).
 template <int ACT>
 __device__ __forceinline__ float act_value(float z)

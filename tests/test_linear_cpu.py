@@ -43,11 +43,12 @@ def test_sizes(L):
     assert L.rtn_checkpoint_bytes(1, 1) == 264
     assert L.rtn_checkpoint_bytes(33, 9) == 4 * 264
     assert L.rtn_checkpoint_bytes(0, 9) == 0 and L.rtn_checkpoint_bytes(5, -1) == 0
-    # rows of whole 16 bytes are read where they lie, others are copied; a few tokens never are
-    assert L.rtn_linear_workspace_bytes(FAKE, 128, 500, 300, 128, 0) == 0
-    assert L.rtn_linear_workspace_bytes(FAKE, 131, 500, 300, 128, 0) == 500 * 128 * 2
-    assert L.rtn_linear_workspace_bytes(FAKE, 136, 500, 300, 130, 0) == 500 * 192 * 2
-    assert L.rtn_linear_workspace_bytes(HALF, 128, 500, 300, 128, 0) == 500 * 128 * 2
+    # rows of whole 16 bytes are read where they lie, others are copied for the large tiles
+    assert L.rtn_linear_workspace_bytes(FAKE, 128, 5000, 3000, 128, 0) == 0
+    assert L.rtn_linear_workspace_bytes(FAKE, 131, 5000, 3000, 128, 0) == 5000 * 128 * 2
+    assert L.rtn_linear_workspace_bytes(FAKE, 136, 5000, 3000, 130, 0) == 5000 * 192 * 2
+    assert L.rtn_linear_workspace_bytes(HALF, 128, 5000, 3000, 128, 0) == 5000 * 128 * 2
+    assert L.rtn_linear_workspace_bytes(HALF, 128, 500, 300, 128, 0) == 0
     assert L.rtn_linear_workspace_bytes(HALF, 131, 1, 300, 130, 0) == 0
     assert L.rtn_linear_workspace_bytes(FAKE, 100, 500, 300, 128, 0) == 0          # a pitch below the row's length
     assert L.rtn_linear_backward_workspace_bytes(100, 64, 0) == 0
@@ -74,7 +75,8 @@ def test_linear_refuses(L):
         ({6: (1 << 21) + 1, 2: 1 << 22}, B.RTN_ERR_SHAPE), ({1: ODD}, B.RTN_ERR_ALIGN), ({13: ODD}, B.RTN_ERR_ALIGN), ({9: ODD}, B.RTN_ERR_ALIGN),
         ({11: ODD}, B.RTN_ERR_ALIGN), ({3: HALF}, B.RTN_ERR_ALIGN), ({15: HALF}, B.RTN_ERR_ALIGN),
         ({16: 4 * 8 * 264 - 1}, B.RTN_ERR_WORKSPACE),
-        ({1: HALF, 17: None}, B.RTN_ERR_WORKSPACE), ({1: HALF, 18: 100 * 128 - 1}, B.RTN_ERR_WORKSPACE), ({1: HALF, 17: HALF}, B.RTN_ERR_ALIGN)])
+        ({1: HALF, 4: 20000, 17: None}, B.RTN_ERR_WORKSPACE), ({1: HALF, 4: 20000, 18: 20000 * 128 - 1}, B.RTN_ERR_WORKSPACE),
+        ({1: HALF, 4: 20000, 17: HALF}, B.RTN_ERR_ALIGN)])
     assert L.rtn_linear(*[0 if i == 4 else None if i in (1, 13) else v for i, v in enumerate(ok)]) == B.RTN_OK   # nothing to do
 
 

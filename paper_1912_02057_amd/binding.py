@@ -564,10 +564,9 @@ def checkpoint_pack(x, ckpt=None):
 
 def checkpoint_unpack(ckpt, M, Cc, dtype, out=None):
     """What the checkpoint of an [M, Cc] tensor stands for, in bfloat16 or float16."""
-    if out is None:
-        out = torch.empty((M, Cc), dtype=dtype, device=ckpt.device)
-    assert tuple(out.shape) == (M, Cc) and out.dtype == dtype
-    return _made(_native().checkpoint_unpack(ckpt, out), "rtn_checkpoint_unpack")
+    if dtype not in (torch.bfloat16, torch.float16):
+        raise AssertionError("dtype: bfloat16 or float16 is required")
+    return _made(_native().checkpoint_unpack(ckpt, M, Cc, dtype is torch.float16, out), "rtn_checkpoint_unpack")
 
 
 def linear_backward(dy, prepared_t, K, alpha_w, x_ckpt, act=RTN_ACT_NONE, z_ckpt=None, want_dx=True, want_dw=True, want_dbias=True,

@@ -457,21 +457,22 @@ PyObject* checkpoint_pack(PyObject*, Args a, Py_ssize_t n)
     });
 }
 
-// ckpt, out
+// ckpt, M, C, float16 (else bfloat16), out
 PyObject* checkpoint_unpack(PyObject*, Args a, Py_ssize_t n)
 {
-    return call_for<1>(2, n, [&](at::Tensor* out) {
-        const at::Tensor& t = matrix(a[1], "out");
-        const rtn_dtype dt = dtype(t.scalar_type(), "out");
-        const int64_t M = t.size(0), C = t.size(1);
+    return call_for<1>(5, n, [&](at::Tensor* out) {
+        const at::Tensor& k = tensor(a[0], "ckpt");
+        const int64_t M = integer(a[1]), C = integer(a[2]);
+        const c10::ScalarType type = truth(a[3]) ? c10::kHalf : c10::kBFloat16;
+        const void* kp = bytes_of(k, rtn_checkpoint_bytes(M, C), "ckpt");
+        out[0] = given_or(a[4], "out", [&] { return make_rows(M, C, type, k); });
         int64_t ld;
-        void* y = rows2d(t, t.scalar_type(), M, C, "out", ld);
-        const void* k = bytes_of(a[0], rtn_checkpoint_bytes(M, C), "ckpt");
-        const size_t kb = raw_bytes(a[0], "ckpt");
-        out[0] = t;
+        void* y = rows2d(out[0], type, M, C, "out", ld);
+        const size_t kb = k.nbytes();
+        const rtn_dtype dt = dtype(type, "out");
         void* st = stream();
         const Unlocked u;
-        return rtn_checkpoint_unpack(dt, k, kb, M, C, y, ld, st);
+        return rtn_checkpoint_unpack(dt, kp, kb, M, C, y, ld, st);
     });
 }
 

@@ -512,8 +512,8 @@ struct SplitTile {
 
 // Small grids: a block has 32 TT tokens x 32 RB outputs and its waves share the columns, every WAVES-th step each, with rings
 // of their own in LDS (D stages) and no barrier until their sums are added up in LDS.  ROW16: rows of whole 16-byte units, which
-// direct loads bring there; any others come through registers, a step ahead (1000 x 1003 x 2187: COPYT us where rows copied into
-// such units first take 15.5).
+// direct loads bring there; any others come through registers, two steps ahead (1000 x 1003 x 2187 with gelu: 13.7 us, rows copied into
+// such units first 15.5).
 template <class T, int TT, int RB, int WAVES, int D, bool ROW16>
 __global__ __launch_bounds__(WAVES * 64) void k_linear_split(LinParams p)
 {
@@ -773,8 +773,8 @@ hipError_t run(const LinearArgs& a, LinParams p, hipStream_t st)
         p.K = (int)ld;
     }
     switch (form) {
-        case LinearForm::kSplit32: return run_split<T, 1, 1, 8, 4>(p, st);
-        case LinearForm::kSplit32x64: return run_split<T, 1, 2, 8, 3>(p, st);
+        case LinearForm::kSplit32: return run_split<T, 1, 1, 8, 2>(p, st);
+        case LinearForm::kSplit32x64: return run_split<T, 1, 2, 8, 2>(p, st);
         case LinearForm::kSplit64: return run_split<T, 2, 2, 8, 2>(p, st);
         case LinearForm::kTile128: return run_tile<T, 128, 128, 4>(p, st);
         default: return run_tile<T, 128, 256, 4>(p, st);

@@ -243,14 +243,15 @@ inline int pick_ksplit(const KsplitShape& s)
 enum class LinearForm { kFew, kSplit32, kSplit32x64, kSplit64, kTile128, kTile256 };
 constexpr int kFewTokens = 16, kFewOutputs = 4096;
 
-// The least of the forms' times, each a line through measured ones, in us (bf16, no activation; k = K / 1024):
-//   rounds of 256 blocks: split 32 x 32  2 + r (1.9 + 1.2 k), 32 x 64  2 + r (2.2 + 1.45 k), 64 x 64  2 + r (4 + 2 k)
-//   tiles (blocks of one round share their CU's memory path): 128 x 128  3.5 + 6.9 k up to 128 blocks, 4 + 9.2 k up to 256, and
-//   128 x 256  4 + 10.3 k, 11.8 k and 15 k up to 64, 128 and 256 blocks; then rounds of 512 blocks of 3 + 16.5 k and 5 + 25.5 k
-// Measured, M x N x K: 32 x 32 / 32 x 64 / 64 x 64 / 128 x 128 / 128 x 256
-//     64 x 4096 x 4096    7.6 / 8.7 / 11.8 / 29.9 / 42.0      1024 x 4096 x 1024  46.7 / 32.0 / 26.2 / 13.4 / 18.0
-//     512 x 2048 x 2048  18.1 / 12.7 / 10.8 / 18.4 / 25.3     1024 x 8192 x 4096   186 / 124 / 102 / 67.0 / 60.6
-//     256 x 4096 x 4096  27.3 / 18.1 / 13.8 / 31.2 / 43.7     4096 x 4096 x 4096   363 / 239 / 199 / 124 / 108
+// The smallest blocks that all run at once, one per CU, then the tiles: 128 x 128 while the chip holds half of them, else 128 x
+// 256.  Long products go on two rounds of split 64 x 64.  us, M x N x K: 32 x 32 / 32 x 64 / 64 x 64 / 128 x 128 / 128 x 256
+//     64 x 4096 x 4096    7.5 / 8.7 / 11.8 / 30 / 42        500 x 500 x 500     7.7 / 7.5 / 9.0 / 10 / 14
+//     128 x 4096 x 4096   12.5 / 10.1 / 13.0 / 29 / 41      640 x 640 x 640     8.1 / 7.0 / 8.9 / 9.5 / 12
+//     200 x 3000 x 1000   9.2 / 9.6 / 8.3 / 11.9 / 16       1024 x 1024 x 8192  33 / 26 / 22.5 / 54 / 74
+//     512 x 4096 x 4096   35 / 32 / 26.7 / 30.8 / 40        256 x 8192 x 8192   60 / 51 / 42 / 57 / 77
+//     768 x 4096 x 2048   34 / 33 / 27.6 / 19.4 / 25        2304 x 528 x 128    9.1 / 10.6 / 10.4 / 7.1 / 9.4
+//     2048 x 2048 x 8192  122 / 99 / 82 / 63 / 82           1536 x 4096 x 4096  93 / 88 / 72 / 51 / 46
+//     304 x 12032 x 2048  40 / 43 / 35 / 27.5 / 25.7        918 x 9600 x 11008  851 / 444 / 392 / 214 / 221
 // kFew, blocks of 16 outputs up to kFewOutputs of them (a block per CU), of 32 beyond, where x is loaded half as often (us):
 //     tokens                          1      4      8     16     (32 x 32 split)
 //     4096 x 4096, blocks of 16      3.5    4.2           6.0     6.8
@@ -261,21 +262,49 @@ inline LinearForm linear_form(int64_t M, int64_t N, int64_t K, bool keeps_z)
 {
     if (M <= (N > kFewOutputs ? kFewTokens / 2 : kFewTokens) && !keeps_z) return LinearForm::kFew;
     auto blocks = [&](int64_t m, int64_t n) { return ((M + m - 1) / m) * ((N + n - 1) / n); };
-    const double k = (double)K / 1024;
-    auto split = [&](int64_t n, double base, double slope) { return 2 + (double)((n + 255) / 256) * (base + slope * k); };
-    auto tile = [&](int64_t n, double two_base, double two, double b0, double s0, double b1, double s1, double b2, double s2) {
-        if (n <= 64) return b0 + s0 * k;
-        if (n <= 128) return b1 + s1 * k;
-        if (n <= 256) return b2 + s2 * k;
-        return (double)((n + 511) / 512) * (two_base + two * k);
+    if (blocks(32, 32) <= 256) return LinearForm::kSplit32;
+    if (blocks(32, 64) <= 256) return LinearForm::kSplit32x64;
+    if (blocks(64, 64) <= (K >= 2560 ? 512 : 256)) return LinearForm::kSplit64;
+    return blocks(128, 128) <= 256 ? LinearForm::kTile128 : LinearForm::kTile256;
+}
+
+// The weight gradient's product over M tokens (linear_backward.hip): tiles of 256, 128 or 64 squared of dw, one, two and four a
+// CU; the tokens split into runs whose sums another launch adds up, where the tiles alone leave CUs idle over many tokens.
+//
+// The least estimated time, us: a round of blocks takes a start and an end and, per step of 64 tokens, what a step was measured to
+// take with so many blocks at work (a small tile's blocks wait for their loads, so more of them on a CU cost little); adding up
+// takes a launch and 8 bytes per weight and split at 4.5 TB/s.  Measured with the pass before it, M x N x K, tile / splits:
+//     16384 x 1024 x 1024  128 / 4 67, 64 / 1 124, 256 / 8 81      2048 x 2048 x 2048   128 / 1 33, 64 / 1 39, 256 / 1 51
+//     10546 x 724 x 320    64 / 8 32, 64 / 1 80, 128 / 8 34        1024 x 4096 x 4096   256 / 1 46, 128 / 1 49, 64 / 1 61
+//     11497 x 13983 x 256  256 / 3 243, 128 / 1 278, 64 / 1 300    9000 x 3000 x 3000   256 / 1 196, 128 / 1 222, 256 / 3 223
+//     16384 x 4096 x 1024  256 / 4 186, 128 / 1 193, 64 / 1 248    256 x 1024 x 1024    64 / 1 9.6, 128 / 1 11, 256 / 1 17
+struct WgradForm {
+    int tile, splits;
+};
+inline WgradForm wgrad_form(int64_t M, int64_t N, int64_t K)
+{
+    struct Rate {
+        int tile, per_cu;
+        double ends, step[4];  // step: up to 1, 2, 3 and 4 blocks on a CU
     };
-    const double t[5] = {split(blocks(32, 32), 1.9, 1.2), split(blocks(32, 64), 2.2, 1.45), split(blocks(64, 64), 4, 2),
-                         tile(blocks(128, 128), 3, 16.5, 3.5, 6.9, 3.5, 6.9, 4, 9.2),
-                         tile(blocks(128, 256), 5, 25.5, 4, 10.3, 4, 11.8, 4, 15)};
-    int best = 4;
-    for (int i = 3; i >= 0; --i)
-        if (t[i] < t[best]) best = i;
-    return (LinearForm)((int)LinearForm::kSplit32 + best);
+    constexpr Rate rates[] = {{256, 1, 12, {1.3, 0, 0, 0}}, {128, 2, 5, {0.55, 0.85, 0, 0}}, {64, 4, 4, {0.36, 0.40, 0.60, 0.60}}};
+    constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16};
+    const double steps = (double)((M + 63) / 64);
+    WgradForm best = {64, 1};
+    double least = 1e300;
+    for (const Rate& r : rates)
+        for (const int splits : kSplits) {
+            const int64_t per = (int64_t)((steps + splits - 1) / splits);
+            if (splits > 1 && per < 4) break;
+            const double blocks = (double)((N + r.tile - 1) / r.tile) * (double)((K + r.tile - 1) / r.tile) * splits;
+            const double rounds = (double)(int64_t)(blocks / (256 * r.per_cu)), left = blocks - rounds * 256 * r.per_cu;
+            double t = rounds * ((double)per * r.step[r.per_cu - 1] + r.ends);
+            // (a chip that is a quarter idle runs the large tile at a higher clock)
+            if (left > 0) t += (double)per * (r.tile == 256 && rounds == 0 && left <= 192 ? 1.05 : r.step[(int)(left - 1) / 256]) + r.ends;
+            if (splits > 1) t += 3 + splits * (double)N * (double)K * 8 / 4.5e6;
+            if (t < least) least = t, best = {r.tile, splits};
+        }
+    return best;
 }
 
 }  // namespace rtn

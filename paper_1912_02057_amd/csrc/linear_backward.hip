@@ -36,7 +36,8 @@ __device__ __forceinline__ void bias_sum(const BiasSum& b, int block, float* sum
 
 struct WgParams {
     const char *x, *d;  // x^ and dz in operand order
-    int N, K, nk;       // nk: steps of 64 tokens
+    int N, K, steps;    // steps of 64 tokens,
+    int per, splits;    // of which a block takes `per`; split s > 0 writes N K floats behind split 0's
     int64_t xpitch, dpitch;  // bytes from one block of tokens to the next
     int tilesN, ntiles, band_tiles;
     FastDiv div_band, div_lastband;
@@ -71,22 +72,25 @@ __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgP
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wn = wave >> 1, wk = wave & 1, l32 = lane & 31, h = lane >> 5;
-    int tn, tk;
+    int tn, tk, split;
     {
         // each XCD has a run of the tiles, then of the sums
-        const int chunk = (p.ntiles + 7) >> 3, at = (int)(blockIdx.x >> 3), bid = (int)(blockIdx.x & 7) * chunk + at;
+        const int blocks = p.ntiles * p.splits, chunk = (blocks + 7) >> 3, at = (int)(blockIdx.x >> 3);
+        int bid = (int)(blockIdx.x & 7) * chunk + at;
         if (at >= chunk) {
             bias_sum<T>(p.bias, (at - chunk) * 8 + (int)(blockIdx.x & 7), (float*)smem);
             return;
         }
-        if (bid >= p.ntiles) return;
+        if (bid >= blocks) return;
+        split = bid / p.ntiles;
+        bid -= split * p.ntiles;
         band_tile(bid, p.tilesN, p.band_tiles, [&](int n) { return (int)fastdiv((uint32_t)n, p.div_band); },
                   [&](int n) { return (int)fastdiv((uint32_t)n, p.div_lastband); }, tn, tk);
     }
-    const int n0 = tn * BN, k0 = tk * BK, nk = p.nk, nh = 2 * nk;
+    const int n0 = tn * BN, k0 = tk * BK, step0 = split * p.per, nk = p.steps - step0 < p.per ? p.steps - step0 : p.per, nh = 2 * nk;
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-    const int8_t* xg = (const int8_t*)p.x + (int64_t)(k0 / 32) * 2048 + wave * L::XDMA * 1024;
-    const int8_t* dg = (const int8_t*)p.d + (int64_t)(n0 / 32) * 2048 + wave * L::DDMA * 1024;
+    const int8_t* xg = (const int8_t*)p.x + (int64_t)(k0 / 32) * 2048 + wave * L::XDMA * 1024 + 2 * step0 * p.xpitch;
+    const int8_t* dg = (const int8_t*)p.d + (int64_t)(n0 / 32) * 2048 + wave * L::DDMA * 1024 + 2 * step0 * p.dpitch;
     const unsigned voff = (unsigned)lane * 16u;
     // load i of token block q into its slot at LDS address `base`
     auto load_one = [&](auto index, int q, unsigned base) {
@@ -213,7 +217,7 @@ __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgP
             if (n >= p.N) continue;
             const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
             if constexpr (F32) {
-                float* o = (float*)p.dw + (int64_t)n * p.K + k8;
+                float* o = (float*)p.dw + ((int64_t)split * p.N + n) * p.K + k8;
                 if (k8 + 8 <= p.K) {
                     __builtin_memcpy(o, v, 32);
                 } else {
@@ -243,7 +247,7 @@ hipError_t run_tile(WgParams& p, hipStream_t st)
     p.tilesN = (p.N + BN - 1) / BN;
     const int tilesK = (p.K + BK - 1) / BK;
     const int64_t nt = (int64_t)p.tilesN * tilesK;
-    const int64_t blocks = (nt + 7) / 8 * 8 + bias_blocks(p.bias);
+    const int64_t blocks = (nt * p.splits + 7) / 8 * 8 + bias_blocks(p.bias);
     if (blocks > 0x7fffff00) return hipErrorInvalidValue;
     p.ntiles = (int)nt;
     p.band_tiles = 8 * tilesK;
@@ -257,12 +261,38 @@ hipError_t run_tile(WgParams& p, hipStream_t st)
 }
 
 template <class T, bool F32>
-hipError_t run(WgParams& p, hipStream_t st)
+hipError_t run(WgParams& p, int tile, hipStream_t st)
 {
-    const int64_t t256 = (int64_t)((p.N + 255) / 256) * ((p.K + 255) / 256), t128 = (int64_t)((p.N + 127) / 128) * ((p.K + 127) / 128);
-    if (t256 >= 192) return run_tile<T, 256, 256, F32>(p, st);
-    if (t128 >= 192) return run_tile<T, 128, 128, F32>(p, st);
+    if (tile == 256) return run_tile<T, 256, 256, F32>(p, st);
+    if (tile == 128) return run_tile<T, 128, 128, F32>(p, st);
     return run_tile<T, 64, 64, F32>(p, st);
+}
+
+// dw = the sum of the splits, in their order
+template <class T, bool F32>
+__global__ __launch_bounds__(256) void k_wgrad_sum(const float* part, int splits, int64_t n, void* out)
+{
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * 1024) {
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        const int m = n - i < 4 ? (int)(n - i) : 4;
+        for (int s = 0; s < splits; ++s) {
+            const float* q = part + s * n + i;
+            if (m == 4) {
+                float w[4];
+                __builtin_memcpy(w, q, 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += w[e];
+            } else {
+                for (int e = 0; e < m; ++e) v[e] += q[e];
+            }
+        }
+        for (int e = 0; e < m; ++e) {
+            if constexpr (F32)
+                ((float*)out)[i + e] = v[e];
+            else
+                ((unsigned short*)out)[i + e] = T::from_float(v[e]);
+        }
+    }
 }
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
@@ -275,7 +305,7 @@ int64_t blocks_per_run(int64_t M, int64_t N)
 }
 
 struct BwdWork {
-    int64_t dza, dzt, xt, part, total;
+    int64_t dza, dzt, xt, part, dwpart, total;
     BwdWork(int64_t M, int64_t N, int64_t K)
     {
         dza = 0;
@@ -283,7 +313,9 @@ struct BwdWork {
         xt = dzt + operand_bytes(M, N);
         part = xt + operand_bytes(M, K);
         const int64_t tb = operand_blocks(M), per = blocks_per_run(M, N);
-        total = part + round_up((tb + per - 1) / per * N * 4, 256);
+        dwpart = part + round_up((tb + per - 1) / per * N * 4, 256);
+        const WgradForm f = wgrad_form(M, N, K);
+        total = dwpart + (f.splits > 1 ? round_up(f.splits * N * K * 4, 256) : 0);
     }
 };
 
@@ -300,14 +332,29 @@ hipError_t launch_bias_sum(const BiasSum& b, int f16, hipStream_t st)
 
 hipError_t launch_linear_wgrad(const WgradArgs& a, hipStream_t st)
 {
+    const WgradForm f = wgrad_form(a.M, a.N, a.K);
     WgParams p = {};
     p.x = a.xt, p.d = a.dzt;
-    p.N = (int)a.N, p.K = (int)a.K, p.nk = (int)((a.M + 63) / 64);
+    p.N = (int)a.N, p.K = (int)a.K, p.steps = (int)((a.M + 63) / 64);
+    p.splits = f.splits, p.per = (p.steps + f.splits - 1) / f.splits;
     p.xpitch = (a.K + 31) / 32 * 2048, p.dpitch = (a.N + 31) / 32 * 2048;
-    p.dw = a.dw;
+    p.dw = f.splits > 1 ? a.part : a.dw;
     p.bias = a.bias;
-    if (a.f16) return a.dw_f32 ? run<F16, true>(p, st) : run<F16, false>(p, st);
-    return a.dw_f32 ? run<BF16, true>(p, st) : run<BF16, false>(p, st);
+    hipError_t e;
+    if (a.dw_f32 || f.splits > 1)
+        e = a.f16 ? run<F16, true>(p, f.tile, st) : run<BF16, true>(p, f.tile, st);
+    else
+        e = a.f16 ? run<F16, false>(p, f.tile, st) : run<BF16, false>(p, f.tile, st);
+    if (e != hipSuccess || f.splits == 1) return e;
+    const int64_t n = a.N * a.K, blocks = (n + 1023) / 1024;
+    const unsigned grid = (unsigned)(blocks < 4096 ? blocks : 4096);
+    if (a.dw_f32)
+        k_wgrad_sum<BF16, true><<<grid, 256, 0, st>>>(a.part, f.splits, n, a.dw);
+    else if (a.f16)
+        k_wgrad_sum<F16, false><<<grid, 256, 0, st>>>(a.part, f.splits, n, a.dw);
+    else
+        k_wgrad_sum<BF16, false><<<grid, 256, 0, st>>>(a.part, f.splits, n, a.dw);
+    return hipGetLastError();
 }
 
 size_t linear_backward_workspace(int64_t M, int64_t N, int64_t K) { return (size_t)BwdWork(M, N, K).total; }
@@ -342,7 +389,7 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t st)
     }
     BiasSum bias = {};
     if (a.dbias) bias = {g.part, (operand_blocks(a.M) + g.per - 1) / g.per, a.N, a.dbias};
-    if (a.dw) return launch_linear_wgrad(WgradArgs{g.dzt, g.xt, a.M, a.N, a.K, a.dw, a.f16, a.dw_f32, bias}, st);
+    if (a.dw) return launch_linear_wgrad(WgradArgs{g.dzt, g.xt, a.M, a.N, a.K, a.dw, a.f16, a.dw_f32, (float*)(a.workspace + w.dwpart), bias}, st);
     return a.dbias ? launch_bias_sum(bias, a.f16, st) : hipSuccess;
 }
 

@@ -291,6 +291,7 @@ struct WgradArgs {
     int64_t M, N, K;
     void* dw;  // [N][K]
     int f16, dw_f32;
+    float* part;   // wgrad_form's splits x [N][K], where there are several
     BiasSum bias;  // in the same launch
 };
 hipError_t launch_linear_wgrad(const WgradArgs& a, hipStream_t st);

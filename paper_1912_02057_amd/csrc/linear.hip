@@ -51,27 +51,32 @@ __device__ __forceinline__ void load_affine(const LinParams& p, int n, float (&a
     }
 }
 
-// act(z) + residual of outputs n .. n + 7 of row m -> y.  WHOLE: the row exists and so do all eight.
-template <class T, int ACT, bool WHOLE>
-__device__ __forceinline__ void finish_row(const LinParams& p, int m, int n, const float (&z)[8])
+// Eight outputs, of which the first `left` exist, rounded
+template <class T>
+__device__ __forceinline__ void store_row8(unsigned short* y, int left, const float (&v)[8])
 {
-    if (!WHOLE && (m >= p.M || n >= p.N)) return;
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = act_value<ACT>(z[i]);
-    if (p.res) {
-        const u32x4 q = WHOLE ? load16(p.res + m * p.ldr + n) : load_row8(p.res + m * p.ldr, n, p.N);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += half_of<T>(q[i >> 1], i & 1);
-    }
-    unsigned short* y = p.y + m * p.ldy + n;
-    if (WHOLE || n + 8 <= p.N) {
+    if (left >= 8) {
         store16(y, u32x4{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])});
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (n + i < p.N) y[i] = T::from_float(v[i]);
+            if (i < left) y[i] = T::from_float(v[i]);
     }
+}
+// act(z) + residual of outputs n .. n + 7 of row m -> y
+template <class T, int ACT>
+__device__ __forceinline__ void finish_row(const LinParams& p, int m, int n, const float (&z)[8])
+{
+    if (m >= p.M || n >= p.N) return;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = act_value<ACT>(z[i]);
+    if (p.res) {
+        const u32x4 q = load_row8(p.res + m * p.ldr, n, p.N);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += half_of<T>(q[i >> 1], i & 1);
+    }
+    store_row8<T>(p.y + m * p.ldy + n, p.N - n, v);
 }
 
 template <class F>
@@ -90,12 +95,14 @@ __device__ __forceinline__ void with_act(int act, F&& f)
 // Scales of 8 channels from the largest magnitudes (as bits) of their groups
 template <class T>
 struct CkptScale {
-    unsigned ex[2] = {0, 0};
+    unsigned ex[2];
     float inv[8];
     bool clamp;
+    CkptScale() = default;
     __device__ __forceinline__ CkptScale(const unsigned (&am)[8])
     {
         bool end = false;
+        ex[0] = ex[1] = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int e = ckpt_exponent<T>(__uint_as_float(am[i]));
@@ -310,11 +317,36 @@ __global__ __launch_bounds__(256, 2) void k_linear(LinParams p)
     __syncthreads();
     constexpr int CL = L::WN / 8, TPL = CL / 2;
     char* zs = smem + wave * L::ZBYTES;
-    const int n8 = n0 + wave * L::WN + (lane % CL) * 8, t0 = (lane / CL) * TPL;
-    float al[8], bi[8];
-    if (n8 < p.N) load_affine<T>(p, n8, al, bi);
+    const int nw = n0 + wave * L::WN, n8 = nw + (lane % CL) * 8, t0 = (lane / CL) * TPL;
+    if (nw >= p.N) return;
+    float al[L::TN], bi[L::TN];  // of the columns that this lane has in its accumulators
+#pragma unroll
+    for (int i = 0; i < L::TN; ++i) {
+        const int n = nw + i * 32 + l32;
+        al[i] = bi[i] = 0.f;
+        if (n < p.N) {
+            al[i] = 0.5f * (p.alpha.ptr ? p.alpha.ptr[n] : p.alpha.s);
+            if (p.bias) bi[i] = T::to_float(p.bias[n]);
+        }
+    }
+    // the residual of the rows of a round, fetched before they pass through LDS
+    u32x4 res[TPL];
+    auto fetch = [&](int k) {
+        const int mt = m0 + k * 32 + t0;
+        const unsigned short* r = p.res + mt * p.ldr;
+        if (mt + TPL <= p.M && nw + L::WN <= p.N) {
+#pragma unroll
+            for (int t = 0; t < TPL; ++t) res[t] = load16(r + t * p.ldr + n8);
+        } else {
+#pragma unroll
+            for (int t = 0; t < TPL; ++t) res[t] = mt + t < p.M ? load_row8(r + t * p.ldr, n8, p.N) : u32x4{0, 0, 0, 0};
+        }
+    };
 #pragma unroll 1
     for (int k = 0; k < L::TM; ++k) {
+        const int mt = m0 + k * 32;  // first token
+        if (mt >= p.M) break;
+        if (p.res) fetch(k);
         auto put = [&](auto index) {
             constexpr int kk = decltype(index)::value;
             if (kk != k) return;
@@ -322,36 +354,33 @@ __global__ __launch_bounds__(256, 2) void k_linear(LinParams p)
             for (int i = 0; i < L::TN; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)  // row 8 (r / 4) + 4 h + r % 4, column l32
-                    *(float*)(zs + (8 * (r >> 2) + 4 * h + (r & 3)) * L::ZPITCH + (i * 32 + l32) * 4) = acc[i][kk][r];
+                    *(float*)(zs + (8 * (r >> 2) + 4 * h + (r & 3)) * L::ZPITCH + (i * 32 + l32) * 4) = fmaf(acc[i][kk][r], al[i], bi[i]);
         };
         for_each_index(put, std::make_integer_sequence<int, L::TM>{});
-        const int mt = m0 + k * 32;  // first token
-        if (mt >= p.M || n0 + wave * L::WN >= p.N) continue;
-        const bool whole = mt + 32 <= p.M && n0 + (wave + 1) * L::WN <= p.N;
+        const bool whole = mt + 32 <= p.M && nw + L::WN <= p.N;
         wait_lgkm0();
-        auto row_z = [&](int t, float(&z)[8]) {
+        auto read_z = [&](int t, float(&z)[8]) {
             const float* row = (const float*)(zs + (t0 + t) * L::ZPITCH + (lane % CL) * 32);
             const float4 a = *(const float4*)row, b = *(const float4*)(row + 4);
-            const float s[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            z[0] = a.x, z[1] = a.y, z[2] = a.z, z[3] = a.w, z[4] = b.x, z[5] = b.y, z[6] = b.z, z[7] = b.w;
+            if (!whole) {  // (a checkpoint's tokens past the end are zeros)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = fmaf(s[i], al[i], bi[i]);
+                for (int i = 0; i < 8; ++i) z[i] = mt + t0 + t < p.M ? z[i] : 0.f;
+            }
         };
-        // R rows at a time: more of them would not fit beside the accumulators of a tile that shares its CU
-        constexpr int R = TPL < 4 ? TPL : 4;
+        CkptScale<T> scale;
         if (p.zq) {
             unsigned am[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll 1
-            for (int r = 0; r < TPL; r += R)
 #pragma unroll
-                for (int t = 0; t < R; ++t) {
-                    float z[8];
-                    row_z(r + t, z);
+            for (int t = 0; t < TPL; ++t) {
+                float z[8];
+                read_z(t, z);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const unsigned u = mt + t0 + r + t < p.M ? __float_as_uint(z[i]) & 0x7fffffffu : 0u;
-                        am[i] = u > am[i] ? u : am[i];
-                    }
+                for (int i = 0; i < 8; ++i) {
+                    const unsigned u = __float_as_uint(z[i]) & 0x7fffffffu;
+                    am[i] = u > am[i] ? u : am[i];
                 }
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -359,43 +388,34 @@ __global__ __launch_bounds__(256, 2) void k_linear(LinParams p)
                     const unsigned o = (unsigned)__shfl_xor((int)am[i], d);
                     am[i] = o > am[i] ? o : am[i];
                 }
-            const CkptScale<T> scale(am);
-            if (n8 < p.N) {
-                if (t0 == 0) store_scales(p, mt, n8, scale);
-#pragma unroll 1
-                for (int r = 0; r < TPL; r += R) {
-                    float z[R][8];
-#pragma unroll
-                    for (int t = 0; t < R; ++t) {
-                        row_z(r + t, z[t]);
-                        if (mt + t0 + r + t >= p.M)
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) z[t][i] = 0.f;
-                    }
-                    store_codes<T, R>(p, mt, t0 + r, n8, z, scale);
-                }
-            }
+            scale = CkptScale<T>(am);
+            if (t0 == 0 && n8 < p.N) store_scales(p, mt, n8, scale);
         }
-        if (whole)
-            with_act(p.act, [&](auto which) {
-#pragma unroll 1
-                for (int r = 0; r < TPL; r += R)
+        unsigned short* y = p.y + (mt + t0) * p.ldy + n8;
+        with_act(p.act, [&](auto which) {
+            constexpr int ACT = decltype(which)::value;
 #pragma unroll
-                    for (int t = 0; t < R; ++t) {
-                        float z[8];
-                        row_z(r + t, z);
-                        finish_row<T, decltype(which)::value, true>(p, mt + t0 + r + t, n8, z);
+            for (int r = 0; r < TPL; r += 2) {  // two rows at a time: more do not fit beside the accumulators
+                float z[2][8];
+                read_z(r, z[0]);
+                read_z(r + 1, z[1]);
+                if (p.zq && n8 < p.N) store_codes<T, 2>(p, mt, t0 + r, n8, z, scale);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) z[t][i] = act_value<ACT>(z[t][i]);
+                    if (p.res) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) z[t][i] += half_of<T>(res[r + t][i >> 1], i & 1);
                     }
-            });
-        else
-            with_act(p.act, [&](auto which) {
-#pragma unroll 1
-                for (int t = 0; t < TPL; ++t) {
-                    float z[8];
-                    row_z(t, z);
-                    finish_row<T, decltype(which)::value, false>(p, mt + t0 + t, n8, z);
+                    if (whole)
+                        store16(y + (r + t) * p.ldy, u32x4{pack2<T>(z[t][0], z[t][1]), pack2<T>(z[t][2], z[t][3]), pack2<T>(z[t][4], z[t][5]), pack2<T>(z[t][6], z[t][7])});
+                    else if (mt + t0 + r + t < p.M)
+                        store_row8<T>(y + (r + t) * p.ldy, p.N - n8, z[t]);
                 }
-            });
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        });
         // (the next round's writes to `zs` are this wave's own and come after its reads)
     }
 }
@@ -668,7 +688,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_linear_split(LinParams p)
         const bool in = m0 + t < p.M;
 #pragma unroll
         for (int i = 0; i < 8; ++i) z[o][i] = in ? fmaf(s[i], al[i], bi[i]) : 0.f;
-        with_act(p.act, [&](auto which) { finish_row<T, decltype(which)::value, false>(p, m0 + t, n, z[o]); });
+        with_act(p.act, [&](auto which) { finish_row<T, decltype(which)::value>(p, m0 + t, n, z[o]); });
         if (p.zq)
 #pragma unroll
             for (int i = 0; i < 8; ++i) atomicMax(&amax[(t >> 5) * (32 * RB) + g * 8 + i], __float_as_uint(z[o][i]) & 0x7fffffffu);

@@ -117,8 +117,8 @@ __device__ __forceinline__ float normal_tail(float z, float& e)
 {
     const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.3275911f * 0.70710678f, 1.f));
     e = exp_scaled(z * z, -0.72134752f);  // log2(e) / 2
-    const float p = fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f) * 0.5f;
-    return p * t * e;
+    constexpr float a1 = 0.5f * 0.254829592f, a2 = 0.5f * -0.284496736f, a3 = 0.5f * 1.421413741f, a4 = 0.5f * -1.453152027f, a5 = 0.5f * 1.061405429f;
+    return fmaf(fmaf(fmaf(fmaf(a5, t, a4), t, a3), t, a2), t, a1) * t * e;
 }
 // 16 bytes wherever they start (global accesses need no alignment on this target)
 __device__ __forceinline__ u32x4 load16(const void* p)

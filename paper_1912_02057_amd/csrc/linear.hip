@@ -806,7 +806,9 @@ hipError_t run(const LinearArgs& a, LinParams p, hipStream_t st)
 bool linear_copies_x(const LinearArgs& a)
 {
     const LinearForm form = linear_form(a.M, a.N, a.K, a.zq != nullptr);
-    return (form == LinearForm::kTile128 || form == LinearForm::kTile256) && !direct_rows(a.x, a.ldx, a.K);
+    if (form == LinearForm::kFew || direct_rows(a.x, a.ldx, a.K)) return false;
+    // (the split forms take any rows, but many steps of them longer than a copy: us: 216 x 6016 x 7223 62, with the copy 41; 1000 x 1003 x 2187 13.7, 15.5)
+    return form == LinearForm::kTile128 || form == LinearForm::kTile256 || a.K > 4096;
 }
 
 hipError_t launch_linear(const LinearArgs& a, hipStream_t st)

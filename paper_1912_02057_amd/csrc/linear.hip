@@ -1,8 +1,12 @@
 // Ternary linear layer of 16-bit activations: y = act(alpha (x t^T) + bias) + residual, on the bf16 / fp16 matrix cores.
 //
 // The weights are two bits each in the order the matrix instruction takes them (WeightShape); a register of two weights is
-// a shift and an AND away from its word (-2, 0, +2; the halves are made up for in alpha), so 32 operand registers of a
-// 64-step cost 64 vector operations beside 64 matrix instructions of 32 cycles.
+// a shift and an AND away from its word (-2, 0, +2; the halves are made up for in alpha).  Products with them are exact; sums
+// are the instruction's fp32 accumulators, along the columns in one order per form, and y is rounded once.
+//
+// Three kernels, chosen by the sizes (linear_form): k_linear_few for a token or a few, bound by the weights' bytes and their
+// widening; k_linear_split for grids that do not fill the chip, bound by the latency of its loads and by the bytes of x that
+// pass through a CU; k_linear, tiles of a full grid, bound by the power limit of the matrix cores.
 #include "linear_math.h"
 #include "tmm_kernel.h"
 
@@ -162,7 +166,11 @@ struct LinTile {
 // 2 instead the redundant vector operations cost 3 to 4 %: 16384 x 8192 x 8192 1540 us against 1490.  Two blocks share a CU, so one's
 // epilogue passes beside the other's products (one block of 256 x 256: 1660 us).  Ring of NS stages of 64 columns: x rows of 128 bytes, 16-byte
 // chunk c of row r at place c ^ (r >> 1 & 7), so that 16 rows' fragments hit all banks; then the weights' words.  One barrier per
-// step, before the last of its four 16-column slices, and fragments are read one slice ahead.
+// step, before the last of its four 16-column slices, and fragments are read one slice ahead.  x is the instruction's first
+// operand: it takes 5 % less time at the power limit with the ternary values as the second.  Per step of 64 columns a wave has 32 matrix
+// instructions (128 x 256), 64 vector operations that widen weights, 16 + 2 fragment reads and 5 direct loads, spread between
+// them.  16384 x 8192 x 8192: 1404 us, 1566 TFLOP/s (a large library product of these values 1665, at its own clock); 4096^3 with gelu 98 us, of
+// which the launch, the first loads and the epilogue (33.5 MB of y, the activation on the vector ALU) are 13.
 template <class T, int BM, int BN, int NS>
 __global__ __launch_bounds__(256, 2) void k_linear(LinParams p)
 {

@@ -469,8 +469,8 @@ int rtn_linear(rtn_dtype dt, const void *x, int64_t ldx, const void *prepared, i
  * kept as q = rint(v / 2^e) (ties to even), |q| <= 127:
  *   e = floor(log2(max |v|)) - 6, one more where max |v| / 2^e would round to 128; at least -126 (RTN_BF16) or -24 (RTN_F16)
  *   and at most 121 or 9 (64 times the next power would be infinite in dt; |v| / 2^e beyond 127 there is kept as 127)
- * so the error is at most 2^e / 2 (2^e there), 1/128 of the group's largest magnitude, and what is read back, q 2^e, is exact in dt.  A
- * group that holds an infinity or NaN reads back as NaN.  rtn_checkpoint_bytes(M, C) = 264 bytes per 32 tokens and 8 channels,
+ * so the error is at most 2^e / 2 (2^e there), below 1/127 of the group's largest magnitude unless e is at its least, and what
+ * is read back, q 2^e, is exact in dt.  A group that holds an infinity or NaN reads back as NaN.  rtn_checkpoint_bytes(M, C) = 264 bytes per 32 tokens and 8 channels,
  * 16-byte aligned; the layout belongs to the build of the library.  M = 0: nothing to do. */
 size_t rtn_checkpoint_bytes(int64_t M, int64_t C);
 int rtn_checkpoint_pack(rtn_dtype dt, const void *x, int64_t ldx, int64_t M, int64_t C, void *ckpt, size_t ckpt_bytes,

@@ -162,15 +162,15 @@ struct LinTile {
 };
 
 // A block of 4 waves owns BM tokens x BN outputs, a wave all the tokens of a quarter of the outputs, so that no weight is widened
-// twice: large products are bound by the power limit (clock 1.7 GHz while the matrix cores are busy 84 % of it), and with the waves 2 x
-// 2 instead the redundant vector operations cost 3 to 4 %: 16384 x 8192 x 8192 1540 us against 1490.  Two blocks share a CU, so one's
+// twice: large products are bound by the power limit (clock 1.5 to 1.7 GHz while the matrix cores are busy 88 % of it), and with the
+// waves 2 x 2 instead the redundant vector operations cost 3 %: 16384 x 8192 x 8192 1540 us against 1490.  Two blocks share a CU, so one's
 // epilogue passes beside the other's products (one block of 256 x 256: 1660 us).  Ring of NS stages of 64 columns: x rows of 128 bytes, 16-byte
 // chunk c of row r at place c ^ (r >> 1 & 7), so that 16 rows' fragments hit all banks; then the weights' words.  One barrier per
 // step, before the last of its four 16-column slices, and fragments are read one slice ahead.  x is the instruction's first
-// operand: it takes 5 % less time at the power limit with the ternary values as the second.  Per step of 64 columns a wave has 32 matrix
+// operand: it takes 4 % less time at the power limit with the ternary values as the second (1490 -> 1430 us).  Per step of 64 columns a wave has 32 matrix
 // instructions (128 x 256), 64 vector operations that widen weights, 16 + 2 fragment reads and 5 direct loads, spread between
-// them.  16384 x 8192 x 8192: 1404 us, 1566 TFLOP/s (a large library product of these values 1665, at its own clock); 4096^3 with gelu 98 us, of
-// which the launch, the first loads and the epilogue (33.5 MB of y, the activation on the vector ALU) are 13.
+// them.  16384 x 8192 x 8192: 1397 us, 1574 TFLOP/s (a large library product of such values reaches 1665); 4096^3 with gelu
+// 98 us, of which the launch, the first loads and the epilogue (33.5 MB of y, the activation on the vector ALU) are 13.
 template <class T, int BM, int BN, int NS>
 __global__ __launch_bounds__(256, 2) void k_linear(LinParams p)
 {
@@ -815,7 +815,8 @@ bool linear_copies_x(const LinearArgs& a)
 {
     const LinearForm form = linear_form(a.M, a.N, a.K, a.zq != nullptr);
     if (form == LinearForm::kFew || direct_rows(a.x, a.ldx, a.K)) return false;
-    // (the split forms take any rows, but many steps of them longer than a copy: us: 216 x 6016 x 7223 62, with the copy 41; 1000 x 1003 x 2187 13.7, 15.5)
+    // The split forms take any rows, but over many steps that costs more than a copy.  us, without and with one: 216 x 6016 x 7223
+    // 62 and 41, 1000 x 1003 x 2187 13.7 and 15.5.
     return form == LinearForm::kTile128 || form == LinearForm::kTile256 || a.K > 4096;
 }
 

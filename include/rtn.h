@@ -483,8 +483,9 @@ int rtn_checkpoint_unpack(rtn_dtype dt, const void *ckpt, size_t ckpt_bytes, int
  *   dx[m][k] = sum_n dz[m][n] alpha_w[n] t_w[n][k]     dw[n][k] = sum_m dz[m][n] x^[m][k]     dbias[n] = sum_m dz[m][n]
  * dw is the gradient of the reparameterized weights alpha_w * t_w: as RTN_F32 it is what rtn_weight_backward takes.  The
  * gradient of the residual is dy.  dx (rows lddx apart) and dbias have type dt, dw type dw_type (dt or RTN_F32) in dense rows;
- * each may be NULL, not all.  dz and dz * alpha_w are rounded to dt once, on their way into the products; the sums and dbias'
- * terms are fp32.  The sums' order follows from the sizes (no atomics): the same arguments give the same bits.
+ * each may be NULL, not all.  dz and (alpha_w a vector) dz * alpha_w are rounded to dt's precision once, on their way into the
+ * products; the sums and dbias' terms are fp32.  RTN_F16: as multiples of powers of two that follow from max |dy| and max |alpha_w|, so that small
+ * gradients keep 11 bits (down to 2^-28 of the largest) and large ones stay finite: no loss scale is needed for this pass.  The sums' order follows from the sizes (no atomics): the same arguments give the same bits.
  * x_ckpt is needed for dw, prepared_t for dx, z_ckpt unless act is RTN_ACT_NONE.  M = 0 writes zeros to dw and dbias.
  * dx may not overlap dy.  workspace: rtn_linear_backward_workspace_bytes(M, N, K), 16-byte aligned. */
 size_t rtn_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K);

@@ -157,17 +157,60 @@ __device__ __forceinline__ void store_operand(char* out, int64_t blocks, const M
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
-template <class T, int ACT>
+// The powers of two that dz (z) and dz alpha (za) are multiplied by on their way to float16.  dz and alpha may be of any size (a
+// gradient without a loss scale is 1e-5, alpha 1 / sqrt(K)), and float16 has its 11 bits from 2^-14 on only: the largest dy is brought
+// to 2^14 .. 2^15, which a slope (at most 1.13) leaves finite, and the largest alpha to 1/2 .. 1.  Then what is 2^-28 of the largest still has
+// all its bits.  The products are exact in these factors, and the sums are divided by them (unit: 2^-z, 2^-za) in fp32.
+struct GradUnits {
+    float z = 1.f, za = 1.f, unit = 1.f, unit_a = 1.f;
+    // What a lane takes of the parts: fetched here, looked at in `reduce`, behind the loads that do not depend on it
+    uint4 q[kRangeParts / 256];
+    unsigned al;
+    __device__ __forceinline__ void fetch(const unsigned* range, int parts)
+    {
+        const int lane = threadIdx.x & 63;
+        al = range[kRangeParts + lane];
+#pragma unroll
+        for (int i = 0; i < kRangeParts / 256; ++i)  // (past the last part: the first ones again)
+            q[i] = *(const uint4*)(range + (256 * i < parts ? 256 * i : 0) + 4 * lane);
+    }
+    __device__ __forceinline__ void reduce()
+    {
+        unsigned m[2] = {0, al};
+#pragma unroll
+        for (int i = 0; i < kRangeParts / 256; ++i) {
+            const unsigned a = q[i].x > q[i].y ? q[i].x : q[i].y, b = q[i].z > q[i].w ? q[i].z : q[i].w, c = a > b ? a : b;
+            m[0] = c > m[0] ? c : m[0];
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const unsigned o = (unsigned)__shfl_xor((int)m[k], d);
+                m[k] = o > m[k] ? o : m[k];
+            }
+        const unsigned top = __float_as_uint(F16::to_float((unsigned short)m[0]));
+        const int s = top && top < 0x7f800000u ? 14 - ((int)(top >> 23) - 127) : 0;  // -1 .. 38
+        int p = m[1] && m[1] < 0x7f800000u ? 126 - (int)(m[1] >> 23) : 0;            // (a subnormal alpha counts as 2^-127)
+        p = p > 126 - s ? 126 - s : p < -126 - s ? -126 - s : p;                     // both 2^(s + p) and its inverse are normal
+        z = power(s), za = power(s + p), unit = power(-s), unit_a = power(-s - p);
+    }
+    static __device__ __forceinline__ float power(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
+};
+
+template <class T, int ACT, bool UNITS>
 __device__ __forceinline__ void grad_unit(const GradArgs& a, int64_t tb0, int64_t strip, char* lds)
 {
     const int64_t nb = (a.N + 31) / 32, tbs = operand_blocks(a.M);
     const CkptShape cs(a.M, a.N);
     float sum[8], al[8];
+    GradUnits units;
+    if constexpr (UNITS) units.fetch(a.range, a.parts);
     const int64_t c = micro_of(0, strip).c;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         sum[i] = 0.f;
-        al[i] = c + i < a.N ? (a.alpha.ptr ? a.alpha.ptr[c + i] : a.alpha.s) : 0.f;
+        al[i] = c + i < a.N ? (a.alpha.ptr ? a.alpha.ptr[c + i] : 1.f) : 0.f;
     }
     for (int64_t mb = tb0; mb < tb0 + a.per && mb < tbs; ++mb) {
         const Micro u = micro_of(mb, strip);
@@ -180,6 +223,17 @@ __device__ __forceinline__ void grad_unit(const GradArgs& a, int64_t tb0, int64_
                 k.load(a.zq, cs, u);
             else
                 k.zero();
+        }
+        if (UNITS && mb == tb0) {
+            units.reduce();
+            const bool vector = a.alpha.ptr;
+            const float as = vector ? units.za : units.z;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) al[i] *= as;
+            if (blockIdx.x == 0 && threadIdx.x == 0) {
+                float* unit = (float*)(a.range + kRangeParts + 64);
+                unit[0] = units.unit, unit[1] = vector ? units.unit_a : units.unit;
+            }
         }
         unsigned o[8][kTok / 2];
 #pragma unroll
@@ -197,7 +251,7 @@ __device__ __forceinline__ void grad_unit(const GradArgs& a, int64_t tb0, int64_
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const unsigned b = ACT == kActNone ? v[t][i >> 1] >> (16 * (i & 1)) & 0xffffu : (unsigned)T::from_float(d[i]);
+                const unsigned b = ACT == kActNone ? v[t][i >> 1] >> (16 * (i & 1)) & 0xffffu : (unsigned)T::from_float(d[i] * units.z);
                 o[i][t >> 1] = t & 1 ? o[i][t >> 1] | b << 16 : b;
             }
             const int64_t m = mb * 32 + u.t0 + t;
@@ -227,28 +281,10 @@ __device__ __forceinline__ void grad_unit(const GradArgs& a, int64_t tb0, int64_
             if (c + i < a.N) a.part[row * a.N + c + i] = sum[i];
 }
 
-// The gradient before the activation, dz = dy act'(z^), as the two products take it: times alpha, row-major (dx), and in
-// operand order (dw); its sums over a run of tokens (dbias); and the layer's input from its checkpoint in operand order.
+// The layer's input from its checkpoint in operand order, 32 tokens x 64 channels of it
 template <class T>
-__global__ __launch_bounds__(256) void k_linear_grad(GradArgs a)
+__device__ __forceinline__ void x_unit(const GradArgs& a, int64_t unit, char* lds)
 {
-    __shared__ __attribute__((aligned(16))) char smem[4 * 4096];
-    char* lds = smem + (threadIdx.x >> 6) * 4096;  // of this wave
-    int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (unit < a.dz_units) {
-        const int64_t run = unit / a.dz_strips, strip = unit - run * a.dz_strips, tb0 = run * a.per;
-        if (a.act == kActNone)
-            grad_unit<T, kActNone>(a, tb0, strip, lds);
-        else if (a.act == kActRelu)
-            grad_unit<T, kActRelu>(a, tb0, strip, lds);
-        else if (a.act == kActGelu)
-            grad_unit<T, kActGelu>(a, tb0, strip, lds);
-        else
-            grad_unit<T, kActSilu>(a, tb0, strip, lds);
-        return;
-    }
-    unit -= a.dz_units;
-    if (unit >= a.x_units) return;
     const int64_t mb = unit / a.x_strips;
     const Micro u = micro_of(mb, unit - mb * a.x_strips);
     const int64_t kb = (a.K + 31) / 32;
@@ -271,6 +307,83 @@ __global__ __launch_bounds__(256) void k_linear_grad(GradArgs a)
         o[i] = make_uint2(w[0], w[1]);
     }
     store_operand(a.xt, kb, u, o, lds);
+}
+
+// float16: the largest magnitudes of dy (a block each of `parts`, its waves over units of 32 tokens x 64 channels) and of alpha (the first
+// 64 blocks), every part written; and beside them, in the blocks behind, the input in operand order, which needs neither.  Without this
+// launch, dx of a gradient of 1e-5 is off by 11 % at K = N = 4096.  It makes the backward pass 15 -> 18.5 us at 256 x 1024 x 1024, 37 -> 42
+// at 1000 x 1003 x 2187, 265 -> 275 at 4096^3 and 3210 -> 3270 at 16384 x 8192 x 8192; bfloat16 needs none of it.
+__global__ __launch_bounds__(256) void k_grad_range(GradArgs a)
+{
+    __shared__ __attribute__((aligned(16))) char smem[4 * 4096];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if ((int)blockIdx.x >= a.parts) {
+        const int64_t unit = (int64_t)((int)blockIdx.x - a.parts) * 4 + wave;
+        if (unit < a.x_units) x_unit<F16>(a, unit, smem + wave * 4096);
+        return;
+    }
+    const int64_t units = (a.M + 31) / 32 * a.dz_strips;
+    unsigned top = 0, al = 0;  // as bits: a NaN is larger than an infinity, and that than any number
+    for (int64_t unit = (int64_t)wave * a.parts + blockIdx.x; unit < units; unit += 4 * a.parts) {
+        const int64_t mb = unit / a.dz_strips;
+        const Micro u = micro_of(mb, unit - mb * a.dz_strips);
+        u32x4 v[kTok];
+#pragma unroll
+        for (int t = 0; t < kTok; ++t) v[t] = load_row((const unsigned short*)a.dy, a.lddy, mb * 32 + u.t0 + t, a.M, u.c, a.N);
+#pragma unroll
+        for (int t = 0; t < kTok; ++t)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const unsigned b = (v[t][i >> 1] >> (16 * (i & 1))) & 0x7fffu;
+                top = b > top ? b : top;
+            }
+    }
+    if (blockIdx.x < 64 && a.alpha.ptr)
+        for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < a.N; n += 64 * 256) {
+            const unsigned b = __float_as_uint(a.alpha.ptr[n]) & 0x7fffffffu;
+            al = b > al ? b : al;
+        }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const unsigned o = (unsigned)__shfl_xor((int)top, d), p = (unsigned)__shfl_xor((int)al, d);
+        top = o > top ? o : top;
+        al = p > al ? p : al;
+    }
+    unsigned* tops = (unsigned*)smem;  // [2][4]
+    if (lane == 0) tops[wave] = top, tops[4 + wave] = al;
+    __syncthreads();
+    if (threadIdx.x >= 2 || (threadIdx.x == 1 && blockIdx.x >= 64)) return;
+    unsigned m = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m = tops[threadIdx.x * 4 + w] > m ? tops[threadIdx.x * 4 + w] : m;
+    a.range[threadIdx.x * kRangeParts + blockIdx.x] = m;
+}
+
+// The gradient before the activation, dz = dy act'(z^), as the two products take it: row-major, times an alpha per output (dx), and in
+// operand order (dw); its sums over a run of tokens (dbias), in fp32 throughout; and the layer's input from its checkpoint in operand order.
+// Both forms of dz are rounded to T here, for the matrix cores take 16-bit operands: one rounding of u a term beside the one of the
+// result.  (dz without an activation is dy and is not rounded, and one alpha for all outputs is left to the product's epilogue.)
+template <class T, bool UNITS>
+__global__ __launch_bounds__(256) void k_linear_grad(GradArgs a)
+{
+    __shared__ __attribute__((aligned(16))) char smem[4 * 4096];
+    char* lds = smem + (threadIdx.x >> 6) * 4096;  // of this wave
+    int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (unit < a.dz_units) {
+        const int64_t run = unit / a.dz_strips, strip = unit - run * a.dz_strips, tb0 = run * a.per;
+        if (a.act == kActNone)
+            grad_unit<T, kActNone, UNITS>(a, tb0, strip, lds);
+        else if (a.act == kActRelu)
+            grad_unit<T, kActRelu, UNITS>(a, tb0, strip, lds);
+        else if (a.act == kActGelu)
+            grad_unit<T, kActGelu, UNITS>(a, tb0, strip, lds);
+        else
+            grad_unit<T, kActSilu, UNITS>(a, tb0, strip, lds);
+        return;
+    }
+    unit -= a.dz_units;
+    if (unit >= a.x_units) return;
+    x_unit<T>(a, unit, lds);
 }
 
 }  // namespace
@@ -302,12 +415,22 @@ hipError_t launch_linear_grad(GradArgs a, int f16, hipStream_t st)
     a.dz_units = (tbs + a.per - 1) / a.per * a.dz_strips;
     a.x_strips = a.xt ? (a.K + kStrip - 1) / kStrip : 0;
     a.x_units = tbs * a.x_strips;
+    if (a.range) {
+        const int64_t want = (a.M + 31) / 32 * a.dz_strips / 4;  // a unit a wave, up to 4096 waves
+        a.parts = want >= kRangeParts ? kRangeParts : want <= 256 ? 256 : (int)((want + 255) / 256 * 256);
+        k_grad_range<<<(unsigned)(a.parts + (a.x_units + 3) / 4), 256, 0, st>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        a.x_units = 0;
+    }
     const int64_t blocks = (a.dz_units + a.x_units + 3) / 4;
     if (!blocks) return hipSuccess;
-    if (f16)
-        k_linear_grad<F16><<<(unsigned)blocks, 256, 0, st>>>(a);
+    if (f16 && a.range)
+        k_linear_grad<F16, true><<<(unsigned)blocks, 256, 0, st>>>(a);
+    else if (f16)
+        k_linear_grad<F16, false><<<(unsigned)blocks, 256, 0, st>>>(a);
     else
-        k_linear_grad<BF16><<<(unsigned)blocks, 256, 0, st>>>(a);
+        k_linear_grad<BF16, false><<<(unsigned)blocks, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 

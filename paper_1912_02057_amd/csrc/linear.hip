@@ -24,16 +24,21 @@ struct LinParams {
     int tilesM, ntiles, band_tiles;
     FastDiv div_band, div_lastband;
     Param alpha;
+    const float* unit;      // nullable: a factor of alpha
     const unsigned short *bias, *res;
     unsigned short* y;
     int8_t* zq;
     int act;
 };
 
+// What the sums are multiplied by beside alpha: the weights' operands are twice the weights.
+__device__ __forceinline__ float sum_unit(const LinParams& p) { return p.unit ? 0.5f * *p.unit : 0.5f; }
+
 // The parameters of 8 consecutive outputs (0 past the end).
 template <class T>
 __device__ __forceinline__ void load_affine(const LinParams& p, int n, float (&al)[8], float (&bi)[8])
 {
+    const float unit = sum_unit(p);
     if (n + 8 <= p.N) {
         if (p.alpha.ptr) {
             __builtin_memcpy(al, p.alpha.ptr + n, 32);
@@ -44,12 +49,12 @@ __device__ __forceinline__ void load_affine(const LinParams& p, int n, float (&a
         u32x4 b = {0, 0, 0, 0};
         if (p.bias) b = load16(p.bias + n);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) al[i] *= 0.5f, bi[i] = half_of<T>(b[i >> 1], i & 1);
+        for (int i = 0; i < 8; ++i) al[i] *= unit, bi[i] = half_of<T>(b[i >> 1], i & 1);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const bool in = n + i < p.N;
-            al[i] = in ? 0.5f * (p.alpha.ptr ? p.alpha.ptr[n + i] : p.alpha.s) : 0.f;
+            al[i] = in ? unit * (p.alpha.ptr ? p.alpha.ptr[n + i] : p.alpha.s) : 0.f;
             bi[i] = in && p.bias ? T::to_float(p.bias[n + i]) : 0.f;
         }
     }
@@ -327,13 +332,14 @@ __global__ __launch_bounds__(256, 2) void k_linear(LinParams p)
     char* zs = smem + wave * L::ZBYTES;
     const int nw = n0 + wave * L::WN, n8 = nw + (lane % CL) * 8, t0 = (lane / CL) * TPL;
     if (nw >= p.N) return;
+    const float unit = sum_unit(p);
     float al[L::TN], bi[L::TN];  // of the columns that this lane has in its accumulators
 #pragma unroll
     for (int i = 0; i < L::TN; ++i) {
         const int n = nw + i * 32 + l32;
         al[i] = bi[i] = 0.f;
         if (n < p.N) {
-            al[i] = 0.5f * (p.alpha.ptr ? p.alpha.ptr[n] : p.alpha.s);
+            al[i] = unit * (p.alpha.ptr ? p.alpha.ptr[n] : p.alpha.s);
             if (p.bias) bi[i] = T::to_float(p.bias[n]);
         }
     }
@@ -465,13 +471,14 @@ __global__ __launch_bounds__(WAVES * 64) void k_linear_few(LinParams p)
     };
     // what the outputs need beside the sums, fetched with the first weights: thread 16 RB m + i has output i of token m
     constexpr int OUTS = 16 * RB, PER = (kFewTokens * OUTS + WAVES * 64 - 1) / (WAVES * 64);
+    const float unit = sum_unit(p);
     float al[PER], bi[PER], re[PER];
 #pragma unroll
     for (int o = 0; o < PER; ++o) {
         const int at = tid + o * WAVES * 64, om = at / OUTS, on = n0 + at % OUTS;
         al[o] = bi[o] = re[o] = 0.f;
         if (om >= p.M || on >= p.N) continue;
-        al[o] = 0.5f * (p.alpha.ptr ? p.alpha.ptr[on] : p.alpha.s);
+        al[o] = unit * (p.alpha.ptr ? p.alpha.ptr[on] : p.alpha.s);
         if (p.bias) bi[o] = T::to_float(p.bias[on]);
         if (p.res) re[o] = T::to_float(p.res[om * p.ldr + on]);
     }
@@ -828,7 +835,7 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t st)
     p.ldx = a.ldx, p.ldr = a.ldr, p.ldy = a.ldy;
     const WeightShape ws(a.N, a.K);
     p.nk = (int)ws.cb, p.rb = (int)ws.rb;
-    p.alpha = a.alpha;
+    p.alpha = a.alpha, p.unit = a.unit;
     p.bias = (const unsigned short*)a.bias, p.res = (const unsigned short*)a.res;
     p.y = (unsigned short*)a.y;
     p.zq = a.zq;

@@ -42,6 +42,7 @@ struct WgParams {
     int tilesN, ntiles, band_tiles;
     FastDiv div_band, div_lastband;
     void* dw;
+    const float* unit;  // nullable: of the sums
     BiasSum bias;       // blocks behind the tiles'
 };
 
@@ -193,6 +194,7 @@ __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgP
     constexpr int CL = L::WK / 8, TPL = CL / 2;
     char* zs = smem + wave * L::ZBYTES;
     const int k8 = k0 + wk * L::WK + (lane % CL) * 8, t0 = (lane / CL) * TPL;
+    const float unit = p.unit ? *p.unit : 1.f;
 #pragma unroll 1
     for (int k = 0; k < L::TN; ++k) {
         auto put = [&](auto index) {
@@ -215,7 +217,7 @@ __global__ __launch_bounds__(256, BN * BK >= 256 * 256 ? 1 : 2) void k_wgrad(WgP
             const float* row = (const float*)(zs + (t0 + t) * L::ZPITCH + (lane % CL) * 32);
             const float4 a = *(const float4*)row, b = *(const float4*)(row + 4);
             if (n >= p.N) continue;
-            const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            const float v[8] = {a.x * unit, a.y * unit, a.z * unit, a.w * unit, b.x * unit, b.y * unit, b.z * unit, b.w * unit};
             if constexpr (F32) {
                 float* o = (float*)p.dw + ((int64_t)split * p.N + n) * p.K + k8;
                 if (k8 + 8 <= p.K) {
@@ -305,7 +307,7 @@ int64_t blocks_per_run(int64_t M, int64_t N)
 }
 
 struct BwdWork {
-    int64_t dza, dzt, xt, part, dwpart, total;
+    int64_t dza, dzt, xt, part, range, dwpart, total;
     BwdWork(int64_t M, int64_t N, int64_t K)
     {
         dza = 0;
@@ -313,7 +315,8 @@ struct BwdWork {
         xt = dzt + operand_bytes(M, N);
         part = xt + operand_bytes(M, K);
         const int64_t tb = operand_blocks(M), per = blocks_per_run(M, N);
-        dwpart = part + round_up((tb + per - 1) / per * N * 4, 256);
+        range = part + round_up((tb + per - 1) / per * N * 4, 256);
+        dwpart = range + round_up(kRangeBytes, 256);
         const WgradForm f = wgrad_form(M, N, K);
         total = dwpart + (f.splits > 1 ? round_up(f.splits * N * K * 4, 256) : 0);
     }
@@ -339,6 +342,7 @@ hipError_t launch_linear_wgrad(const WgradArgs& a, hipStream_t st)
     p.splits = f.splits, p.per = (p.steps + f.splits - 1) / f.splits;
     p.xpitch = (a.K + 31) / 32 * 2048, p.dpitch = (a.N + 31) / 32 * 2048;
     p.dw = f.splits > 1 ? a.part : a.dw;
+    p.unit = a.unit;
     p.bias = a.bias;
     hipError_t e;
     if (a.dw_f32 || f.splits > 1)
@@ -373,6 +377,12 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t st)
     g.dzt = a.dw ? a.workspace + w.dzt : nullptr;
     g.xt = a.dw ? a.workspace + w.xt : nullptr;
     g.part = a.dbias ? (float*)(a.workspace + w.part) : nullptr;
+    // float16 operands that dz is rounded to, or multiplied by alpha for, are brought into the type's range
+    const float* unit = nullptr;
+    if (a.f16 && a.M && (g.dza || (g.dzt && a.act != kActNone))) {
+        g.range = (unsigned*)(a.workspace + w.range);
+        unit = (const float*)(g.range + kRangeParts + 64);
+    }
     hipError_t e;
     if (a.M && (e = launch_linear_grad(g, a.f16, st)) != hipSuccess) return e;
     if (a.dx && a.M) {
@@ -381,7 +391,8 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t st)
         l.ldx = direct ? a.lddy : g.lda;
         l.w = a.wt;
         l.M = a.M, l.N = a.K, l.K = direct ? a.N : g.lda;
-        l.alpha.s = direct ? a.alpha.s : 1.f;
+        l.alpha.s = a.alpha.ptr ? 1.f : a.alpha.s;
+        l.unit = unit ? unit + 1 : nullptr;
         l.y = a.dx, l.ldy = a.lddx;
         l.f16 = a.f16;
         l.workspace = a.workspace + w.dza;
@@ -389,7 +400,7 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t st)
     }
     BiasSum bias = {};
     if (a.dbias) bias = {g.part, (operand_blocks(a.M) + g.per - 1) / g.per, a.N, a.dbias};
-    if (a.dw) return launch_linear_wgrad(WgradArgs{g.dzt, g.xt, a.M, a.N, a.K, a.dw, a.f16, a.dw_f32, (float*)(a.workspace + w.dwpart), bias}, st);
+    if (a.dw) return launch_linear_wgrad(WgradArgs{g.dzt, g.xt, a.M, a.N, a.K, a.dw, a.f16, a.dw_f32, a.act != kActNone ? unit : nullptr, (float*)(a.workspace + w.dwpart), bias}, st);
     return a.dbias ? launch_bias_sum(bias, a.f16, st) : hipSuccess;
 }
 

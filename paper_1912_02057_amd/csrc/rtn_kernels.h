@@ -247,6 +247,7 @@ struct LinearArgs {
     int8_t* zq;         // nullable: 8-bit checkpoint of the value before the activation
     int act;            // LinearAct
     int f16;            // 1: float16, 0: bfloat16
+    const float* unit;  // nullable: a factor of alpha in device memory
     void* workspace;    // x in rows of whole steps, where its own are not (linear_copies_x)
 };
 bool linear_copies_x(const LinearArgs& a);
@@ -262,6 +263,10 @@ struct CkptArgs {
 hipError_t launch_checkpoint_pack(const CkptArgs& a, hipStream_t st);
 hipError_t launch_checkpoint_unpack(const CkptArgs& a, hipStream_t st);
 
+// Of float16: the largest magnitude of dy, as the bits of a 16-bit value, in up to kRangeParts parts; that of alpha, as a float's, in 64; and
+// behind them the units of dzt and dza, two floats.
+constexpr int kRangeParts = 1024, kRangeBytes = (kRangeParts + 64 + 2) * 4;
+
 // What k_linear_grad writes, each of the outputs nullable.
 struct GradArgs {
     const void* dy;
@@ -269,13 +274,15 @@ struct GradArgs {
     int64_t M, N, K, lddy, lda;
     Param alpha;
     int act;
-    void* dza;    // dz alpha, row-major [M][lda], lda whole steps of 64, zeros past N
+    void* dza;    // dz times alpha where that is a vector, row-major [M][lda], lda whole steps of 64, zeros past N
     char *dzt;    // dz in operand order
+    unsigned* range;  // nullable: kRangeBytes; dza and, with an activation, dzt are then in units that end up here
     char *xt;     // x^ in operand order
     float* part;  // [runs][N]: sums of dz over runs of `per` blocks of 32 tokens
     int64_t per;
     // set by launch_linear_grad
     int64_t dz_strips, dz_units, x_strips, x_units;
+    int parts;
 };
 hipError_t launch_linear_grad(GradArgs a, int f16, hipStream_t st);
 // out[n] = sum over r of part[r][n], 16 bit; out NULL: nothing
@@ -291,6 +298,7 @@ struct WgradArgs {
     int64_t M, N, K;
     void* dw;  // [N][K]
     int f16, dw_f32;
+    const float* unit;  // nullable: the unit of dzt, in device memory
     float* part;   // wgrad_form's splits x [N][K], where there are several
     BiasSum bias;  // in the same launch
 };

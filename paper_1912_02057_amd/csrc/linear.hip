@@ -449,7 +449,6 @@ __global__ __launch_bounds__(WAVES * 64) void k_linear_few(LinParams p)
 #pragma unroll
     for (int r = 0; r < RB; ++r) acc[r][0] = acc[r][1] = f32x4{0.f, 0.f, 0.f, 0.f};
     const bool mine = l16 < p.M;  // the other lanes' columns of the result are not looked at, whatever they hold
-    const int ktail = p.K & 63;
     const auto xr = __builtin_amdgcn_make_buffer_rsrc((void*)p.x, 0, (int)(((p.M - 1) * p.ldx + p.K) * 2), 0x00020000);
     const int xoff = (int)(l16 * p.ldx * 2) + c * 16;
     int woff[RB];
@@ -485,7 +484,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_linear_few(LinParams p)
     for (int s0 = wave; s0 < p.nk; s0 += WAVES * BATCH) {
         uint2 word[BATCH][RB];
         u32x4 xf[BATCH][2];
-        // past the last step: that one again, with weights of zero
+        // past the last step: that one again, with x of zero (weights of zero would make a NaN of an infinity in x)
         auto step_at = [&](int b) {
             const int step = s0 + b * WAVES;
             return step < p.nk ? step : p.nk - 1;
@@ -502,16 +501,15 @@ __global__ __launch_bounds__(WAVES * 64) void k_linear_few(LinParams p)
                 for (int s = 0; s < 2; ++s) xf[b][s] = load_x(step_at(b), s);
 #pragma unroll
         for (int b = 0; b < BATCH; ++b) {
-            const int step = s0 + b * WAVES;
-            const unsigned real = step < p.nk ? ~0u : 0u;
-            if (ROW16 && ktail && step >= p.nk - 1) {  // columns past K
+            const int left = p.K - (s0 + b * WAVES) * 64;  // columns from the step on; 0 or less behind the last one
+            if (ROW16 ? left < 64 : left <= 0) {
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
-                    if (32 * s + 8 * c >= ktail) xf[b][s] = u32x4{0, 0, 0, 0};
+                    if (32 * s + 8 * c >= left) xf[b][s] = u32x4{0, 0, 0, 0};
             }
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
-                const uint2 w2 = make_uint2((word[b][r].x & real) << up, (word[b][r].y & real) << up);
+                const uint2 w2 = make_uint2(word[b][r].x << up, word[b][r].y << up);
                 acc[r][0] = T::mfma16(expand<0>(w2), xf[b][0], acc[r][0]);
                 acc[r][1] = T::mfma16(expand<2>(w2), xf[b][1], acc[r][1]);
             }

@@ -346,6 +346,12 @@ void* bytes_of(const at::Tensor& t, size_t need, const char* what)
     }
     return t.data_ptr();
 }
+// A workspace: the kernels write all over it (its size is the library's to check).
+void* scratch(const at::Tensor& t)
+{
+    if (!t.is_cuda() || !t.is_contiguous()) fail(PyExc_ValueError, "%s: a contiguous device buffer is required", "workspace");
+    return t.data_ptr();
+}
 void* rows2d(PyObject* o, c10::ScalarType type, int64_t rows, int64_t len, const char* what, int64_t& ld)
 {
     ld = len;
@@ -432,7 +438,7 @@ PyObject* linear(PyObject*, Args a, Py_ssize_t n)
         const size_t zb = raw_bytes(a[8], "z_ckpt"), need = rtn_linear_workspace_bytes(x, ldx, M, N, K, z != nullptr);
         at::Tensor work;
         if (need) work = given_or(a[9], "workspace", [&] { return make_bytes(need, xt); });
-        void *ws = need ? work.data_ptr() : nullptr, *st = stream();
+        void *ws = need ? scratch(work) : nullptr, *st = stream();
         const size_t wsb = need ? work.nbytes() : 0;
         const Unlocked u;
         return rtn_linear(dt, x, ldx, w, M, N, K, al.ptr, al.gran, bias, act, res, ldr, y, ldy, z, zb, ws, wsb, st);
@@ -511,7 +517,7 @@ PyObject* linear_backward(PyObject*, Args a, Py_ssize_t n)
             db = out[2].data_ptr();
         }
         const at::Tensor work = given_or(a[14], "workspace", [&] { return make_bytes(rtn_linear_backward_workspace_bytes(M, N, K), t); });
-        void *ws = work.data_ptr(), *st = stream();
+        void *ws = scratch(work), *st = stream();
         const size_t wsb = work.nbytes();
         const Unlocked u;
         return rtn_linear_backward(dt, dy, lddy, x, xb, z, zb, act, w, M, N, K, al.ptr, al.gran, dx, lddx, dw, dwt, db, ws, wsb, st);

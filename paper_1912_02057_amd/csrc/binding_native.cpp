@@ -10,6 +10,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/rtn.h"
@@ -123,7 +124,8 @@ struct Unlocked {
     ~Unlocked() { PyEval_RestoreThread(state); }
 };
 
-// Runs `f` on the arguments; a C++ exception or a wrong argument count becomes a Python error.
+// Runs `f` on the arguments; a C++ exception or a wrong argument count becomes a Python error, and torch's of a full
+// device torch.OutOfMemoryError.
 template <class F>
 PyObject* call(Py_ssize_t want, Py_ssize_t n, F f)
 {
@@ -134,6 +136,9 @@ PyObject* call(Py_ssize_t want, Py_ssize_t n, F f)
     try {
         return PyLong_FromLong(f());
     } catch (const PyError&) {
+        return nullptr;
+    } catch (const c10::OutOfMemoryError&) {
+        torch::translate_exception_to_python(std::current_exception());
         return nullptr;
     } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());

@@ -302,7 +302,8 @@ inline WgradForm wgrad_form(int64_t M, int64_t N, int64_t K)
             // (a chip that is a quarter idle runs the large tile at a higher clock)
             if (left > 0) t += (double)per * (r.tile == 256 && rounds == 0 && left <= 192 ? 1.05 : r.step[(int)(left - 1) / 256]) + r.ends;
             if (splits > 1) t += 3 + splits * (double)N * (double)K * 8 / 4.5e6;
-            if (t < least) least = t, best = {r.tile, splits};
+            // (the runs that `per` steps each make, which may be fewer)
+            if (t < least) least = t, best = {r.tile, splits > 1 ? (int)((steps + per - 1) / per) : 1};
         }
     return best;
 }

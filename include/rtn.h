@@ -437,7 +437,8 @@ int rtn_epilogue_reparam_conv2d(const int32_t *acc, int64_t Nb, int64_t C, int64
  *   z[m][n] = alpha_w[n] * sum_k x[m][k] * t_w[n][k] + bias[n]
  *   y[m][n] = act(z[m][n]) + residual[m][n]
  * from one token (m) to many.  The products with -1, 0, +1 are exact, the sums are held in fp32 and y is rounded
- * once; the order of the sums follows from the sizes, so the same arguments give the same bits.
+ * once.  Both are held at twice their size (alpha_w at half of its): a finite |x| of 2^127 or more, or a sum over k that reaches
+ * 2^127 on its way, counts as infinite (bfloat16 alone has such values; so has dz in the backward pass).  The order of the sums follows from the sizes, so the same arguments give the same bits.
  * dt: RTN_BF16 or RTN_F16, the type of x, bias, residual and y.  x, residual and y are row-major with their rows ldx, ldr,
  * ldy elements apart (at least the row's length); alpha_w: RTN_SCALAR (host) or RTN_VECTOR (device, [N]); bias and residual may
  * be NULL.  y may be the residual (the same rows at the same pitch), and may not overlap anything else.

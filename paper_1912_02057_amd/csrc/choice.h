@@ -308,4 +308,12 @@ inline WgradForm wgrad_form(int64_t M, int64_t N, int64_t K)
     return best;
 }
 
+// Blocks of 32 tokens in a run whose sums of dz are kept apart (checkpoint.hip): few runs for a long batch, one block each while there are few
+// waves.
+inline int64_t grad_blocks_per_run(int64_t M, int64_t N)
+{
+    const int64_t units = (M + 63) / 64 * 2 * ((N + 63) / 64);
+    return units >= 8 * 8192 ? 8 : units >= 2 * 8192 ? 2 : 1;
+}
+
 }  // namespace rtn

@@ -299,13 +299,6 @@ __global__ __launch_bounds__(256) void k_wgrad_sum(const float* part, int splits
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
-// Runs of token blocks whose sums of dz are kept apart: few for a long batch, one block each while there are few waves.
-int64_t blocks_per_run(int64_t M, int64_t N)
-{
-    const int64_t units = operand_blocks(M) * ((N + 63) / 64);
-    return units >= 8 * 8192 ? 8 : units >= 2 * 8192 ? 2 : 1;
-}
-
 struct BwdWork {
     int64_t dza, dzt, xt, part, range, dwpart, total;
     BwdWork(int64_t M, int64_t N, int64_t K)
@@ -314,7 +307,7 @@ struct BwdWork {
         dzt = dza + round_up(M * round_up(N, 64) * 2, 256);
         xt = dzt + operand_bytes(M, N);
         part = xt + operand_bytes(M, K);
-        const int64_t tb = operand_blocks(M), per = blocks_per_run(M, N);
+        const int64_t tb = operand_blocks(M), per = grad_blocks_per_run(M, N);
         range = part + round_up((tb + per - 1) / per * N * 4, 256);
         dwpart = range + round_up(kRangeBytes, 256);
         const WgradForm f = wgrad_form(M, N, K);
@@ -372,7 +365,7 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t st)
     g.dy = a.dy, g.zq = a.zq, g.xq = a.xq;
     g.M = a.M, g.N = a.N, g.K = a.K, g.lddy = a.lddy, g.lda = round_up(a.N, 64);
     g.alpha = a.alpha, g.act = a.act;
-    g.per = blocks_per_run(a.M, a.N);
+    g.per = grad_blocks_per_run(a.M, a.N);
     g.dza = a.dx && !direct ? a.workspace + w.dza : nullptr;
     g.dzt = a.dw ? a.workspace + w.dzt : nullptr;
     g.xt = a.dw ? a.workspace + w.xt : nullptr;

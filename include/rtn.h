@@ -438,11 +438,13 @@ int rtn_epilogue_reparam_conv2d(const int32_t *acc, int64_t Nb, int64_t C, int64
  *   y[m][n] = act(z[m][n]) + residual[m][n]
  * from one token (m) to many.  The products with -1, 0, +1 are exact, the sums are held in fp32 and y is rounded
  * once.  Both are held at twice their size (alpha_w at half of its): a finite |x| of 2^127 or more, or a sum over k that reaches
- * 2^127 on its way, counts as infinite (bfloat16 alone has such values; so has dz in the backward pass).  The order of the sums follows from the sizes, so the same arguments give the same bits.
+ * 2^127 on its way, counts as infinite (bfloat16 alone has such values; the same holds for dz in the backward pass).  The order
+ * of the sums follows from the sizes, so the same arguments give the same bits.
  * dt: RTN_BF16 or RTN_F16, the type of x, bias, residual and y.  x, residual and y are row-major with their rows ldx, ldr,
  * ldy elements apart (at least the row's length); alpha_w: RTN_SCALAR (host) or RTN_VECTOR (device, [N]); bias and residual may
  * be NULL.  y may be the residual (the same rows at the same pitch), and may not overlap anything else.
- * act: RTN_ACT_NONE, RTN_ACT_RELU, RTN_ACT_GELU (z times the normal distribution function), RTN_ACT_SILU (z / (1 + exp(-z))).
+ * act: RTN_ACT_NONE, RTN_ACT_RELU, RTN_ACT_GELU (z times the normal distribution function, within 2^-15 of itself before y's
+ * rounding), RTN_ACT_SILU (z / (1 + exp(-z))).
  * M = 0 is a call with nothing to do.  N, K <= 2^21, pitches <= 2^31, 2-byte aligned; rows of 16-byte units
  * (pointer 16-byte aligned, pitch and row length multiples of 8 elements) are read and written fastest.
  * workspace: rtn_linear_workspace_bytes() of the same x, ldx, M, N, K and z_ckpt != NULL, 0 wherever rows can be read where
@@ -480,7 +482,7 @@ int rtn_checkpoint_unpack(rtn_dtype dt, const void *ckpt, size_t ckpt_bytes, int
                           void *stream);
 
 /* Gradients of the layer from dy = dL/dy [M][N] (rows lddy apart), with z^ and x^ read back from their checkpoints:
- *   dz = dy * act'(z^)                       (act' of a relu at 0 is 0)
+ *   dz = dy * act'(z^)                       (act' of a relu at 0 is 0, and a z below half a step of its group is 0 in z^)
  *   dx[m][k] = sum_n dz[m][n] alpha_w[n] t_w[n][k]     dw[n][k] = sum_m dz[m][n] x^[m][k]     dbias[n] = sum_m dz[m][n]
  * dw is the gradient of the reparameterized weights alpha_w * t_w: as RTN_F32 it is what rtn_weight_backward takes.  The
  * gradient of the residual is dy.  dx (rows lddx apart) and dbias have type dt, dw type dw_type (dt or RTN_F32) in dense rows;

@@ -3,7 +3,7 @@
 //
 // All of them are one pass over memory.  A wave has 32 tokens x 64 channels, a lane 4 tokens of 8 channels: 4 rows of 16 bytes
 // of a 16-bit tensor (8 lanes beside each other read 128 bytes of a row), 32 bytes in a row of a checkpoint.  (8 tokens a lane need
-// twice the registers: the gradient's pass over 16384 x 8192, without an activation, took 282 us with 190 of them and takes 212 with 153.)
+// twice the registers: the gradient's pass over 16384 x 8192, without an activation, took 282 us with 190 of them and takes 212 with 163.)
 #include "linear_math.h"
 #include "rtn_kernels.h"
 

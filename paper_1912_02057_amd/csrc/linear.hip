@@ -437,8 +437,8 @@ __global__ __launch_bounds__(256, 2) void k_linear(LinParams p)
 // A few tokens (at most 16): a block has 16 RB outputs, its waves share the columns, the weights are read once and x and weights
 // go straight into registers.  v_mfma 16x16x32 takes row l & 15, columns 8 (l >> 4) .. + 7 from lane l, which lane
 // (l & 15) + 16 half + 32 (l >> 4 & 1) of the 32-row order has, in the word's first four registers (slice 2 s) or its last.
-// Bound by the widening of the weights, two vector operations for two of them, and for small layers by the latency of a load
-// after the launch.
+// Bound by the widening of the weights, two vector operations for two of them, and for small layers by latencies: the launch, what the
+// outputs need, then a round of loads for every BATCH steps of a wave, each waited for before the next is issued.
 template <class T, int RB, int WAVES, int BATCH, bool ROW16>
 __global__ __launch_bounds__(WAVES * 64) void k_linear_few(LinParams p)
 {
@@ -468,7 +468,8 @@ __global__ __launch_bounds__(WAVES * 64) void k_linear_few(LinParams p)
             return load_row8(xrow, step * 64 + 32 * s + 8 * c, p.K);
         }
     };
-    // what the outputs need beside the sums, fetched with the first weights: thread 16 RB m + i has output i of token m
+    // What the outputs need beside the sums: thread 16 RB m + i has output i of token m.  (Converted where they are loaded, so that a wave
+    // that has outputs waits for them before its first weights.)
     constexpr int OUTS = 16 * RB, PER = (kFewTokens * OUTS + WAVES * 64 - 1) / (WAVES * 64);
     const float unit = sum_unit(p);
     float al[PER], bi[PER], re[PER];

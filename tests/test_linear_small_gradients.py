@@ -92,3 +92,26 @@ def test_scales_at_their_ends(M):
     (want, ex), _, _ = L.grads64("gelu", xhat, zhat)          # terms with the subnormal steps of the unscaled type
     T.assert_within(dx[keep], want[keep], L.rounded(want, ex)[keep], "dx")
     assert not np.isfinite(dx[[1, M - 1]]).any() and np.isfinite(dw[rows]).all() and not np.isfinite(dw[[5, 40]]).any()
+
+
+def test_units_follow_the_data_of_a_replay():
+    """A recorded backward pass takes its powers of two from the dy and alpha of each replay."""
+    M, N, K = 96, 200, 136
+    L = T.Layer("fp16", M, N, K, seed=3)
+    w, wt = B.linear_prepare(L.codes, N, K, backward=True)
+    x8, z8 = B.checkpoint_pack(L.x), B.checkpoint_empty(M, N, T.DEV)
+    B.linear(L.x, w, N, L.alpha, bias=L.bias, act=T.ACTS["gelu"], z_ckpt=z8)
+    dy, alpha = L.dy.clone(), L.alpha.clone()
+    ws = torch.empty(B.lib().rtn_linear_backward_workspace_bytes(M, N, K), dtype=torch.uint8, device=T.DEV)
+    call = lambda **kw: B.linear_backward(dy, wt, K, alpha, x8, act=T.ACTS["gelu"], z_ckpt=z8, **kw)
+    dx, dw, db = call(workspace=ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(dx=dx, dw=dw, dbias=db, workspace=ws)
+    for size in (1.0, 1e-5, 3e3, 1e-3):
+        dy.copy_(L.dy * size)
+        alpha.copy_(L.alpha * size ** 0.5)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((dx, dw, db), call()))

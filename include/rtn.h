@@ -497,6 +497,94 @@ int rtn_linear_backward(rtn_dtype dt, const void *dy, int64_t lddy, const void *
                         int64_t K, const float *alpha_w, rtn_gran gran_w, void *dx, int64_t lddx, void *dw,
                         rtn_dtype dw_type, void *dbias, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- Microscaled 4-bit values --------------------------------------------------------------------
+ * A matrix v [R][C] (RTN_BF16, RTN_F16 or RTN_F32; rows ldx elements apart) in 4.25 bits a value: 32 consecutive columns of a row share
+ * a power of two 2^e, kept in 8 bits (E8M0), and a value is q 2^e with q an E2M1 code, 0, 1/2, 1, 3/2, 2, 3, 4, 6 and a sign.
+ * With a the largest magnitude of the group:
+ *   seed NULL (to nearest): e = floor(log2 a) - 2, at least -127; q is the nearest to v / 2^e, ties to the even code, 6 beyond 6.
+ *   stochastic: e is one more where a / 2^e > 6, so that nothing is beyond 6; q is the upper neighbour of |v| / 2^e in the place of the lower
+ *     one where k < 65536 times its distance from that in units of their gap, so that the expected value is v (within 2^-16 of a gap).
+ *     k are 16 bits of Philox4x32-10: key = the seed's low and high word, counter = (low and high word of the group's index
+ *     row * ceil(C / 32) + group, j, 0; for the transposed packing its own rows and groups, and 1), element i of the group takes
+ *     bits 16 (i & 1) .. of word (i / 2) & 3 of the result of j = i / 8.  The seed lies on the device, so that a captured graph can
+ *     be given another one: the same seed gives the same bits.
+ * A group that holds an infinity or NaN stands for NaN.  packed: of v; packed_t: of the transposed matrix [C][R], its groups along v's rows
+ * (the operands of products that contract over the rows); either may be NULL, not both.  rtn_mx4_bytes(R, C) and (C, R) bytes, 16-byte
+ * aligned; the layout belongs to the build of the library.  R, C <= 2^21; R = 0: nothing to do.
+ * rtn_mx4_unpack: the values that a packing stands for, rounded once to dt (exact in RTN_F32 but for 4 x 2^126, which stochastic
+ * rounding can make of the largest values; in RTN_BF16 unless e < -126; in RTN_F16 where the packed values were RTN_F16). */
+size_t rtn_mx4_bytes(int64_t R, int64_t C);
+int rtn_mx4_pack(rtn_dtype dt, const void *x, int64_t ldx, int64_t R, int64_t C, void *packed, size_t packed_bytes, void *packed_t,
+                 size_t packed_t_bytes, const uint64_t *seed, void *stream);
+int rtn_mx4_unpack(rtn_dtype dt, const void *packed, size_t packed_bytes, int64_t R, int64_t C, void *y, int64_t ldy, void *stream);
+
+/* A linear layer on the scaled FP4 matrix cores, Q(v) being what the packing of v to nearest stands for:
+ *   z[m][n] = sum_k Q(x)[m][k] Q(w)[n][k] + bias[n]        y[m][n] = act(z[m][n]) + residual[m][n]
+ * from one token (m) to many.  Products are exact, sums are held in fp32 (terms below 2^-126 count as 0) and y is rounded once; the
+ * order of the sums follows from the sizes, so the same arguments give the same bits.  packed: of w [N][K] (rtn_mx4_pack).
+ * x: [M][K] of type dt (RTN_BF16 or RTN_F16), packed on the way; or x_packed, its packing, where the program has it (training: with
+ * the transposed one, in one pass), and then x is not read and may be NULL.  bias [N] and residual [M][N] of type dt may be NULL; y may be the
+ * residual (the same rows at the same pitch) and may not overlap anything else.  act as in rtn_linear.  z_out (nullable, type dt):
+ * receives z, for the backward pass.  M, N, K <= 2^21, pitches <= 2^31.  M = 0: nothing to do.
+ * workspace: rtn_mx4_linear_workspace_bytes(M, N, K), not needed with x_packed; 16-byte aligned. */
+size_t rtn_mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int rtn_mx4_linear(rtn_dtype dt, const void *x, int64_t ldx, const void *x_packed, size_t x_packed_bytes, const void *packed,
+                   size_t packed_bytes, int64_t M, int64_t N, int64_t K, const void *bias, rtn_act act, const void *residual,
+                   int64_t ldr, void *y, int64_t ldy, void *z_out, int64_t ldz, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gradients of the layer from dy [M][N], products of packings along the dimension that each contracts over (the straight-through
+ * estimator: the gradient of Q is 1), with Qt(v) = Q(v^T):
+ *   dz = dy act'(z)             (z as z_out left it, not needed for RTN_ACT_NONE; act' of a relu at 0 is 0; fp32, not rounded)
+ *   dx[m][k] = sum_n Q(dz)[m][n] Qt(w)[k][n]    dw[n][k] = sum_m Qt(dz)[n][m] Qt(x)[k][m]    dbias[n] = sum_m dz[m][n]
+ * seed: dz is rounded stochastically (unbiased), NULL: to nearest.  packed_t of w, x_packed_t of x: from rtn_mx4_pack.  dx (rows lddx apart)
+ * and dbias have type dt, dw type dw_type (dt or RTN_F32) in dense rows; each may be NULL, not all; what only they need may be NULL then.
+ * Sums are fp32 in an order that follows from the sizes (no atomics).  M = 0 writes zeros to dw and dbias.
+ * dx may not overlap dy or z.  workspace: rtn_mx4_linear_backward_workspace_bytes(M, N, K), 16-byte aligned. */
+size_t rtn_mx4_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int rtn_mx4_linear_backward(rtn_dtype dt, const void *dy, int64_t lddy, const void *z, int64_t ldz, rtn_act act, const void *packed_t,
+                            size_t packed_t_bytes, const void *x_packed_t, size_t x_packed_t_bytes, int64_t M, int64_t N, int64_t K,
+                            const uint64_t *seed, void *dx, int64_t lddx, void *dw, rtn_dtype dw_type, void *dbias, void *workspace,
+                            size_t workspace_bytes, void *stream);
+
+/* ---- Norms before and after a block, with its gate and residual scale -------------------------------
+ *   n(v) = v / sqrt(mean v^2 + eps) (RTN_NORM_RMS) or (v - mean v) / sqrt(mean (v - mean v)^2 + eps) (RTN_NORM_LAYER) of each row
+ *   rtn_norm        u = n(x) weight + bias
+ *   rtn_block_norm  y = scale x + gate (n(h) weight + bias),  u = n(y) next_weight + next_bias
+ * the latter the end of one block, whose output is h, and the start of the next in one pass; u is of y as rounded.  u NULL: without the
+ * second line (next_weight and next_bias are then not read).
+ * dt: RTN_BF16 or RTN_F16, the type of the [M][C] tensors, each with its pitch.  weight, bias, next_weight, next_bias: device fp32 [C], the
+ * biases may be NULL.  gate: device fp32 [ceil(M / gate_run)][C], a row for every gate_run consecutive tokens (a sequence's own
+ * gate; gate_run >= M for one of all tokens), or NULL for 1 (gate_run is then not read).  scale, eps >= 0: by value.
+ * Statistics and sums are fp32 (the sum of a row's squares has to be finite there), outputs are rounded once.  C <= 16384; M = 0:
+ * nothing to do.  y may be x and u may be h or x (the same rows at the same pitch); no other overlap. */
+typedef enum { RTN_NORM_RMS = 0, RTN_NORM_LAYER = 1 } rtn_norm_kind;
+int rtn_norm(rtn_dtype dt, rtn_norm_kind kind, const void *x, int64_t ldx, int64_t M, int64_t C, const float *weight, const float *bias,
+             float eps, void *u, int64_t ldu, void *stream);
+int rtn_block_norm(rtn_dtype dt, rtn_norm_kind kind, const void *h, int64_t ldh, const void *x, int64_t ldx, int64_t M, int64_t C,
+                   const float *weight, const float *bias, const float *gate, int64_t gate_run, float scale, const float *next_weight,
+                   const float *next_bias, float eps, void *y, int64_t ldy, void *u, int64_t ldu, void *stream);
+
+/* Their gradients.  The statistics are formed again from the tensors that the forward pass read (h) and wrote (y).
+ *   rtn_norm_backward        dx = dx_add + n'(x) (du weight)         dweight = sum_m du n(x)       dbias = sum_m du
+ *     dx_add (nullable): the gradient that reaches x past the norm; dx may be dx_add or du.
+ *   rtn_block_norm_backward  d = dy + n'(y) (du next_weight), the whole gradient of y, then
+ *     dx = scale d     dh = n'(h) (d gate weight)     dweight = sum_m d gate n(h)     dbias = sum_m d gate
+ *     dgate[r] = sum over the tokens of r of d (n(h) weight + bias)     dnext_weight = sum_m du n(y)     dnext_bias = sum_m du
+ *     du NULL: y had no norm behind it (y is then not read); dy NULL: y was read by that norm alone.  Not both NULL.
+ *     bias is read for dgate only (nullable: none).  dx may be dy or du, dh may be h or the other of them.
+ * dx, dh have type dt; the gradients of the vectors are fp32, summed in an order that follows from the sizes (no atomics).  Each output may
+ * be NULL, not all.  M = 0 writes zeros to the gradients of [C].  workspace: rtn_norm_backward_workspace_bytes(M, C, gate_run)
+ * (gate_run = M without a gate and for rtn_norm_backward), 16-byte aligned; not needed if no gradient of a vector is wanted. */
+size_t rtn_norm_backward_workspace_bytes(int64_t M, int64_t C, int64_t gate_run);
+int rtn_norm_backward(rtn_dtype dt, rtn_norm_kind kind, const void *du, int64_t lddu, const void *x, int64_t ldx, int64_t M, int64_t C,
+                      const float *weight, float eps, const void *dx_add, int64_t lddx_add, void *dx, int64_t lddx, float *dweight,
+                      float *dbias, void *workspace, size_t workspace_bytes, void *stream);
+int rtn_block_norm_backward(rtn_dtype dt, rtn_norm_kind kind, const void *dy, int64_t lddy, const void *du, int64_t lddu, const void *h,
+                            int64_t ldh, const void *y, int64_t ldy, int64_t M, int64_t C, const float *weight, const float *bias,
+                            const float *gate, int64_t gate_run, float scale, const float *next_weight, float eps, void *dh,
+                            int64_t lddh, void *dx, int64_t lddx, float *dweight, float *dbias, float *dgate, float *dnext_weight,
+                            float *dnext_bias, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

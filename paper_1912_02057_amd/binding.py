@@ -24,6 +24,7 @@ RTN_PAD_TRUE_ZERO, RTN_PAD_CODE_ZERO = 0, 1
 RTN_PATH_AUTO, RTN_PATH_MFMA_I8, RTN_PATH_POPC, RTN_PATH_MFMA_FP4 = 0, 1, 2, 3
 RTN_BF16, RTN_F16, RTN_F32 = 0, 1, 2
 RTN_ACT_NONE, RTN_ACT_RELU, RTN_ACT_GELU, RTN_ACT_SILU = 0, 1, 2, 3
+RTN_NORM_RMS, RTN_NORM_LAYER = 0, 1
 
 EXPORTS = ["rtn_status_string", "rtn_last_hip_error", "rtn_num_tile_configs", "rtn_set_tile_config", "rtn_padded_k", "rtn_padded_k_format",
            "rtn_codes_bytes",
@@ -41,7 +42,10 @@ EXPORTS = ["rtn_status_string", "rtn_last_hip_error", "rtn_num_tile_configs", "r
            "rtn_ternary_depthwise_conv2d",
            "rtn_linear_prepared_bytes", "rtn_linear_prepare", "rtn_linear_workspace_bytes", "rtn_linear",
            "rtn_checkpoint_bytes", "rtn_checkpoint_pack", "rtn_checkpoint_unpack",
-           "rtn_linear_backward_workspace_bytes", "rtn_linear_backward"]
+           "rtn_linear_backward_workspace_bytes", "rtn_linear_backward",
+           "rtn_mx4_bytes", "rtn_mx4_pack", "rtn_mx4_unpack", "rtn_mx4_linear_workspace_bytes", "rtn_mx4_linear",
+           "rtn_mx4_linear_backward_workspace_bytes", "rtn_mx4_linear_backward",
+           "rtn_norm", "rtn_block_norm", "rtn_norm_backward_workspace_bytes", "rtn_norm_backward", "rtn_block_norm_backward"]
 
 
 class RtnEpilogue(C.Structure):
@@ -157,6 +161,32 @@ def lib():
         L.rtn_linear_backward_workspace_bytes.argtypes = [i64, i64, i64]
         L.rtn_linear_backward.restype = ci
         L.rtn_linear_backward.argtypes = [ci, vp, i64, vp, sz, vp, sz, ci, vp, i64, i64, i64, vp, ci, vp, i64, vp, ci, vp, vp, sz, vp]
+        cf = C.c_float
+        L.rtn_mx4_bytes.restype = sz
+        L.rtn_mx4_bytes.argtypes = [i64, i64]
+        L.rtn_mx4_pack.restype = ci
+        L.rtn_mx4_pack.argtypes = [ci, vp, i64, i64, i64, vp, sz, vp, sz, vp, vp]
+        L.rtn_mx4_unpack.restype = ci
+        L.rtn_mx4_unpack.argtypes = [ci, vp, sz, i64, i64, vp, i64, vp]
+        L.rtn_mx4_linear_workspace_bytes.restype = sz
+        L.rtn_mx4_linear_workspace_bytes.argtypes = [i64, i64, i64]
+        L.rtn_mx4_linear.restype = ci
+        L.rtn_mx4_linear.argtypes = [ci, vp, i64, vp, sz, vp, sz, i64, i64, i64, vp, ci, vp, i64, vp, i64, vp, i64, vp, sz, vp]
+        L.rtn_mx4_linear_backward_workspace_bytes.restype = sz
+        L.rtn_mx4_linear_backward_workspace_bytes.argtypes = [i64, i64, i64]
+        L.rtn_mx4_linear_backward.restype = ci
+        L.rtn_mx4_linear_backward.argtypes = [ci, vp, i64, vp, i64, ci, vp, sz, vp, sz, i64, i64, i64, vp, vp, i64, vp, ci, vp, vp, sz, vp]
+        L.rtn_norm.restype = ci
+        L.rtn_norm.argtypes = [ci, ci, vp, i64, i64, i64, vp, vp, cf, vp, i64, vp]
+        L.rtn_block_norm.restype = ci
+        L.rtn_block_norm.argtypes = [ci, ci, vp, i64, vp, i64, i64, i64, vp, vp, vp, i64, cf, vp, vp, cf, vp, i64, vp, i64, vp]
+        L.rtn_norm_backward_workspace_bytes.restype = sz
+        L.rtn_norm_backward_workspace_bytes.argtypes = [i64, i64, i64]
+        L.rtn_norm_backward.restype = ci
+        L.rtn_norm_backward.argtypes = [ci, ci, vp, i64, vp, i64, i64, i64, vp, cf, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+        L.rtn_block_norm_backward.restype = ci
+        L.rtn_block_norm_backward.argtypes = [ci, ci, vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, vp, vp, vp, i64, cf, vp, cf, vp, i64, vp,
+                                              i64, vp, vp, vp, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -577,3 +607,81 @@ def linear_backward(dy, prepared_t, K, alpha_w, x_ckpt, act=RTN_ACT_NONE, z_ckpt
     assert dw_dtype in (None, dy.dtype, torch.float32)
     return _made(_native().linear_backward(dy, prepared_t, K, alpha_w, x_ckpt, act, z_ckpt, want_dx, want_dw, want_dbias,
                                            dw_dtype is torch.float32, dx, dw, dbias, workspace), "rtn_linear_backward")
+
+
+_MX4_TYPES = {torch.bfloat16: RTN_BF16, torch.float16: RTN_F16, torch.float32: RTN_F32}
+
+
+def mx4_pack(x, seed=None, transposed=False, packed=None, packed_t=None):
+    """Microscaled 4-bit values of x, cuda bfloat16 / float16 / float32 [R, C] (rows may lie apart): groups of 32 columns share a
+    power of two.  seed: cuda int64 [1] for stochastic rounding, else to nearest.  Returns the packing, and with
+    transposed=True also that of x.t(), its groups along x's rows."""
+    r = _made(_native().mx4_pack(x, seed, transposed, packed, packed_t), "rtn_mx4_pack")
+    return r if r[1] is not None else r[0]
+
+
+def mx4_unpack(packed, R, Cc, dtype, out=None):
+    """What the packing of an [R, Cc] matrix stands for, in bfloat16, float16 or float32."""
+    if dtype not in _MX4_TYPES:
+        raise AssertionError("dtype: bfloat16, float16 or float32 is required")
+    return _made(_native().mx4_unpack(packed, R, Cc, _MX4_TYPES[dtype], out), "rtn_mx4_unpack")
+
+
+def mx4_linear(x, packed, N, bias=None, act=RTN_ACT_NONE, residual=None, y_out=None, z_out=None, x_packed=None, workspace=None):
+    """y = act(Q(x) Q(w)^T + bias) + residual on 4-bit values: x cuda bfloat16 / float16 [M, K] (rows may lie apart), packed =
+    mx4_pack(w) of w [N, K], bias [N] and residual [M, N] in x's type.  x_packed: mx4_pack(x), where the program has it; then only
+    x's shape and type are used.  z_out [M, N] receives the value before the activation.  Returns y [M, N]."""
+    return _made(_native().mx4_linear(x, packed, N, bias, act, residual, y_out, z_out, x_packed, workspace), "rtn_mx4_linear")
+
+
+def mx4_linear_backward(dy, packed_t, K, x_packed_t, act=RTN_ACT_NONE, z=None, seed=None, want_dx=True, want_dw=True, want_dbias=True,
+                        dw_dtype=None, dx=None, dw=None, dbias=None, workspace=None):
+    """Gradients of mx4_linear() from dy [M, N] (rows may lie apart) and the transposed packings of its weights and its input; z,
+    as z_out left it, unless act is RTN_ACT_NONE; seed: cuda int64 [1], dy act'(z) is then rounded stochastically.  Returns
+    (dx [M, K], dw [N, K], dbias [N]) or None in the place of what is not wanted; dw is of dy's type or dw_dtype=torch.float32."""
+    if dw_dtype not in (None, dy.dtype, torch.float32):
+        raise AssertionError("dw_dtype: dy's type or float32 is required")
+    return _made(_native().mx4_linear_backward(dy, packed_t, K, x_packed_t, act, z, seed, want_dx, want_dw, want_dbias,
+                                               dw_dtype is torch.float32, dx, dw, dbias, workspace), "rtn_mx4_linear_backward")
+
+
+def norm(x, weight, bias=None, kind=RTN_NORM_RMS, eps=1e-6, u_out=None):
+    """n(x) * weight + bias of the rows of x, cuda bfloat16 / float16 [M, C] (rows may lie apart); weight, bias cuda float32 [C]."""
+    return _made(_native().norm(x, weight, bias, kind, eps, u_out), "rtn_norm")
+
+
+def norm_backward(du, x, weight, kind=RTN_NORM_RMS, eps=1e-6, dx_add=None, want_dx=True, want_dweight=True, want_dbias=True, dx=None,
+                  dweight=None, dbias=None, workspace=None):
+    """Gradients of norm() from du [M, C] and its input; dx_add: the gradient that reaches x past the norm, added to dx.  Returns
+    (dx [M, C], dweight [C], dbias [C]), the latter two float32, or None in the place of what is not wanted."""
+    return _made(_native().norm_backward(du, x, weight, kind, eps, dx_add, want_dx, want_dweight, want_dbias, dx, dweight, dbias,
+                                         workspace), "rtn_norm_backward")
+
+
+def block_norm(h, x, weight, bias=None, gate=None, gate_run=None, scale=1.0, next_weight=None, next_bias=None, kind=RTN_NORM_RMS,
+               eps=1e-6, y_out=None, u_out=None):
+    """y = scale * x + gate * (n(h) * weight + bias) and, with next_weight, u = n(y) * next_weight + next_bias: the end of a block with
+    output h and residual x, both cuda bfloat16 / float16 [M, C] (rows may lie apart), and the start of the next.  Vectors are cuda
+    float32 [C]; gate [C], or [G, C] with a row for every gate_run consecutive tokens.  Returns (y, u), u None without next_weight."""
+    return _made(_native().block_norm(h, x, weight, bias, gate, _gate_run(gate, gate_run, h), scale, next_weight, next_bias, kind, eps, y_out,
+                                      u_out), "rtn_block_norm")
+
+
+def block_norm_backward(dy, h, weight, bias=None, gate=None, gate_run=None, scale=1.0, du=None, y=None, next_weight=None,
+                        kind=RTN_NORM_RMS, eps=1e-6, want_dh=True, want_dx=True, want_dweight=True, want_dbias=True, want_dgate=True,
+                        want_dnext_weight=True, want_dnext_bias=True, workspace=None):
+    """Gradients of block_norm() from dy (or None) and du (None without next_weight), with h and, for du, the y that it returned.
+    Returns (dh, dx, dweight, dbias, dgate, dnext_weight, dnext_bias): [M, C] in h's type, the others float32 in their vectors' shapes;
+    None in the place of what is not wanted or does not exist."""
+    return _made(_native().block_norm_backward(dy, h, weight, bias, gate, _gate_run(gate, gate_run, h), scale, du, y, next_weight, kind, eps,
+                                               want_dh, want_dx, want_dweight, want_dbias, want_dgate, want_dnext_weight, want_dnext_bias,
+                                               workspace), "rtn_block_norm_backward")
+
+
+def _gate_run(gate, gate_run, h):
+    """Tokens to a row of the gate: all of them where it has one row."""
+    if gate_run is not None:
+        return gate_run
+    if gate is not None and gate.dim() == 2 and gate.shape[0] != 1:
+        raise AssertionError("gate_run: needed for a gate of several rows")
+    return max(1, h.shape[0])

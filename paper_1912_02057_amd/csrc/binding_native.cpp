@@ -529,10 +529,300 @@ PyObject* linear_backward(PyObject*, Args a, Py_ssize_t n)
     });
 }
 
+// Kernels run on torch's current stream, which belongs to the current device: tensors of another one would be read there.
+void on_current_device(Args a, Py_ssize_t n)
+{
+    for (Py_ssize_t i = 0; i < n; ++i)
+        if (THPVariable_Check(a[i]) && THPVariable_Unpack(a[i]).is_cuda() && THPVariable_Unpack(a[i]).get_device() != c10::hip::current_device())
+            fail(PyExc_ValueError, "%s: all tensors have to be on the current device", "device");
+}
+rtn_dtype any_dtype(const at::Tensor& t, const char* what) { return dtype(t.scalar_type(), what, true); }
+const uint64_t* seed_of(PyObject* o)
+{
+    const void* p = dev(o, c10::kLong, "seed");
+    if (p && tensor(o, "seed").numel() != 1) fail(PyExc_AssertionError, "%s: one int64 on the device is required", "seed");
+    return (const uint64_t*)p;
+}
+// A given workspace of the size that is needed, or one made here; NULL where none is needed
+void* work_of(PyObject* given, size_t need, const at::Tensor& like, at::Tensor& keep, size_t& bytes)
+{
+    bytes = 0;
+    if (!need) return nullptr;
+    keep = given_or(given, "workspace", [&] { return make_bytes(need, like); });
+    bytes = keep.nbytes();
+    return scratch(keep);
+}
+float number(PyObject* o)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw PyError();
+    return (float)v;
+}
+
+// x, seed, transposed, packed, packed_t
+PyObject* mx4_pack(PyObject*, Args a, Py_ssize_t n)
+{
+    return call_for<2>(5, n, [&](at::Tensor* out) {
+        const at::Tensor& t = matrix(a[0], "x");
+        const rtn_dtype dt = any_dtype(t, "x");
+        const int64_t R = t.size(0), C = t.size(1);
+        int64_t ld;
+        const void* x = rows2d(t, t.scalar_type(), R, C, "x", ld);
+        const uint64_t* seed = seed_of(a[1]);
+        const bool both = truth(a[2]) || a[4] != Py_None;
+        on_current_device(a, n);
+        const size_t b = rtn_mx4_bytes(R, C), bt = R ? rtn_mx4_bytes(C, R) : 0;
+        out[0] = given_or(a[3], "packed", [&] { return make_bytes(b, t); });
+        void *p = bytes_of(out[0], b, "packed"), *pt = nullptr, *st = stream();
+        if (both) {
+            out[1] = given_or(a[4], "packed_t", [&] { return make_bytes(bt, t); });
+            pt = bytes_of(out[1], bt, "packed_t");
+        }
+        if (R == 0) return (int)RTN_OK;
+        const size_t pb = out[0].nbytes(), ptb = both ? out[1].nbytes() : 0;
+        const Unlocked u;
+        return rtn_mx4_pack(dt, x, ld, R, C, p, pb, pt, ptb, seed, st);
+    });
+}
+
+// packed, R, C, dtype (0 bfloat16, 1 float16, 2 float32), out
+PyObject* mx4_unpack(PyObject*, Args a, Py_ssize_t n)
+{
+    return call_for<1>(5, n, [&](at::Tensor* out) {
+        const at::Tensor& k = tensor(a[0], "packed");
+        const int64_t R = integer(a[1]), C = integer(a[2]), code = integer(a[3]);
+        const c10::ScalarType type = code == RTN_F32 ? c10::kFloat : code == RTN_F16 ? c10::kHalf : c10::kBFloat16;
+        if (R < 0 || C < 0) fail(PyExc_ValueError, "%s: sizes may not be negative", "mx4_unpack");
+        const void* kp = bytes_of(k, rtn_mx4_bytes(R, C), "packed");
+        on_current_device(a, n);
+        out[0] = given_or(a[4], "out", [&] { return make_rows(R, C, type, k); });
+        int64_t ld;
+        void *y = rows2d(out[0], type, R, C, "out", ld), *st = stream();
+        if (R == 0) return (int)RTN_OK;
+        const size_t kb = k.nbytes();
+        const Unlocked u;
+        return rtn_mx4_unpack((rtn_dtype)code, kp, kb, R, C, y, ld, st);
+    });
+}
+
+// x, packed, N, bias, act, residual, y_out, z_out, x_packed, workspace
+PyObject* mx4_linear(PyObject*, Args a, Py_ssize_t n)
+{
+    return call_for<1>(10, n, [&](at::Tensor* out) {
+        const at::Tensor& xt = matrix(a[0], "x");
+        const c10::ScalarType type = xt.scalar_type();
+        const rtn_dtype dt = dtype(type, "x");
+        const int64_t M = xt.size(0), K = xt.size(1), N = integer(a[2]);
+        if (N < 0) fail(PyExc_ValueError, "%s: sizes may not be negative", "N");
+        int64_t ldx, ldr, ldy, ldz;
+        const void* x = rows2d(xt, type, M, K, "x", ldx);
+        const void* w = bytes_of(a[1], rtn_mx4_bytes(N, K), "packed");
+        const void* bias = vector_of(a[3], type, N, "bias");
+        const rtn_act act = (rtn_act)integer(a[4]);
+        const void* res = rows2d(a[5], type, M, N, "residual", ldr);
+        void* z = rows2d(a[7], type, M, N, "z_out", ldz);
+        const void* xp = bytes_of(a[8], rtn_mx4_bytes(M, K), "x_packed");
+        on_current_device(a, n);
+        out[0] = given_or(a[6], "y_out", [&] { return make_rows(M, N, type, xt); });
+        void* y = rows2d(out[0], type, M, N, "y_out", ldy);
+        at::Tensor work;
+        size_t wsb;
+        void *ws = work_of(a[9], a[8] != Py_None ? 0 : rtn_mx4_linear_workspace_bytes(M, N, K), xt, work, wsb), *st = stream();
+        const size_t wb = raw_bytes(a[1], "packed"), xb = raw_bytes(a[8], "x_packed");
+        const Unlocked u;
+        return rtn_mx4_linear(dt, x, ldx, xp, xb, w, wb, M, N, K, bias, act, res, ldr, y, ldy, z, ldz, ws, wsb, st);
+    });
+}
+
+// dy, packed_t, K, x_packed_t, act, z, seed, want_dx, want_dw, want_dbias, dw in fp32, dx, dw, dbias, workspace
+PyObject* mx4_linear_backward(PyObject*, Args a, Py_ssize_t n)
+{
+    return call_for<3>(15, n, [&](at::Tensor* out) {
+        const at::Tensor& t = matrix(a[0], "dy");
+        const c10::ScalarType type = t.scalar_type();
+        const rtn_dtype dt = dtype(type, "dy");
+        const int64_t M = t.size(0), N = t.size(1), K = integer(a[2]);
+        if (K < 0) fail(PyExc_ValueError, "%s: sizes may not be negative", "K");
+        int64_t lddy, ldz, lddx = K, lddw;
+        const void* dy = rows2d(t, type, M, N, "dy", lddy);
+        const void* w = bytes_of(a[1], rtn_mx4_bytes(K, N), "packed_t");
+        const void* x = bytes_of(a[3], M ? rtn_mx4_bytes(K, M) : 0, "x_packed_t");
+        const rtn_act act = (rtn_act)integer(a[4]);
+        const void* z = rows2d(a[5], type, M, N, "z", ldz);
+        const uint64_t* seed = seed_of(a[6]);
+        on_current_device(a, n);
+        void *dx = nullptr, *dw = nullptr, *db = nullptr;
+        rtn_dtype dwt = dt;
+        if (truth(a[7])) {
+            out[0] = given_or(a[11], "dx", [&] { return make_rows(M, K, type, t); });
+            dx = rows2d(out[0], type, M, K, "dx", lddx);
+        }
+        if (truth(a[8])) {
+            out[1] = given_or(a[12], "dw", [&] { return make_rows(N, K, truth(a[10]) ? c10::kFloat : type, t); });
+            dwt = dtype(out[1].scalar_type(), "dw", true);
+            dw = rows2d(out[1], out[1].scalar_type(), N, K, "dw", lddw);
+            if (lddw != K) fail(PyExc_AssertionError, "%s: a contiguous tensor is required", "dw");
+        }
+        if (truth(a[9])) {
+            out[2] = given_or(a[13], "dbias", [&] { return at::empty({N}, t.options()); });
+            if (!out[2].is_cuda() || out[2].scalar_type() != type || !out[2].is_contiguous() || out[2].numel() != N)
+                fail(PyExc_AssertionError, "%s: a contiguous device tensor of dy's type, one entry per output, is required", "dbias");
+            db = out[2].data_ptr();
+        }
+        at::Tensor work;
+        size_t wsb;
+        void *ws = work_of(a[14], rtn_mx4_linear_backward_workspace_bytes(M, N, K), t, work, wsb), *st = stream();
+        const size_t wb = raw_bytes(a[1], "packed_t"), xb = raw_bytes(a[3], "x_packed_t");
+        const Unlocked u;
+        return rtn_mx4_linear_backward(dt, dy, lddy, z, ldz, act, w, wb, x, xb, M, N, K, seed, dx, lddx, dw, dwt, db, ws, wsb, st);
+    });
+}
+
+// fp32 vectors and matrices of gradients: wanted or not, given or made
+float* grad_of(at::Tensor& out, PyObject* given, bool want, int64_t rows, int64_t C, const at::Tensor& like, const char* what)
+{
+    if (!want && given == Py_None) return nullptr;
+    out = given_or(given, what, [&] { return rows < 0 ? at::empty({C}, like.options().dtype(c10::kFloat)) : make_rows(rows, C, c10::kFloat, like); });
+    if (!out.is_cuda() || out.scalar_type() != c10::kFloat || !out.is_contiguous() || out.numel() != (rows < 0 ? 1 : rows) * C)
+        fail(PyExc_AssertionError, "%s: a contiguous device float32 tensor of the documented shape is required", what);
+    return (float*)out.data_ptr();
+}
+
+// x, weight, bias, kind, eps, u_out
+PyObject* norm(PyObject*, Args a, Py_ssize_t n)
+{
+    return call_for<1>(6, n, [&](at::Tensor* out) {
+        const at::Tensor& t = matrix(a[0], "x");
+        const c10::ScalarType type = t.scalar_type();
+        const rtn_dtype dt = dtype(type, "x");
+        const int64_t M = t.size(0), C = t.size(1);
+        int64_t ldx, ldu;
+        const void* x = rows2d(t, type, M, C, "x", ldx);
+        const float *w = (const float*)vector_of(a[1], c10::kFloat, C, "weight"), *b = (const float*)vector_of(a[2], c10::kFloat, C, "bias");
+        const rtn_norm_kind kind = (rtn_norm_kind)integer(a[3]);
+        const float eps = number(a[4]);
+        on_current_device(a, n);
+        out[0] = given_or(a[5], "u_out", [&] { return make_rows(M, C, type, t); });
+        void *u = rows2d(out[0], type, M, C, "u_out", ldu), *st = stream();
+        const Unlocked un;
+        return rtn_norm(dt, kind, x, ldx, M, C, w, b, eps, u, ldu, st);
+    });
+}
+
+// du, x, weight, kind, eps, dx_add, want_dx, want_dweight, want_dbias, dx, dweight, dbias, workspace
+PyObject* norm_backward(PyObject*, Args a, Py_ssize_t n)
+{
+    return call_for<3>(13, n, [&](at::Tensor* out) {
+        const at::Tensor& t = matrix(a[0], "du");
+        const c10::ScalarType type = t.scalar_type();
+        const rtn_dtype dt = dtype(type, "du");
+        const int64_t M = t.size(0), C = t.size(1);
+        int64_t lddu, ldx, lda, lddx = C;
+        const void *du = rows2d(t, type, M, C, "du", lddu), *x = rows2d(a[1], type, M, C, "x", ldx);
+        const float* w = (const float*)vector_of(a[2], c10::kFloat, C, "weight");
+        const rtn_norm_kind kind = (rtn_norm_kind)integer(a[3]);
+        const float eps = number(a[4]);
+        const void* add = rows2d(a[5], type, M, C, "dx_add", lda);
+        on_current_device(a, n);
+        void* dx = nullptr;
+        if (truth(a[6]) || a[9] != Py_None) {
+            out[0] = given_or(a[9], "dx", [&] { return make_rows(M, C, type, t); });
+            dx = rows2d(out[0], type, M, C, "dx", lddx);
+        }
+        float *dw = grad_of(out[1], a[10], truth(a[7]), -1, C, t, "dweight"), *db = grad_of(out[2], a[11], truth(a[8]), -1, C, t, "dbias");
+        at::Tensor work;
+        size_t wsb;
+        void *ws = work_of(a[12], dw || db ? rtn_norm_backward_workspace_bytes(M, C, M) : 0, t, work, wsb), *st = stream();
+        const Unlocked u;
+        return rtn_norm_backward(dt, kind, du, lddu, x, ldx, M, C, w, eps, add, lda, dx, lddx, dw, db, ws, wsb, st);
+    });
+}
+
+// The rows of a gate [rows][C] or [C], of which each serves `run` of M tokens
+const float* gate_of(PyObject* o, int64_t M, int64_t C, int64_t run)
+{
+    const float* p = (const float*)dev(o, c10::kFloat, "gate");
+    if (!p) return nullptr;
+    if (run <= 0 || tensor(o, "gate").numel() < (M ? (M + run - 1) / run : 0) * C || (M && tensor(o, "gate").size(-1) != C))
+        fail(PyExc_AssertionError, "%s: a row of entries for every gate_run tokens is required", "gate");
+    return p;
+}
+
+// h, x, weight, bias, gate, gate_run, scale, next_weight, next_bias, kind, eps, y_out, u_out
+PyObject* block_norm(PyObject*, Args a, Py_ssize_t n)
+{
+    return call_for<2>(13, n, [&](at::Tensor* out) {
+        const at::Tensor& t = matrix(a[0], "h");
+        const c10::ScalarType type = t.scalar_type();
+        const rtn_dtype dt = dtype(type, "h");
+        const int64_t M = t.size(0), C = t.size(1), run = integer(a[5]);
+        int64_t ldh, ldx, ldy, ldu = C;
+        const void *h = rows2d(t, type, M, C, "h", ldh), *x = rows2d(a[1], type, M, C, "x", ldx);
+        const float *w = (const float*)vector_of(a[2], c10::kFloat, C, "weight"), *b = (const float*)vector_of(a[3], c10::kFloat, C, "bias"),
+                    *g = gate_of(a[4], M, C, run), *nw = (const float*)vector_of(a[7], c10::kFloat, C, "next_weight"),
+                    *nb = (const float*)vector_of(a[8], c10::kFloat, C, "next_bias");
+        const float scale = number(a[6]), eps = number(a[10]);
+        const rtn_norm_kind kind = (rtn_norm_kind)integer(a[9]);
+        on_current_device(a, n);
+        out[0] = given_or(a[11], "y_out", [&] { return make_rows(M, C, type, t); });
+        void *y = rows2d(out[0], type, M, C, "y_out", ldy), *u = nullptr, *st = stream();
+        if (nw || a[12] != Py_None) {
+            out[1] = given_or(a[12], "u_out", [&] { return make_rows(M, C, type, t); });
+            u = rows2d(out[1], type, M, C, "u_out", ldu);
+        }
+        const Unlocked un;
+        return rtn_block_norm(dt, kind, h, ldh, x, ldx, M, C, w, b, g, run, scale, nw, nb, eps, y, ldy, u, ldu, st);
+    });
+}
+
+// dy, h, weight, bias, gate, gate_run, scale, du, y, next_weight, kind, eps, want (dh, dx, dweight, dbias, dgate, dnext_weight,
+// dnext_bias), workspace
+PyObject* block_norm_backward(PyObject*, Args a, Py_ssize_t n)
+{
+    return call_for<7>(20, n, [&](at::Tensor* out) {
+        const at::Tensor& t = matrix(a[1], "h");
+        const c10::ScalarType type = t.scalar_type();
+        const rtn_dtype dt = dtype(type, "h");
+        const int64_t M = t.size(0), C = t.size(1), run = integer(a[5]);
+        int64_t lddy, ldh, lddu, ldy;
+        const void *dy = rows2d(a[0], type, M, C, "dy", lddy), *h = rows2d(t, type, M, C, "h", ldh), *du = rows2d(a[7], type, M, C, "du", lddu),
+                   *y = rows2d(a[8], type, M, C, "y", ldy);
+        const float *w = (const float*)vector_of(a[2], c10::kFloat, C, "weight"), *b = (const float*)vector_of(a[3], c10::kFloat, C, "bias"),
+                    *g = gate_of(a[4], M, C, run), *nw = (const float*)vector_of(a[9], c10::kFloat, C, "next_weight");
+        const float scale = number(a[6]), eps = number(a[11]);
+        const rtn_norm_kind kind = (rtn_norm_kind)integer(a[10]);
+        on_current_device(a, n);
+        void* d[2] = {nullptr, nullptr};
+        for (int i = 0; i < 2; ++i)
+            if (truth(a[12 + i])) {
+                out[i] = make_rows(M, C, type, t);
+                d[i] = out[i].data_ptr();
+            }
+        float* s[5];
+        const char* const names[5] = {"dweight", "dbias", "dgate", "dnext_weight", "dnext_bias"};
+        bool any = false;
+        for (int i = 0; i < 5; ++i) {
+            // (by the arguments, not their pointers, which are NULL for tensors of no rows)
+            const bool rows = i == 2 && a[4] != Py_None, exists = i == 2 ? rows : i < 3 || a[7] != Py_None;
+            s[i] = grad_of(out[2 + i], Py_None, truth(a[14 + i]) && exists, rows ? tensor(a[4], "gate").numel() / C : -1, C, t, names[i]);
+            any |= s[i] != nullptr;
+        }
+        if (out[4].defined()) out[4] = out[4].view(tensor(a[4], "gate").sizes());
+        at::Tensor work;
+        size_t wsb;
+        void *ws = work_of(a[19], any ? rtn_norm_backward_workspace_bytes(M, C, g ? run : M) : 0, t, work, wsb), *st = stream();
+        const Unlocked u;
+        return rtn_block_norm_backward(dt, kind, dy, lddy, du, lddu, h, ldh, y, ldy, M, C, w, b, g, run, scale, nw, eps, d[0], C, d[1], C, s[0],
+                                       s[1], s[2], s[3], s[4], ws, wsb, st);
+    });
+}
+
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(pack), FAST(gemm), FAST(conv2d), FAST(conv2d_ternarize), FAST(depthwise), FAST(weight_gemm),
                          FAST(weight_conv2d_prepared), FAST(activation_backward), FAST(weight_backward),
-                         FAST(linear_prepare), FAST(linear), FAST(checkpoint_pack), FAST(checkpoint_unpack), FAST(linear_backward), {nullptr, nullptr, 0, nullptr}};
+                         FAST(linear_prepare), FAST(linear), FAST(checkpoint_pack), FAST(checkpoint_unpack), FAST(linear_backward),
+                         FAST(mx4_pack), FAST(mx4_unpack), FAST(mx4_linear), FAST(mx4_linear_backward), FAST(norm), FAST(norm_backward),
+                         FAST(block_norm), FAST(block_norm_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

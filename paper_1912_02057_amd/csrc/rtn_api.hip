@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include "linear_math.h"
+#include "mx4_math.h"
 #include "rtn_kernels.h"
 
 namespace {
@@ -96,6 +97,12 @@ constexpr int64_t kMaxFeatures = 1LL << 21;
 bool linear_dims(int64_t N, int64_t K) { return N > 0 && K > 0 && N <= kMaxFeatures && K <= kMaxFeatures; }
 bool linear_rows(int64_t M, int64_t len, int64_t ld) { return M >= 0 && M <= kMaxDim && ld >= len && ld <= (1LL << 31); }
 bool ckpt_units(int64_t M, int64_t C) { return (double)((M + 63) / 32) * (double)((C + 63) / 64) < (double)(1LL << 31); }
+// Microscaled 4-bit matrices: either dimension may be the one that a product contracts over.
+bool mx4_dims(int64_t R, int64_t C) { return R >= 0 && R <= kMaxFeatures && C > 0 && C <= kMaxFeatures; }
+bool row_pitch(int64_t len, int64_t ld) { return ld >= len && ld <= (1LL << 31); }
+size_t type_bytes(rtn_dtype dt) { return dt == RTN_F32 ? 4 : 2; }
+constexpr int64_t kMaxNormed = 16384;  // columns of a row that one unit of k_norm keeps in registers
+bool norm_dims(int64_t M, int64_t C) { return M >= 0 && M <= kMaxDim && C > 0 && C <= kMaxNormed; }
 bool known_act(rtn_act act) { return act >= RTN_ACT_NONE && act <= RTN_ACT_SILU; }
 
 }  // namespace
@@ -802,6 +809,200 @@ int rtn_linear_backward(rtn_dtype dt, const void* dy, int64_t lddy, const void* 
     a.dx = dx, a.dw = dw, a.dbias = dbias;
     a.workspace = (char*)workspace;
     const hipError_t e = rtn::launch_linear_backward(a, (hipStream_t)stream);
+    return e == hipSuccess ? RTN_OK : hip_fail(e);
+}
+
+size_t rtn_mx4_bytes(int64_t R, int64_t C) { return mx4_dims(R, C) ? (size_t)rtn::Mx4Shape(R, C).bytes() : 0; }
+
+int rtn_mx4_pack(rtn_dtype dt, const void* x, int64_t ldx, int64_t R, int64_t C, void* packed, size_t packed_bytes, void* packed_t,
+                 size_t packed_t_bytes, const uint64_t* seed, void* stream)
+{
+    if ((!packed && !packed_t) || (R != 0 && !x)) return RTN_ERR_NULL;
+    if (dt != RTN_BF16 && dt != RTN_F16 && dt != RTN_F32) return RTN_ERR_UNSUPPORTED;
+    if (!mx4_dims(R, C) || !row_pitch(C, ldx)) return RTN_ERR_SHAPE;
+    if (!aligned(x, type_bytes(dt)) || !aligned(packed, 16) || !aligned(packed_t, 16) || !aligned(seed, 8)) return RTN_ERR_ALIGN;
+    if ((packed && packed_bytes < rtn_mx4_bytes(R, C)) || (packed_t && R && packed_t_bytes < rtn_mx4_bytes(C, R))) return RTN_ERR_WORKSPACE;
+    if (R == 0) return RTN_OK;
+    rtn::Mx4PackArgs a = {};
+    a.x = x, a.R = R, a.C = C, a.ldx = ldx;
+    a.out = packed, a.out_t = packed_t, a.seed = seed;
+    a.type = (int)dt;
+    const hipError_t e = rtn::launch_mx4_pack(a, (hipStream_t)stream);
+    return e == hipSuccess ? RTN_OK : hip_fail(e);
+}
+
+int rtn_mx4_unpack(rtn_dtype dt, const void* packed, size_t packed_bytes, int64_t R, int64_t C, void* y, int64_t ldy, void* stream)
+{
+    if (R != 0 && (!packed || !y)) return RTN_ERR_NULL;
+    if (dt != RTN_BF16 && dt != RTN_F16 && dt != RTN_F32) return RTN_ERR_UNSUPPORTED;
+    if (!mx4_dims(R, C) || !row_pitch(C, ldy)) return RTN_ERR_SHAPE;
+    if (!aligned(y, type_bytes(dt)) || !aligned(packed, 16)) return RTN_ERR_ALIGN;
+    if (packed_bytes < rtn_mx4_bytes(R, C)) return RTN_ERR_WORKSPACE;
+    if (R == 0) return RTN_OK;
+    const rtn::Mx4UnpackArgs a = {packed, R, C, ldy, y, (int)dt};
+    const hipError_t e = rtn::launch_mx4_unpack(a, (hipStream_t)stream);
+    return e == hipSuccess ? RTN_OK : hip_fail(e);
+}
+
+size_t rtn_mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K)
+{
+    if (!mx4_dims(M, K) || !linear_dims(N, K) || M == 0) return 0;
+    return rtn::mx4_packs_x(M, N, K) ? rtn_mx4_bytes(M, K) : 0;
+}
+
+int rtn_mx4_linear(rtn_dtype dt, const void* x, int64_t ldx, const void* x_packed, size_t x_packed_bytes, const void* packed,
+                   size_t packed_bytes, int64_t M, int64_t N, int64_t K, const void* bias, rtn_act act, const void* residual,
+                   int64_t ldr, void* y, int64_t ldy, void* z_out, int64_t ldz, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!packed || (M != 0 && ((!x && !x_packed) || !y))) return RTN_ERR_NULL;
+    if ((dt != RTN_BF16 && dt != RTN_F16) || !known_act(act)) return RTN_ERR_UNSUPPORTED;
+    if (!mx4_dims(M, K) || !linear_dims(N, K) || (!x_packed && !row_pitch(K, ldx)) || !row_pitch(N, ldy) ||
+        (residual && !row_pitch(N, ldr)) || (z_out && !row_pitch(N, ldz)))
+        return RTN_ERR_SHAPE;
+    if (!aligned(x, 2) || !aligned(y, 2) || !aligned(bias, 2) || !aligned(residual, 2) || !aligned(z_out, 2) || !aligned(packed, 16) ||
+        !aligned(x_packed, 16))
+        return RTN_ERR_ALIGN;
+    if (packed_bytes < rtn_mx4_bytes(N, K) || (x_packed && x_packed_bytes < rtn_mx4_bytes(M, K))) return RTN_ERR_WORKSPACE;
+    if (M == 0) return RTN_OK;
+    const size_t need = x_packed ? 0 : rtn_mx4_linear_workspace_bytes(M, N, K);
+    if (need && (!workspace || workspace_bytes < need)) return RTN_ERR_WORKSPACE;
+    if (need && !aligned(workspace, 16)) return RTN_ERR_ALIGN;
+    rtn::Mx4LinArgs a = {};
+    a.x = x, a.a = x_packed, a.w = packed;
+    a.M = M, a.N = N, a.K = K, a.ldx = ldx, a.ldr = ldr, a.ldy = ldy, a.ldz = ldz;
+    a.bias = bias, a.res = residual, a.y = y, a.z = z_out;
+    a.act = (int)act, a.f16 = dt == RTN_F16;
+    a.workspace = workspace;
+    const hipError_t e = rtn::launch_mx4_linear(a, (hipStream_t)stream);
+    return e == hipSuccess ? RTN_OK : hip_fail(e);
+}
+
+size_t rtn_mx4_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K)
+{
+    return mx4_dims(M, K) && linear_dims(N, K) ? rtn::mx4_backward_workspace(M, N, K) : 0;
+}
+
+int rtn_mx4_linear_backward(rtn_dtype dt, const void* dy, int64_t lddy, const void* z, int64_t ldz, rtn_act act, const void* packed_t,
+                            size_t packed_t_bytes, const void* x_packed_t, size_t x_packed_t_bytes, int64_t M, int64_t N, int64_t K,
+                            const uint64_t* seed, void* dx, int64_t lddx, void* dw, rtn_dtype dw_type, void* dbias, void* workspace,
+                            size_t workspace_bytes, void* stream)
+{
+    if ((!dx && !dw && !dbias) || (M != 0 && !dy)) return RTN_ERR_NULL;
+    if ((dt != RTN_BF16 && dt != RTN_F16) || !known_act(act)) return RTN_ERR_UNSUPPORTED;
+    if (dw && dw_type != dt && dw_type != RTN_F32) return RTN_ERR_UNSUPPORTED;
+    if (M != 0 && ((dx && !packed_t) || (dw && !x_packed_t) || (act != RTN_ACT_NONE && !z))) return RTN_ERR_NULL;
+    if (!mx4_dims(M, K) || !linear_dims(N, K) || !row_pitch(N, lddy) || (dx && !row_pitch(K, lddx)) ||
+        (act != RTN_ACT_NONE && !row_pitch(N, ldz)))
+        return RTN_ERR_SHAPE;
+    if (!aligned(dy, 2) || !aligned(z, 2) || !aligned(dx, 2) || !aligned(dw, dw_type == RTN_F32 ? 4 : 2) || !aligned(dbias, 2) ||
+        !aligned(packed_t, 16) || !aligned(x_packed_t, 16) || !aligned(seed, 8) || !aligned(workspace, 16))
+        return RTN_ERR_ALIGN;
+    if (M != 0 && ((dx && packed_t_bytes < rtn_mx4_bytes(K, N)) || (dw && x_packed_t_bytes < rtn_mx4_bytes(K, M)) || !workspace ||
+                   workspace_bytes < rtn_mx4_linear_backward_workspace_bytes(M, N, K)))
+        return RTN_ERR_WORKSPACE;
+    rtn::Mx4BwdArgs a = {};
+    a.dy = dy, a.z = z, a.wt = packed_t, a.xt = x_packed_t;
+    a.M = M, a.N = N, a.K = K, a.lddy = lddy, a.ldz = ldz, a.lddx = lddx;
+    a.seed = seed, a.act = (int)act, a.f16 = dt == RTN_F16, a.dw_f32 = dw_type == RTN_F32;
+    a.dx = dx, a.dw = dw, a.dbias = dbias, a.workspace = (char*)workspace;
+    const hipError_t e = rtn::launch_mx4_backward(a, (hipStream_t)stream);
+    return e == hipSuccess ? RTN_OK : hip_fail(e);
+}
+
+int rtn_norm(rtn_dtype dt, rtn_norm_kind kind, const void* x, int64_t ldx, int64_t M, int64_t C, const float* weight, const float* bias,
+             float eps, void* u, int64_t ldu, void* stream)
+{
+    if (!weight || (M != 0 && (!x || !u))) return RTN_ERR_NULL;
+    if ((dt != RTN_BF16 && dt != RTN_F16) || (kind != RTN_NORM_RMS && kind != RTN_NORM_LAYER)) return RTN_ERR_UNSUPPORTED;
+    if (!norm_dims(M, C) || !row_pitch(C, ldx) || !row_pitch(C, ldu) || !(eps >= 0.f)) return RTN_ERR_SHAPE;
+    if (!aligned(x, 2) || !aligned(u, 2) || !aligned(weight, 4) || !aligned(bias, 4)) return RTN_ERR_ALIGN;
+    if (M == 0) return RTN_OK;
+    rtn::NormArgs a = {};
+    a.x = x, a.u = u, a.M = M, a.C = C, a.ldx = ldx, a.ldu = ldu;
+    a.next_weight = weight, a.next_bias = bias, a.run = M, a.eps = eps;
+    a.layer = kind == RTN_NORM_LAYER, a.f16 = dt == RTN_F16;
+    const hipError_t e = rtn::launch_norm(a, (hipStream_t)stream);
+    return e == hipSuccess ? RTN_OK : hip_fail(e);
+}
+
+int rtn_block_norm(rtn_dtype dt, rtn_norm_kind kind, const void* h, int64_t ldh, const void* x, int64_t ldx, int64_t M, int64_t C,
+                   const float* weight, const float* bias, const float* gate, int64_t gate_run, float scale, const float* next_weight,
+                   const float* next_bias, float eps, void* y, int64_t ldy, void* u, int64_t ldu, void* stream)
+{
+    if (!weight || (M != 0 && (!h || !x || !y)) || (u && !next_weight)) return RTN_ERR_NULL;
+    if ((dt != RTN_BF16 && dt != RTN_F16) || (kind != RTN_NORM_RMS && kind != RTN_NORM_LAYER)) return RTN_ERR_UNSUPPORTED;
+    if (!norm_dims(M, C) || !row_pitch(C, ldh) || !row_pitch(C, ldx) || !row_pitch(C, ldy) || (u && !row_pitch(C, ldu)) || !(eps >= 0.f) ||
+        (gate && gate_run <= 0))
+        return RTN_ERR_SHAPE;
+    if (!aligned(h, 2) || !aligned(x, 2) || !aligned(y, 2) || !aligned(u, 2) || !aligned(weight, 4) || !aligned(bias, 4) ||
+        !aligned(gate, 4) || !aligned(next_weight, 4) || !aligned(next_bias, 4))
+        return RTN_ERR_ALIGN;
+    if (M == 0) return RTN_OK;
+    rtn::NormArgs a = {};
+    a.h = h, a.x = x, a.y = y, a.u = u, a.M = M, a.C = C, a.ldh = ldh, a.ldx = ldx, a.ldy = ldy, a.ldu = ldu;
+    a.weight = weight, a.bias = bias, a.gate = gate, a.next_weight = next_weight, a.next_bias = next_bias;
+    a.run = gate ? gate_run : M, a.scale = scale, a.eps = eps;
+    a.layer = kind == RTN_NORM_LAYER, a.f16 = dt == RTN_F16;
+    const hipError_t e = rtn::launch_norm(a, (hipStream_t)stream);
+    return e == hipSuccess ? RTN_OK : hip_fail(e);
+}
+
+size_t rtn_norm_backward_workspace_bytes(int64_t M, int64_t C, int64_t gate_run)
+{
+    return norm_dims(M, C) && (M == 0 || gate_run > 0) ? rtn::norm_backward_workspace(M, C, gate_run) : 0;
+}
+
+int rtn_norm_backward(rtn_dtype dt, rtn_norm_kind kind, const void* du, int64_t lddu, const void* x, int64_t ldx, int64_t M, int64_t C,
+                      const float* weight, float eps, const void* dx_add, int64_t lddx_add, void* dx, int64_t lddx, float* dweight,
+                      float* dbias, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if ((!dx && !dweight && !dbias) || !weight || (M != 0 && (!du || !x))) return RTN_ERR_NULL;
+    if ((dt != RTN_BF16 && dt != RTN_F16) || (kind != RTN_NORM_RMS && kind != RTN_NORM_LAYER)) return RTN_ERR_UNSUPPORTED;
+    if (!norm_dims(M, C) || !row_pitch(C, lddu) || !row_pitch(C, ldx) || (dx_add && !row_pitch(C, lddx_add)) || (dx && !row_pitch(C, lddx)) ||
+        !(eps >= 0.f))
+        return RTN_ERR_SHAPE;
+    if (!aligned(du, 2) || !aligned(x, 2) || !aligned(dx_add, 2) || !aligned(dx, 2) || !aligned(weight, 4) || !aligned(dweight, 4) ||
+        !aligned(dbias, 4) || !aligned(workspace, 16))
+        return RTN_ERR_ALIGN;
+    if (M != 0 && (dweight || dbias) && (!workspace || workspace_bytes < rtn_norm_backward_workspace_bytes(M, C, M))) return RTN_ERR_WORKSPACE;
+    rtn::NormBackArgs a = {};
+    a.dy = dx_add, a.du = du, a.y = x, a.dx = dx;
+    a.M = M, a.C = C, a.lddy = lddx_add, a.lddu = lddu, a.ldy = ldx, a.lddx = lddx;
+    a.next_weight = weight, a.run = M, a.scale = 1.f, a.eps = eps;
+    a.layer = kind == RTN_NORM_LAYER, a.f16 = dt == RTN_F16;
+    rtn::NormGrads g = {};
+    g.dnext_weight = dweight, g.dnext_bias = dbias;
+    const hipError_t e = rtn::launch_norm_backward(a, g, (float*)workspace, (hipStream_t)stream);
+    return e == hipSuccess ? RTN_OK : hip_fail(e);
+}
+
+int rtn_block_norm_backward(rtn_dtype dt, rtn_norm_kind kind, const void* dy, int64_t lddy, const void* du, int64_t lddu, const void* h,
+                            int64_t ldh, const void* y, int64_t ldy, int64_t M, int64_t C, const float* weight, const float* bias,
+                            const float* gate, int64_t gate_run, float scale, const float* next_weight, float eps, void* dh,
+                            int64_t lddh, void* dx, int64_t lddx, float* dweight, float* dbias, float* dgate, float* dnext_weight,
+                            float* dnext_bias, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const bool sums = dweight || dbias || dgate || dnext_weight || dnext_bias;
+    if ((!dh && !dx && !sums) || !weight || (dgate && !gate)) return RTN_ERR_NULL;
+    if (M != 0 && ((!dy && !du) || !h || (du && (!y || !next_weight)))) return RTN_ERR_NULL;
+    if ((dnext_weight || dnext_bias) && M != 0 && !du) return RTN_ERR_NULL;
+    if ((dt != RTN_BF16 && dt != RTN_F16) || (kind != RTN_NORM_RMS && kind != RTN_NORM_LAYER)) return RTN_ERR_UNSUPPORTED;
+    if (!norm_dims(M, C) || (dy && !row_pitch(C, lddy)) || (du && (!row_pitch(C, lddu) || !row_pitch(C, ldy))) || !row_pitch(C, ldh) ||
+        (dh && !row_pitch(C, lddh)) || (dx && !row_pitch(C, lddx)) || !(eps >= 0.f) || (gate && gate_run <= 0))
+        return RTN_ERR_SHAPE;
+    if (!aligned(dy, 2) || !aligned(du, 2) || !aligned(h, 2) || !aligned(y, 2) || !aligned(dh, 2) || !aligned(dx, 2) || !aligned(weight, 4) ||
+        !aligned(bias, 4) || !aligned(gate, 4) || !aligned(next_weight, 4) || !aligned(dweight, 4) || !aligned(dbias, 4) ||
+        !aligned(dgate, 4) || !aligned(dnext_weight, 4) || !aligned(dnext_bias, 4) || !aligned(workspace, 16))
+        return RTN_ERR_ALIGN;
+    const int64_t run = gate ? gate_run : M;
+    if (M != 0 && sums && (!workspace || workspace_bytes < rtn_norm_backward_workspace_bytes(M, C, run))) return RTN_ERR_WORKSPACE;
+    rtn::NormBackArgs a = {};
+    a.dy = dy, a.du = du, a.h = h, a.y = y, a.dh = dh, a.dx = dx;
+    a.M = M, a.C = C, a.lddy = lddy, a.lddu = lddu, a.ldh = ldh, a.ldy = ldy, a.lddh = lddh, a.lddx = lddx;
+    a.weight = weight, a.gate = gate, a.next_weight = next_weight, a.run = run, a.scale = scale, a.eps = eps;
+    a.layer = kind == RTN_NORM_LAYER, a.f16 = dt == RTN_F16;
+    const rtn::NormGrads g = {dweight, dbias, dgate, dnext_weight, dnext_bias, bias};
+    const hipError_t e = rtn::launch_norm_backward(a, g, (float*)workspace, (hipStream_t)stream);
     return e == hipSuccess ? RTN_OK : hip_fail(e);
 }
 

@@ -318,4 +318,91 @@ struct LinearBwdArgs {
 size_t linear_backward_workspace(int64_t M, int64_t N, int64_t K);
 hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t st);
 
+// Microscaled 4-bit values (layout: mx4_math.h).  type: 0 bfloat16, 1 float16, 2 float32.
+struct Mx4PackArgs {
+    const void* x;         // [R][C], row pitch ldx elements
+    int64_t R, C, ldx, ldz;
+    void* out;             // nullable: groups along the rows
+    void* out_t;           // nullable: of the transposed matrix, [C][R]
+    const uint64_t* seed;  // nullable (to nearest): of the stochastic rounding
+    const void* z;         // with an activation: x is multiplied by its slope at z [R][C]
+    float* part;           // nullable: sums of the columns over runs of rows, [mx4_sum_runs][C]
+    int type, act;
+    int64_t per;           // set by launch_mx4_pack
+};
+hipError_t launch_mx4_pack(Mx4PackArgs a, hipStream_t st);
+int64_t mx4_sum_runs(int64_t R, int64_t C);
+hipError_t launch_mx4_sums(const float* part, int64_t R, int64_t C, void* out, int f16, hipStream_t st);
+struct Mx4UnpackArgs {
+    const void* packed;
+    int64_t R, C, ldy;
+    void* y;
+    int type;
+};
+hipError_t launch_mx4_unpack(const Mx4UnpackArgs& a, hipStream_t st);
+
+// y[m][n] = act(sum_k a[m][k] w[n][k] + bias[n]) + residual[m][n]
+struct Mx4LinArgs {
+    const void* x;     // [M][K] 16 bit, row pitch ldx, packed on the way; or
+    const void* a;     // the packed form (x is not read)
+    const void* w;     // packed [N][K]
+    int64_t M, N, K, ldx, ldr, ldy, ldz;
+    const void *bias, *res;  // nullable, 16 bit
+    void* y;
+    void* z;           // nullable, 16 bit: the value before the activation
+    int act, f16, y_f32;
+    void* workspace;   // x packed, where the form needs that (mx4_packs_x)
+};
+bool mx4_packs_x(int64_t M, int64_t N, int64_t K);
+hipError_t launch_mx4_linear(const Mx4LinArgs& a, hipStream_t st);
+
+struct Mx4BwdArgs {
+    const void *dy, *z, *wt, *xt;  // dy, z [M][N] 16 bit; packed [K][N] and [K][M]
+    int64_t M, N, K, lddy, ldz, lddx;
+    const uint64_t* seed;
+    int act, f16, dw_f32;
+    void *dx, *dw, *dbias;  // each nullable
+    char* workspace;
+};
+size_t mx4_backward_workspace(int64_t M, int64_t N, int64_t K);
+hipError_t launch_mx4_backward(const Mx4BwdArgs& a, hipStream_t st);
+
+// Norms around a block: y = scale x + gate (n(h) weight + bias), u = n(y) next_weight + next_bias (norm.hip)
+struct NormArgs {
+    const void *h, *x;  // [M][C] 16 bit; h NULL: y is x
+    void *y, *u;        // u NULL: not wanted
+    int64_t M, C, ldh, ldx, ldy, ldu;
+    const float *weight, *bias, *gate, *next_weight, *next_bias;  // [C]; gate [ceil(M / run)][C]; all nullable
+    int64_t run;        // consecutive rows that share a row of the gate
+    float scale, eps;
+    int layer, f16;
+    int64_t rows;       // set by launch_norm: of a unit
+};
+hipError_t launch_norm(const NormArgs& a, hipStream_t st);
+struct NormBackArgs {
+    const void *dy, *du, *h, *y;  // dy nullable; h NULL: without the first line, du NULL: without the second
+    void *dh, *dx;                // each nullable
+    int64_t M, C, lddy, lddu, ldh, ldy, lddh, lddx;
+    const float *weight, *gate, *next_weight;
+    int64_t run;
+    float scale, eps;
+    int layer, f16;
+    // set by launch_norm_backward: rows of the gate, units of each and their rows, the units' sums
+    int64_t owners, parts, rows;
+    float* part[4];
+};
+struct NormGrads {  // each nullable
+    float *dweight, *dbias, *dgate, *dnext_weight, *dnext_bias;
+    const float* bias;  // of the first line, for dgate
+};
+struct NormSumArgs {
+    const float* part[4];
+    float* out[4];
+    const float *weight, *bias, *gate;
+    float* dgate;
+    int64_t C, owners, parts;
+};
+size_t norm_backward_workspace(int64_t M, int64_t C, int64_t run);
+hipError_t launch_norm_backward(NormBackArgs a, const NormGrads& g, float* workspace, hipStream_t st);
+
 }  // namespace rtn

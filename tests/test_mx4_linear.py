@@ -32,6 +32,20 @@ def test_forward(dtype, M, N, K, act):
     T.assert_within(z, zw, L.rounded(zw, ez), "z")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("M,N,K", [(1800, 1747, 100), (1797, 1800, 900), (3500, 3393, 70), (3489, 3500, 1100), (3490, 3400, 640), (257, 30000, 300),
+                                   (40000, 200, 390)])
+def test_tiles(dtype, M, N, K):
+    """Grids that fill the chip: tiles that end inside the matrix, from one block of columns to more than the ring holds."""
+    L = Q.Layer(dtype, M, N, K, seed=K)
+    w, z = B.mx4_pack(L.w), torch.empty((M, N), dtype=L.type, device=Q.DEV)
+    y = B.mx4_linear(L.x, w, N, bias=L.bias, act=T.ACTS["gelu"], residual=L.res, z_out=z)
+    want, e = L.y64("gelu")
+    T.assert_within(y, want, L.rounded(want, e), "y")
+    zw, ez = L.z64()
+    T.assert_within(z, zw, L.rounded(zw, ez), "z")
+
+
 @pytest.mark.parametrize("act", ["relu", "silu"])
 @pytest.mark.parametrize("M,N,K", [(1, 48, 300), (40, 130, 300), (300, 520, 260)])
 @pytest.mark.parametrize("bias,residual", [(False, False), (True, False), (False, True)])

@@ -316,4 +316,37 @@ inline int64_t grad_blocks_per_run(int64_t M, int64_t N)
     return units >= 8 * 8192 ? 8 : units >= 2 * 8192 ? 2 : 1;
 }
 
+// The product of packed 4-bit matrices (mx4_linear.hip): M tokens of K columns against N outputs.  Up to 16 tokens that are not packed yet
+// have a kernel of their own that packs them.  Forms: blocks of 16 to 64 tokens x 16 to 64 outputs whose waves share the columns and load
+// straight into registers (kSplit..), tiles through LDS.
+//
+// The split forms are bound by the latency of their loads while every block has a CU to itself: the smallest blocks that the 256 CUs
+// hold at once.  Over many columns the larger blocks, which load less, win before the CUs are full.  us, at 4096 columns unless said:
+//                        16x16  16x32  32x32  32x64  64x64  64x64 of 4 waves  128x128  128x256
+//     16 x 4096            3.5    3.6    4.0    4.7    5.7    6.7
+//     24 x 8192 (8192)    14.7   12.9    6.9    8.1    9.3   11.1
+//     64 x 1024 (1024)     2.9    2.8    2.9    3.4    4.4    5.2                6.5      8.8
+//     64 x 4096            8.1    7.6    4.3    5.6    6.1    7.5               12.8     18.2
+//    128 x 4096           15.1   14.8    8.2    6.3    7.0    8.2               12.9     18.4
+//    128 x 8192 (8192)    41.1   40.8   24.0   24.2   14.2   14.8               21.8     30.8
+//    256 x 8192 (8192)    56.4   45.3   41.7   45.8   26.4   24.8               22.4     31.5
+//   2048 x 1024 (1024)                   9.3   10.3    8.7    6.9                7.1      9.5
+//   2048 x 1003 (2187)                  12.2   12.8   10.2    9.1               11.7     17.6
+//   1000 x 4096                         30.1   33.4   26.7   23.2               16.6     22.4
+//   2048 x 4096                                                                 24.0     24.2
+//   4096 x 4096                                       85.1   67.4               43.3     39.3
+enum class Mx4Form { kSplit16, kSplit16x32, kSplit32, kSplit32x64, kSplit64, kSplit64x4, kTile128, kTile256 };
+constexpr int kMx4FewTokens = 16;
+inline Mx4Form mx4_form(int64_t M, int64_t N, int64_t K)
+{
+    auto blocks = [&](int64_t m, int64_t n) { return ((M + m - 1) / m) * ((N + n - 1) / n); };
+    if (blocks(16, 16) <= 256) return Mx4Form::kSplit16;
+    if (M <= 16 || blocks(16, 32) <= 256) return Mx4Form::kSplit16x32;
+    if (blocks(32, 32) <= 256) return Mx4Form::kSplit32;
+    if (K <= 4096 && blocks(32, 64) <= 256) return Mx4Form::kSplit32x64;
+    if (blocks(64, 64) <= 256) return Mx4Form::kSplit64;
+    if (K <= 2560 && blocks(64, 64) <= 512) return Mx4Form::kSplit64x4;
+    return blocks(128, 128) <= 512 ? Mx4Form::kTile128 : Mx4Form::kTile256;
+}
+
 }  // namespace rtn

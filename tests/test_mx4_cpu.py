@@ -1,6 +1,8 @@
 """What the entry points of the microscaled 4-bit operators and of the norms refuse, on a host without a GPU: every check comes before
 any launch."""
 import ctypes as C
+import os
+import subprocess
 
 import numpy as np
 import pytest
@@ -113,3 +115,20 @@ def test_the_binding_takes_device_tensors_only(call):
     import torch
     with pytest.raises(AssertionError):
         call(torch.zeros((4, 4), dtype=torch.bfloat16))
+
+
+def test_sizes_of_the_tests_reach_every_form(tmp_path):
+    """Every form of the product, and tiles with edges inside, over fewer, as many and more steps of 128 columns than their ring holds."""
+    import test_mx4_linear as G
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_1912_02057_amd", "csrc")
+    (tmp_path / "r.cpp").write_text("""#include "choice.h"
+extern "C" int form(int64_t M, int64_t N, int64_t K) { return (int)rtn::mx4_form(M, N, K); }
+""")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I" + csrc, str(tmp_path / "r.cpp"), "-o", str(tmp_path / "r.so")], check=True)
+    form = C.CDLL(str(tmp_path / "r.so")).form
+    form.argtypes = [C.c_int64] * 3
+    sizes = G.SIZES + G.TILES
+    assert {form(*s) for s in sizes} == set(range(8))
+    for f, ring in ((6, 4), (7, 3)):
+        steps = [-(-K // 128) for M, N, K in sizes if form(M, N, K) == f]
+        assert min(steps) == 1 and max(steps) > ring + 1 and any(M % 128 and N % 128 for M, N, K in sizes if form(M, N, K) == f), (f, steps)

@@ -11,8 +11,13 @@ import mx4_testlib as Q
 pytestmark = pytest.mark.gpu
 
 # (M, N, K): one token, a few, many; sizes around the tiles' and the blocks'
-SIZES = [(1, 1, 1), (1, 48, 4096), (1, 4096, 130), (2, 33, 31), (5, 100, 257), (15, 64, 128), (16, 70, 500), (17, 16, 129), (24, 300, 1000),
-         (33, 65, 96), (64, 64, 640), (100, 130, 2187), (129, 257, 300), (256, 1024, 128), (300, 515, 77), (513, 769, 1100)]
+SIZES = [(1, 1, 1), (1, 48, 4096), (1, 4096, 130), (2, 33, 31), (5, 100, 257), (15, 64, 128), (16, 70, 500), (3, 200, 4104), (16, 70, 520), (2, 5000, 904), (17, 16, 129), (24, 300, 1000),
+         (33, 65, 96), (64, 64, 640), (100, 130, 2187), (129, 257, 300), (256, 1024, 128), (300, 515, 77), (513, 769, 1100), (130, 2050, 700),
+         (1000, 1003, 900), (1, 9000, 140)]
+# tiles that end inside the matrix, from one block of columns to more than the ring holds
+TILES = [(1800, 1747, 100), (1797, 1800, 900), (3500, 3393, 70), (3489, 3500, 1100), (3490, 3400, 390), (257, 30000, 300), (40000, 200, 390),
+         (1700, 1300, 3000), (1290, 1030, 2700), (700, 3300, 1030), (1030, 1290, 2600),
+         (1290, 1030, 100), (2900, 2900, 70)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
@@ -33,8 +38,7 @@ def test_forward(dtype, M, N, K, act):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
-@pytest.mark.parametrize("M,N,K", [(1800, 1747, 100), (1797, 1800, 900), (3500, 3393, 70), (3489, 3500, 1100), (3490, 3400, 640), (257, 30000, 300),
-                                   (40000, 200, 390)])
+@pytest.mark.parametrize("M,N,K", TILES)
 def test_tiles(dtype, M, N, K):
     """Grids that fill the chip: tiles that end inside the matrix, from one block of columns to more than the ring holds."""
     L = Q.Layer(dtype, M, N, K, seed=K)

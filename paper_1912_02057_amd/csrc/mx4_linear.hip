@@ -713,7 +713,7 @@ hipError_t launch_mx4_linear(const Mx4LinArgs& a, hipStream_t st)
 size_t mx4_backward_workspace(int64_t M, int64_t N, int64_t)
 {
     if (M == 0) return 0;
-    return (size_t)(up256(Mx4Shape(M, N).bytes()) + up256(Mx4Shape(N, M).bytes()) + mx4_sum_runs(M, N) * N * 4);
+    return (size_t)(up256(Mx4Shape(M, N).bytes()) + up256(Mx4Shape(N, M).bytes()) + mx4_sum_runs(M) * N * 4);
 }
 
 hipError_t launch_mx4_backward(const Mx4BwdArgs& a, hipStream_t st)

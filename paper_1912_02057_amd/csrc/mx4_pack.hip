@@ -14,15 +14,37 @@ __device__ __forceinline__ unsigned quad_larger(unsigned a)
 }
 __device__ __forceinline__ unsigned largest8(const float (&v)[8])
 {
-    unsigned a = magnitude(v[0]);
+    Largest a;
 #pragma unroll
-    for (int i = 1; i < 8; ++i) a = larger(a, magnitude(v[i]));
-    return a;
+    for (int i = 0; i < 8; i += 2) a.take(v[i], v[i + 1]);
+    return a.bits();
+}
+
+// Eight values that are all there
+template <class T>
+__device__ __forceinline__ void load_whole(const char* p, float (&v)[8])
+{
+    if constexpr (std::is_same_v<T, F32>) {
+        __builtin_memcpy(v, p, 32);
+    } else {
+        const u32x4 q = load16(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = half_of<T>(q[i >> 1], i & 1);
+    }
+}
+
+template <class T>
+__device__ __forceinline__ float load_one(const void* p, int64_t i)
+{
+    if constexpr (std::is_same_v<T, F32>)
+        return ((const float*)p)[i];
+    else
+        return T::to_float(((const unsigned short*)p)[i]);
 }
 
 // Along the rows alone.  A block has 64 rows x 128 columns, a wave 16 rows, a lane 8 columns of a row: four lanes have a group, 16 read
 // 256 bytes of a row (of 16-bit values), and the maximum is over a quad of lanes.
-template <class T>
+template <class T, bool RANDOM>
 __global__ __launch_bounds__(256) void k_mx4_rows(Mx4PackArgs a)
 {
     __shared__ unsigned scales[64];
@@ -30,11 +52,18 @@ __global__ __launch_bounds__(256) void k_mx4_rows(Mx4PackArgs a)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, p = lane & 3, g = (lane >> 2) & 3;
     const int64_t kb = (int64_t)blockIdx.x % s.kb, rg = (int64_t)blockIdx.x / s.kb, rb = rg * 4 + wave;
     const int64_t c = kb * 128 + g * 32 + p * 8, groups = (a.C + 31) / 32;
-    const uint64_t seed = a.seed ? *a.seed : 0;
+    const uint64_t seed = RANDOM ? *a.seed : 0;
     float v[4][8];
+    const bool whole = kb * 128 + 128 <= a.C && rg * 64 + 64 <= a.R;
+    if (whole) {
+        const char* x = (const char*)a.x + ((rb * 16 + (lane >> 4)) * a.ldx + c) * kBytesOf<T>;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_whole<T>(x + i * 4 * a.ldx * kBytesOf<T>, v[i]);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int64_t r = rb * 16 + i * 4 + (lane >> 4);
+        if (whole) break;
         if (r < a.R) {
             load_values<T>((const char*)a.x + r * a.ldx * kBytesOf<T>, c, a.C, v[i]);
         } else {
@@ -44,9 +73,9 @@ __global__ __launch_bounds__(256) void k_mx4_rows(Mx4PackArgs a)
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int row = i * 4 + (lane >> 4), e = mx4_scale(quad_larger(largest8(v[i])), a.seed != nullptr);
+        const int row = i * 4 + (lane >> 4), e = mx4_scale(quad_larger(largest8(v[i])), RANDOM);
         const Mx4Random rnd = {seed, (uint64_t)((rb * 16 + row) * groups + kb * 4 + g), 0};
-        const unsigned q = a.seed ? mx4_stochastic(v[i], e, rnd.bits(p)) : mx4_nearest(v[i], e);
+        const unsigned q = RANDOM ? mx4_stochastic(v[i], e, rnd.bits(p)) : mx4_nearest(v[i], e);
         if (rb < s.rb) *(unsigned*)((char*)a.out + (rb * s.kb + kb) * 1024 + (row + 16 * g) * 16 + p * 4) = q;
         if (p == 0) ((unsigned char*)scales)[(row + 16 * g) * 4 + wave] = (unsigned char)e;
     }
@@ -69,98 +98,120 @@ __device__ __forceinline__ float exact_slope(float z)
     }
 }
 
-// Along the rows and along the columns.  A block has 128 rows x 128 columns, 64 rows at a time: the rows' groups as above, straight from
-// the registers; the columns' through LDS as fp32, after which a lane has one group of 32 rows.  Both scales are whole 256-byte
-// pieces.  The sums of the columns (the bias gradient) come on the way; a block then has `per` tiles below each other.
-template <class T, int ACT>
-__global__ __launch_bounds__(256) void k_mx4_both(Mx4PackArgs a)
+// Along the rows and along the columns.  A block has 64 rows x 64 columns: the rows' groups as above, straight from the registers; the
+// columns' through LDS as fp32, after which a lane has one group of 32 rows.  Two blocks beside or below each other fill a piece of
+// 1 KiB of codes and 256 bytes of scales, each in whole 128-byte lines; the last of an odd number fills its neighbour's half with zeros.
+// The sums of the columns (the bias gradient) come on the way, 64 rows each.
+template <class T, int ACT, bool RANDOM>
+__global__ __launch_bounds__(128, 4) void k_mx4_both(Mx4PackArgs a)
 {
-    __shared__ __attribute__((aligned(16))) float tile[64][128];
-    __shared__ unsigned srow[2][64], scol[2][64];
-    __shared__ float sums[128];
+    __shared__ __attribute__((aligned(16))) float tile[64][64];
+    __shared__ unsigned srow[32], scol[32];
+    __shared__ float sums[64];
     const Mx4Shape s(a.R, a.C), st(a.C, a.R);
-    const int tid = threadIdx.x, p = tid & 3, g = (tid >> 2) & 3, rr = tid >> 4, tc = tid & 127, half = tid >> 7;
-    const int64_t cbs = s.kb, cb = (int64_t)blockIdx.x % cbs, run = (int64_t)blockIdx.x / cbs;
-    const int64_t c = cb * 128 + (tid & 15) * 8, groups = (a.C + 31) / 32, groups_t = (a.R + 31) / 32;
-    const uint64_t seed = a.seed ? *a.seed : 0;
-    float sum = 0.f;
-    for (int64_t tb = run * a.per; tb < (run + 1) * a.per && tb < st.kb; ++tb) {
-#pragma unroll 1
-        for (int sub = 0; sub < 2; ++sub) {
-            const int64_t row0 = tb * 128 + sub * 64;
-            float v[4][8];
+    const unsigned tid = threadIdx.x, p = tid & 3, g = (tid >> 2) & 1, rr = tid >> 3, c8 = (tid & 7) * 8, tc = tid & 63, half = tid >> 6;
+    const unsigned cbs = (unsigned)((a.C + 63) / 64), rbs = (unsigned)((a.R + 63) / 64), tb = blockIdx.x / cbs, cb = blockIdx.x - tb * cbs;
+    const uint64_t seed = RANDOM ? *a.seed : 0;
+    float v[4][8];
+    if (cb * 64 + 64 <= a.C && tb * 64 + 64 <= a.R) {
+        const char* x = (const char*)a.x + (((int64_t)tb * 64 + rr) * a.ldx + cb * 64 + c8) * kBytesOf<T>;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_whole<T>(x + i * 16 * a.ldx * kBytesOf<T>, v[i]);
+        if constexpr (ACT != kActNone) {
+            const char* zs = (const char*)a.z + (((int64_t)tb * 64 + rr) * a.ldz + cb * 64 + c8) * kBytesOf<T>;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int64_t r = row0 + i * 16 + rr;
-                if (r < a.R) {
-                    load_values<T>((const char*)a.x + r * a.ldx * kBytesOf<T>, c, a.C, v[i]);
-                    if constexpr (ACT != kActNone) {
-                        float z[8];
-                        load_values<T>((const char*)a.z + r * a.ldz * kBytesOf<T>, c, a.C, z);
+                float z[8];
+                load_whole<T>(zs + i * 16 * a.ldz * kBytesOf<T>, z);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[i][e] = c + e < a.C ? v[i][e] * exact_slope<ACT>(z[e]) : 0.f;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
-                }
+                for (int e = 0; e < 8; ++e) v[i][e] *= exact_slope<ACT>(z[e]);
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float4* t = (float4*)&tile[i * 16 + rr][(tid & 15) * 8];
-                t[0] = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]), t[1] = make_float4(v[i][4], v[i][5], v[i][6], v[i][7]);
-            }
-            if (a.out) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int64_t rb = row0 / 16 + i;
-                    const int e = mx4_scale(quad_larger(largest8(v[i])), a.seed != nullptr);
-                    const Mx4Random rnd = {seed, (uint64_t)((rb * 16 + rr) * groups + cb * 4 + g), 0};
-                    const unsigned q = a.seed ? mx4_stochastic(v[i], e, rnd.bits(p)) : mx4_nearest(v[i], e);
-                    if (rb < s.rb) *(unsigned*)((char*)a.out + (rb * s.kb + cb) * 1024 + (rr + 16 * g) * 16 + p * 4) = q;
-                    if (p == 0) ((unsigned char*)srow[sub])[(rr + 16 * g) * 4 + i] = (unsigned char)e;
-                }
-            }
-            __syncthreads();
-            if (a.out_t || a.part) {
-                float w[32];
-                unsigned m = 0;
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    w[i] = tile[half * 32 + i][tc];
-                    m = larger(m, magnitude(w[i]));
-                }
-                if (a.part) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) sum += w[i];
-                }
-                if (a.out_t) {
-                    const int e = mx4_scale(m, a.seed != nullptr), gt = sub * 2 + half;
-                    const Mx4Random rnd = {seed, (uint64_t)((cb * 128 + tc) * groups_t + tb * 4 + gt), 1};
-                    unsigned q[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) q[j] = a.seed ? mx4_stochastic(w + 8 * j, e, rnd.bits(j)) : mx4_nearest(w + 8 * j, e);
-                    const int64_t b = cb * 8 + (tc >> 4);
-                    if (b < st.rb) *(uint4*)((char*)a.out_t + (b * st.kb + tb) * 1024 + ((tc & 15) + 16 * gt) * 16) = make_uint4(q[0], q[1], q[2], q[3]);
-                    ((unsigned char*)scol[tc >> 6])[((tc & 15) + 16 * gt) * 4 + ((tc >> 4) & 3)] = (unsigned char)e;
-                }
-            }
-            __syncthreads();
         }
-        const int which = (tid >> 6) & 1, l = tid & 63;
-        if (tid < 128) {
-            const int64_t rg = tb * 2 + which;
-            if (a.out && rg < s.rg) *(unsigned*)((char*)a.out + s.codes() + (rg * s.kb + cb) * 256 + l * 4) = srow[which][l];
-        } else {
-            const int64_t rg = cb * 2 + which;
-            if (a.out_t && rg < st.rg) *(unsigned*)((char*)a.out_t + st.codes() + (rg * st.kb + tb) * 256 + l * 4) = scol[which][l];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float4* t = (float4*)&tile[i * 16 + rr][c8];
+            t[0] = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]), t[1] = make_float4(v[i][4], v[i][5], v[i][6], v[i][7]);
         }
-        // (the next tile's scales are written behind a barrier that these reads come before)
-    }
-    if (a.part) {
-        if (half) sums[tc] = sum;
         __syncthreads();
-        if (!half && cb * 128 + tc < a.C) a.part[run * a.C + cb * 128 + tc] = sum + sums[tc];
+    } else {  // at the matrix' ends: through LDS one by one
+#pragma unroll 1
+        for (unsigned i = half; i < 64; i += 2) {
+            const int64_t r = (int64_t)tb * 64 + i, c = (int64_t)cb * 64 + tc;
+            float f = 0.f;
+            if (r < a.R && c < a.C) {
+                f = load_one<T>(a.x, r * a.ldx + c);
+                if constexpr (ACT != kActNone) f *= exact_slope<ACT>(load_one<T>(a.z, r * a.ldz + c));
+            }
+            tile[i][tc] = f;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4* t = (const float4*)&tile[i * 16 + rr][c8];
+            const float4 l = t[0], h = t[1];
+            v[i][0] = l.x, v[i][1] = l.y, v[i][2] = l.z, v[i][3] = l.w, v[i][4] = h.x, v[i][5] = h.y, v[i][6] = h.z, v[i][7] = h.w;
+        }
+    }
+    if (a.out) {
+        const unsigned gr = (cb & 1) * 2 + g;  // the group in its block of 128 columns
+        char* out = (char*)a.out + (tb * 4 * s.kb + (cb >> 1)) * 1024;
+        uint64_t group = ((uint64_t)tb * 64 + rr) * (uint64_t)((a.C + 31) / 32) + cb * 2 + g;
+#pragma unroll
+        for (unsigned i = 0; i < 4; ++i) {
+            const int e = mx4_scale(quad_larger(largest8(v[i])), RANDOM);
+            const Mx4Random rnd = {seed, group, 0};
+            const unsigned q = RANDOM ? mx4_stochastic(v[i], e, rnd.bits((int)p)) : mx4_nearest(v[i], e);
+            if (tb * 4 + i < s.rb) *(unsigned*)(out + i * s.kb * 1024 + ((rr + 16 * gr) * 16 + p * 4)) = q;
+            if (p == 0) ((unsigned char*)srow)[(rr + 16 * g) * 4 + i] = (unsigned char)e;
+            group += 16 * (uint64_t)((a.C + 31) / 32);
+        }
+    }
+    const unsigned kt = tb >> 1;  // the block of 128 rows
+    if (a.out_t || a.part) {
+        float w[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) w[i] = tile[half * 32 + i][tc];
+        if (a.part) {
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) sum += w[i];
+            if (half) sums[tc] = sum;
+            __syncthreads();
+            if (!half && cb * 64 + tc < a.C) a.part[tb * a.C + cb * 64 + tc] = sum + sums[tc];
+        }
+        if (a.out_t) {
+            Largest m;
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) m.take(w[i], w[i + 1]);
+            const int e = mx4_scale(m.bits(), RANDOM);
+            const unsigned gt = (tb & 1) * 2 + half, b = cb * 4 + (tc >> 4);
+            const Mx4Random rnd = {seed, ((uint64_t)cb * 64 + tc) * (uint64_t)((a.R + 31) / 32) + tb * 2 + half, 1};
+            unsigned q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[j] = RANDOM ? mx4_stochastic(w + 8 * j, e, rnd.bits(j)) : mx4_nearest(w + 8 * j, e);
+            if (b < st.rb) *(uint4*)((char*)a.out_t + (b * st.kb + kt) * 1024 + ((tc & 15) + 16 * gt) * 16) = make_uint4(q[0], q[1], q[2], q[3]);
+            ((unsigned char*)scol)[((tc & 15) + 16 * half) * 4 + (tc >> 4)] = (unsigned char)e;
+        }
+    }
+    __syncthreads();
+    const unsigned l = tid & 31, i = tid >> 5;
+    // the second half of a block of 128 columns or rows that has none: codes and scales of groups that are not there
+    const bool lone_c = cb == cbs - 1 && !(cb & 1), lone_r = tb == rbs - 1 && !(tb & 1);
+    if (a.out) {
+        unsigned* scales = (unsigned*)((char*)a.out + s.codes() + (tb * s.kb + (cb >> 1)) * 256) + l;
+        if (i == 0) scales[(cb & 1) * 32] = srow[l];
+        if (lone_c) {
+            if (i == 1) scales[32] = 0;
+            if (tb * 4 + i < s.rb) *(uint4*)((char*)a.out + ((tb * 4 + i) * s.kb + (cb >> 1)) * 1024 + 512 + l * 16) = make_uint4(0, 0, 0, 0);
+        }
+    }
+    if (a.out_t) {
+        unsigned* scales = (unsigned*)((char*)a.out_t + st.codes() + (cb * st.kb + kt) * 256) + l;
+        if (i == 2) scales[(tb & 1) * 32] = scol[l];
+        if (lone_r) {
+            if (i == 3) scales[32] = 0;
+            if (cb * 4 + i < st.rb) *(uint4*)((char*)a.out_t + ((cb * 4 + i) * st.kb + kt) * 1024 + 512 + l * 16) = make_uint4(0, 0, 0, 0);
+        }
     }
 }
 
@@ -210,61 +261,67 @@ __global__ __launch_bounds__(256) void k_mx4_unpack(Mx4UnpackArgs a)
     }
 }
 
-// out[c] = sum over runs of part[run][c], in their order
+// out[c] = sum over runs of part[run][c]: 64 columns a block, its 16 waves share the runs
 template <class T>
-__global__ __launch_bounds__(256) void k_mx4_sums(const float* part, int64_t runs, int64_t C, unsigned short* out)
+__global__ __launch_bounds__(1024) void k_mx4_sums(const float* part, int64_t runs, int64_t C, unsigned short* out)
 {
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c >= C) return;
+    __shared__ float lds[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
     float s = 0.f;
-    for (int64_t r = 0; r < runs; ++r) s += part[r * C + c];
+    if (c < C)
+        for (int64_t r = wave; r < runs; r += 16) s += part[r * C + c];
+    lds[wave][lane] = s;
+    __syncthreads();
+    if (wave || c >= C) return;
+    for (int v = 1; v < 16; ++v) s += lds[v][lane];
     out[c] = T::from_float(s);
 }
 
 template <class T>
+hipError_t run_rows(const Mx4PackArgs& a, unsigned grid, hipStream_t st)
+{
+    if (a.seed)
+        k_mx4_rows<T, true><<<grid, 256, 0, st>>>(a);
+    else
+        k_mx4_rows<T, false><<<grid, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+template <class T, int ACT>
+hipError_t run_both(const Mx4PackArgs& a, unsigned grid, hipStream_t st)
+{
+    if (a.seed)
+        k_mx4_both<T, ACT, true><<<grid, 128, 0, st>>>(a);
+    else
+        k_mx4_both<T, ACT, false><<<grid, 128, 0, st>>>(a);
+    return hipGetLastError();
+}
+template <class T>
 hipError_t run_both(const Mx4PackArgs& a, unsigned grid, hipStream_t st)
 {
     switch (a.act) {
-        case kActNone: k_mx4_both<T, kActNone><<<grid, 256, 0, st>>>(a); break;
-        case kActRelu: k_mx4_both<T, kActRelu><<<grid, 256, 0, st>>>(a); break;
-        case kActGelu: k_mx4_both<T, kActGelu><<<grid, 256, 0, st>>>(a); break;
-        default: k_mx4_both<T, kActSilu><<<grid, 256, 0, st>>>(a); break;
+        case kActNone: return run_both<T, kActNone>(a, grid, st);
+        case kActRelu: return run_both<T, kActRelu>(a, grid, st);
+        case kActGelu: return run_both<T, kActGelu>(a, grid, st);
+        default: return run_both<T, kActSilu>(a, grid, st);
     }
-    return hipGetLastError();
 }
 
 }  // namespace
 
-// Tiles below each other of a block that forms the sums of its columns: few enough partial sums (4 bytes for every 256 or more of the values)
-// while the blocks fill the chip.
-int64_t mx4_sum_tiles(int64_t R, int64_t C)
-{
-    const int64_t tiles = (R + 127) / 128 * ((C + 127) / 128), per = tiles / 2048;
-    return per < 1 ? 1 : per > 8 ? 8 : per;
-}
-int64_t mx4_sum_runs(int64_t R, int64_t C) { return ((R + 127) / 128 + mx4_sum_tiles(R, C) - 1) / mx4_sum_tiles(R, C); }
+int64_t mx4_sum_runs(int64_t R) { return (R + 63) / 64; }
 
-hipError_t launch_mx4_pack(Mx4PackArgs a, hipStream_t st)
+hipError_t launch_mx4_pack(const Mx4PackArgs& a, hipStream_t st)
 {
     const Mx4Shape s(a.R, a.C);
     if (!a.out_t && !a.part && a.act == kActNone) {
         const int64_t n = s.rg * s.kb;
         if (n > 0x7fffffff) return hipErrorInvalidValue;
-        if (a.type == 2)
-            k_mx4_rows<F32><<<(unsigned)n, 256, 0, st>>>(a);
-        else if (a.type == 1)
-            k_mx4_rows<F16><<<(unsigned)n, 256, 0, st>>>(a);
-        else
-            k_mx4_rows<BF16><<<(unsigned)n, 256, 0, st>>>(a);
-        return hipGetLastError();
+        return a.type == 2 ? run_rows<F32>(a, (unsigned)n, st) : a.type == 1 ? run_rows<F16>(a, (unsigned)n, st) : run_rows<BF16>(a, (unsigned)n, st);
     }
-    a.per = a.part ? mx4_sum_tiles(a.R, a.C) : 1;
-    const int64_t n = s.kb * (((a.R + 127) / 128 + a.per - 1) / a.per);
+    const int64_t n = (a.C + 63) / 64 * ((a.R + 63) / 64);
     if (n > 0x7fffffff) return hipErrorInvalidValue;
-    if (a.type == 2) {
-        k_mx4_both<F32, kActNone><<<(unsigned)n, 256, 0, st>>>(a);
-        return hipGetLastError();
-    }
+    if (a.type == 2) return run_both<F32, kActNone>(a, (unsigned)n, st);
     return a.type == 1 ? run_both<F16>(a, (unsigned)n, st) : run_both<BF16>(a, (unsigned)n, st);
 }
 
@@ -284,11 +341,11 @@ hipError_t launch_mx4_unpack(const Mx4UnpackArgs& a, hipStream_t st)
 
 hipError_t launch_mx4_sums(const float* part, int64_t R, int64_t C, void* out, int f16, hipStream_t st)
 {
-    const unsigned grid = (unsigned)((C + 255) / 256);
+    const unsigned grid = (unsigned)((C + 63) / 64);
     if (f16)
-        k_mx4_sums<F16><<<grid, 256, 0, st>>>(part, mx4_sum_runs(R, C), C, (unsigned short*)out);
+        k_mx4_sums<F16><<<grid, 1024, 0, st>>>(part, mx4_sum_runs(R), C, (unsigned short*)out);
     else
-        k_mx4_sums<BF16><<<grid, 256, 0, st>>>(part, mx4_sum_runs(R, C), C, (unsigned short*)out);
+        k_mx4_sums<BF16><<<grid, 1024, 0, st>>>(part, mx4_sum_runs(R), C, (unsigned short*)out);
     return hipGetLastError();
 }
 

@@ -326,12 +326,11 @@ struct Mx4PackArgs {
     void* out_t;           // nullable: of the transposed matrix, [C][R]
     const uint64_t* seed;  // nullable (to nearest): of the stochastic rounding
     const void* z;         // with an activation: x is multiplied by its slope at z [R][C]
-    float* part;           // nullable: sums of the columns over runs of rows, [mx4_sum_runs][C]
+    float* part;           // nullable: sums of the columns over 64 rows each, [mx4_sum_runs][C]
     int type, act;
-    int64_t per;           // set by launch_mx4_pack
 };
-hipError_t launch_mx4_pack(Mx4PackArgs a, hipStream_t st);
-int64_t mx4_sum_runs(int64_t R, int64_t C);
+hipError_t launch_mx4_pack(const Mx4PackArgs& a, hipStream_t st);
+int64_t mx4_sum_runs(int64_t R);
 hipError_t launch_mx4_sums(const float* part, int64_t R, int64_t C, void* out, int f16, hipStream_t st);
 struct Mx4UnpackArgs {
     const void* packed;

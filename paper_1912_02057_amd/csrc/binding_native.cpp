@@ -532,9 +532,13 @@ PyObject* linear_backward(PyObject*, Args a, Py_ssize_t n)
 // Kernels run on torch's current stream, which belongs to the current device: tensors of another one would be read there.
 void on_current_device(Args a, Py_ssize_t n)
 {
+    int device = -1;
     for (Py_ssize_t i = 0; i < n; ++i)
-        if (THPVariable_Check(a[i]) && THPVariable_Unpack(a[i]).is_cuda() && THPVariable_Unpack(a[i]).get_device() != c10::hip::current_device())
+        if (THPVariable_Check(a[i]) && THPVariable_Unpack(a[i]).is_cuda()) {
+            if (device < 0) device = c10::hip::current_device();
+            if (THPVariable_Unpack(a[i]).get_device() == device) continue;
             fail(PyExc_ValueError, "%s: all tensors have to be on the current device", "device");
+        }
 }
 rtn_dtype any_dtype(const at::Tensor& t, const char* what) { return dtype(t.scalar_type(), what, true); }
 const uint64_t* seed_of(PyObject* o)

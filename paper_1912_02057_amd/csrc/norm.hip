@@ -66,18 +66,44 @@ template <int PER>
 struct Cols {
     float v[PER][8];
 };
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));  // of a vector that starts anywhere
 template <int W>
 __device__ __forceinline__ int64_t column(int j) { return (int64_t)(j * W * 64 + Unit<W>::lane()) * 8; }
+// A lane's part of a row.  Loaded without a branch, so that the loads of several rows are in flight together: pieces that the row does not fill
+// come from its last 16 bytes and are put right when they are used (settle).
 template <int W, int PER>
 struct Row {
     u32x4 q[PER];
     __device__ __forceinline__ void load(const void* base, int64_t ld, int64_t m, int64_t C)
     {
         const unsigned short* row = (const unsigned short*)base + m * ld;
+        if (C < 8) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) q[j] = load_row8(row, column<W>(j), C);
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             const int64_t k = column<W>(j);
-            q[j] = C % 8 ? load_row8(row, k, C) : k < C ? load16(row + k) : u32x4{0, 0, 0, 0};
+            q[j] = load16(row + (k < C - 8 ? k : C - 8));
+        }
+    }
+    __device__ __forceinline__ void settle(int64_t C)
+    {
+        if (C < 8) return;
+        if (C % 8 == 0) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+                if (column<W>(j) >= C) q[j] = u32x4{0, 0, 0, 0};
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int64_t over = column<W>(j) + 8 - C;  // elements that are not there
+            const int n = over <= 0 ? 0 : over < 8 ? (int)over * 16 : 128;
+            const uint64_t lo = q[j][0] | (uint64_t)q[j][1] << 32, hi = q[j][2] | (uint64_t)q[j][3] << 32;
+            const uint64_t l = n >= 64 ? hi >> (n & 63) : n ? lo >> n | hi << (64 - n) : lo, u = n >= 64 ? 0 : hi >> n;
+            q[j] = n == 128 ? u32x4{0, 0, 0, 0} : u32x4{(unsigned)l, (unsigned)(l >> 32), (unsigned)u, (unsigned)(u >> 32)};
         }
     }
     template <class T>
@@ -86,17 +112,29 @@ struct Row {
         return half_of<T>(q[j][i >> 1], i & 1);
     }
 };
-// A vector of the columns, or `otherwise` where it is NULL (and past the end: what is there reaches no sum and no output)
+// A vector of the columns, or `otherwise` where it is NULL.  Past the end are others of its entries, which reach no sum and no output.
 template <int W, int PER>
 __device__ __forceinline__ void load_cols(Cols<PER>& c, const float* p, int64_t C, float otherwise)
 {
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-        if (p) {
-            load_values<F32>(p, column<W>(j), C, c.v[j]);
-        } else {
+        const int64_t k = column<W>(j);
+        if (!p) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) c.v[j][i] = otherwise;
+        } else if (C < 8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c.v[j][i] = p[k + i < C ? k + i : C - 1];
+        } else {
+            const f32x4_any* q = (const f32x4_any*)(p + (k < C - 8 ? k : C - 8));
+            const f32x4_any a = q[0], b = q[1];
+            const int over = k < C && k > C - 8 ? (int)(k - (C - 8)) : 0;  // of the lane that has the row's end
+            const bool by4 = over & 4, by2 = over & 2, by1 = over & 1;
+            const f32x4_any a4 = by4 ? b : a, b4 = b;
+            const f32x4_any a2 = by2 ? f32x4_any{a4[2], a4[3], b4[0], b4[1]} : a4, b2 = by2 ? f32x4_any{b4[2], b4[3], b4[2], b4[3]} : b4;
+            const f32x4_any a1 = by1 ? f32x4_any{a2[1], a2[2], a2[3], b2[0]} : a2, b1 = by1 ? f32x4_any{b2[1], b2[2], b2[3], b2[3]} : b2;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c.v[j][i] = a1[i], c.v[j][4 + i] = b1[i];
         }
     }
 }
@@ -133,12 +171,18 @@ __device__ __forceinline__ void each(F f)
         for (int i = 0; i < 8; ++i) f(j, i);
 }
 
+// 1 / sqrt(v) within an ulp, also of numbers that the instruction takes as 0
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const bool small = v < 0x1p-96f;
+    return __builtin_amdgcn_rsqf(small ? v * 0x1p96f : v) * (small ? 0x1p48f : 1.f);
+}
 // K rows v -> n(v), and 1 / sqrt(..) of each.  A mean in fp32 is off by its sum's roundings, which a row of small variance divides by a small
 // number: what is left of it in the centred values is summed with their squares and taken off too.
 template <bool LAYER, int W, int PER, int K>
 __device__ __forceinline__ void normalise(Cols<PER> (&v)[K], float (&r)[K], int64_t C, float eps, float (*lds)[2][W], int& turn)
 {
-    const float n = (float)C;
+    const float inv = 1.f / (float)C;
     float s[K] = {}, rest[K] = {};
     if constexpr (LAYER) {
 #pragma unroll
@@ -147,12 +191,12 @@ __device__ __forceinline__ void normalise(Cols<PER> (&v)[K], float (&r)[K], int6
         float q[2] = {0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const float mean = s[k] / n;
+            const float mean = s[k] * inv;
             each<PER>([&](int j, int i) { v[k].v[j][i] = inside<W>(j, i, C) ? v[k].v[j][i] - mean : 0.f; });
             q[0] = q[1] = 0.f;
             each<PER>([&](int j, int i) { q[0] = fmaf(v[k].v[j][i], v[k].v[j][i], q[0]), q[1] += v[k].v[j][i]; });
             unit_sums<W, 2>(q, lds, turn);
-            rest[k] = q[1] / n;
+            rest[k] = q[1] * inv;
             s[k] = fmaf(-rest[k], q[1], q[0]);
             s[k] = s[k] < 0.f ? 0.f : s[k];  // (a NaN stays one)
         }
@@ -163,7 +207,7 @@ __device__ __forceinline__ void normalise(Cols<PER> (&v)[K], float (&r)[K], int6
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        r[k] = 1.f / sqrtf(s[k] / n + eps);
+        r[k] = inverse_root(fmaf(s[k], inv, eps));
         each<PER>([&](int j, int i) { v[k].v[j][i] = LAYER ? (v[k].v[j][i] - rest[k]) * r[k] : v[k].v[j][i] * r[k]; });
     }
 }
@@ -177,9 +221,9 @@ __device__ __forceinline__ void normalise_back(Cols<PER>& dn, const Cols<PER>& n
         if constexpr (LAYER) s[1] += dn.v[j][i];
     });
     unit_sums<W, LAYER ? 2 : 1>(s, lds, turn);
-    const float a = s[0] / (float)C * r;
+    const float inv = 1.f / (float)C, a = s[0] * inv * r;
     if constexpr (LAYER) {
-        const float b = s[1] / (float)C * r;
+        const float b = s[1] * inv * r;
         each<PER>([&](int j, int i) { dn.v[j][i] = fmaf(dn.v[j][i], r, -fmaf(n.v[j][i], a, b)); });
     } else {
         each<PER>([&](int j, int i) { dn.v[j][i] = fmaf(dn.v[j][i], r, -n.v[j][i] * a); });
@@ -188,7 +232,7 @@ __device__ __forceinline__ void normalise_back(Cols<PER>& dn, const Cols<PER>& n
 
 // POST: y = scale x + gate (n(h) weight + bias); without it y is x.  PRE: u = n(y) next_weight + next_bias.
 // The next row is fetched while this one is worked on: a block of 16 waves has its CU to itself, and a row's sums and barriers take as long as
-// its bytes (16384 x 8192: 260 us without, KEEP_NORM_US with).
+// its bytes (16384 x 8192, both lines: 260 us without, 200 with: 5.4 TB/s, the rate of a large copy).
 template <class T, bool LAYER, bool POST, bool PRE, int W, int PER>
 __global__ __launch_bounds__(Unit<W>::kThreads) void k_norm(NormArgs a)
 {
@@ -210,6 +254,8 @@ __global__ __launch_bounds__(Unit<W>::kThreads) void k_norm(NormArgs a)
         }
         Cols<PER> rows[1], &v = rows[0];
         float r[1];
+        x.settle(a.C);
+        if constexpr (POST) h.settle(a.C);
         if constexpr (POST) {
             if (m >= owner_end) {
                 owner = m / a.run, owner_end = (owner + 1) * a.run;
@@ -235,8 +281,9 @@ __global__ __launch_bounds__(Unit<W>::kThreads) void k_norm(NormArgs a)
 
 // With d the gradient of y, du's part among it:
 //   dx = scale d,  dh = n'(h) (d gate weight),  and per unit, for k_norm_sums: sum d n(h), sum d, sum du n(y), sum du
-// A unit's rows share a row of the gate.  BIASES: the second and fourth sum are wanted.  Rows are fetched ahead as above; with PER of 2 there
-// are no registers for that, and the vectors of the columns are read again for every row.
+// A unit's rows share a row of the gate.  BIASES: the second and fourth sum are wanted.  Rows are fetched ahead as above (16384 x 8192: 411 us
+// with loads that wait for each other, 320 in flight together: 5.0 TB/s); with PER of 2 there are no registers for that, and the vectors of
+// the columns are read again for every row (4096 x 16384: 415 us, 2.3 TB/s).
 template <class T, bool LAYER, bool POST, bool PRE, bool BIASES, int W, int PER>
 __global__ __launch_bounds__(Unit<W>::kThreads) void k_norm_back(NormBackArgs a)
 {
@@ -258,25 +305,25 @@ __global__ __launch_bounds__(Unit<W>::kThreads) void k_norm_back(NormBackArgs a)
     };
     if (KEEP && first < end) load(now, first);
     Cols<PER> gw, nw, sums[4];
-    auto vectors = [&] {
-        if constexpr (POST) {
-            Cols<PER> gate;
-            load_cols<W>(gw, a.weight, a.C, 1.f);
-            load_cols<W>(gate, a.gate ? a.gate + owner * a.C : nullptr, a.C, 1.f);
-            each<PER>([&](int j, int i) { gw.v[j][i] *= gate.v[j][i]; });
-        }
-        if constexpr (PRE) load_cols<W>(nw, a.next_weight, a.C, 1.f);
+    auto post_vectors = [&] {
+        Cols<PER> gate;
+        load_cols<W>(gw, a.weight, a.C, 1.f);
+        load_cols<W>(gate, a.gate ? a.gate + owner * a.C : nullptr, a.C, 1.f);
+        each<PER>([&](int j, int i) { gw.v[j][i] *= gate.v[j][i]; });
     };
-    if (KEEP) vectors();
+    if constexpr (KEEP && POST) post_vectors();
+    if constexpr (KEEP && PRE) load_cols<W>(nw, a.next_weight, a.C, 1.f);
 #pragma unroll
     for (int k = 0; k < 4; ++k) each<PER>([&](int j, int i) { sums[k].v[j][i] = 0.f; });
     for (int64_t m = first; m < end; ++m) {
         if (!KEEP) {
             load(now, m);
-            vectors();
         } else if (m + 1 < end) {
             load(next, m + 1);
         }
+        if (a.dy) now.dy.settle(a.C);
+        if constexpr (PRE) now.du.settle(a.C), now.y.settle(a.C);
+        if constexpr (POST) now.h.settle(a.C);
         constexpr int K = (POST ? 1 : 0) + (PRE ? 1 : 0);
         Cols<PER> d, n[K];  // n(h) first, n(y) last
         float r[K];
@@ -284,6 +331,7 @@ __global__ __launch_bounds__(Unit<W>::kThreads) void k_norm_back(NormBackArgs a)
         if constexpr (PRE) each<PER>([&](int j, int i) { n[K - 1].v[j][i] = now.y.template get<T>(j, i); });
         normalise<LAYER, W, PER, K>(n, r, a.C, a.eps, lds, turn);
         if constexpr (PRE) {
+            if (!KEEP) load_cols<W>(nw, a.next_weight, a.C, 1.f);
             each<PER>([&](int j, int i) {
                 const float g = now.du.template get<T>(j, i);
                 sums[2].v[j][i] = fmaf(g, n[K - 1].v[j][i], sums[2].v[j][i]);
@@ -301,6 +349,7 @@ __global__ __launch_bounds__(Unit<W>::kThreads) void k_norm_back(NormBackArgs a)
             store_row<T, W, PER>(a.dx, a.lddx, m, a.C, v);
         }
         if constexpr (POST) {
+            if (!KEEP) post_vectors();
             each<PER>([&](int j, int i) {
                 sums[0].v[j][i] = fmaf(d.v[j][i], n[0].v[j][i], sums[0].v[j][i]);
                 if (BIASES) sums[1].v[j][i] += d.v[j][i];
@@ -322,7 +371,9 @@ __global__ __launch_bounds__(Unit<W>::kThreads) void k_norm_back(NormBackArgs a)
             for (int j = 0; j < PER; ++j) {
                 const int64_t c = column<W>(j);
                 if (c + 8 <= a.C) {
-                    __builtin_memcpy(out + c, sums[k].v[j], 32);
+                    const float* v = sums[k].v[j];
+                    ((f32x4_any*)(out + c))[0] = f32x4_any{v[0], v[1], v[2], v[3]};
+                    ((f32x4_any*)(out + c))[1] = f32x4_any{v[4], v[5], v[6], v[7]};
                 } else {
 #pragma unroll
                     for (int i = 0; i < 7; ++i)
@@ -332,14 +383,15 @@ __global__ __launch_bounds__(Unit<W>::kThreads) void k_norm_back(NormBackArgs a)
         }
 }
 
-// The units' sums into the gradients of the vectors, in one order: 16 columns a block, its 16 groups of 16 lanes share the units of one owner (a
+// The units' sums into the gradients of the vectors, in one order: 16 columns a block, its SLICES groups of 16 lanes share the units of one owner (a
 // row of the gate), and blockIdx.y owners out of a.owners.  With S, T the first two sums over an owner's units:
 //   dgate = S weight + T bias,  dweight += gate S,  dbias += gate T
 // Several blocks of owners leave partial sums for a second launch.
-constexpr int kSumCols = 16, kSlices = 16;
-__global__ __launch_bounds__(256) void k_norm_sums(NormSumArgs a)
+constexpr int kSumCols = 16;
+template <int SLICES>
+__global__ __launch_bounds__(SLICES * 16) void k_norm_sums(NormSumArgs a)
 {
-    __shared__ float lds[4][kSlices][kSumCols + 1];
+    __shared__ float lds[4][SLICES][kSumCols + 1];
     const int col = threadIdx.x & 15, slice = threadIdx.x >> 4;
     const int64_t c = (int64_t)blockIdx.x * kSumCols + col, per = (a.owners + gridDim.y - 1) / gridDim.y;
     const int64_t o0 = blockIdx.y * per, o1 = o0 + per < a.owners ? o0 + per : a.owners;
@@ -353,7 +405,7 @@ __global__ __launch_bounds__(256) void k_norm_sums(NormSumArgs a)
             if (in && a.part[k]) {
                 const float* p = a.part[k] + o * a.parts * a.C + c;
 #pragma unroll 8
-                for (int64_t u = slice; u < a.parts; u += kSlices) s += p[u * a.C];
+                for (int64_t u = slice; u < a.parts; u += SLICES) s += p[u * a.C];
             }
             lds[k][slice][col] = s;
         }
@@ -361,7 +413,7 @@ __global__ __launch_bounds__(256) void k_norm_sums(NormSumArgs a)
         if (slice < 4) {  // slice k of 16 lanes adds up the k-th sum
             float s = 0.f;
 #pragma unroll
-            for (int v = 0; v < kSlices; ++v) s += lds[slice][v][col];
+            for (int v = 0; v < SLICES; ++v) s += lds[slice][v][col];
             lds[slice][0][col] = s;  // (each lane's own column)
         }
         __syncthreads();
@@ -404,7 +456,7 @@ hipError_t forward(NormArgs a, hipStream_t st)
 {
     return with_shape(a.C, [&](auto wi, auto pi) {
         constexpr int W = decltype(wi)::value, PER = decltype(pi)::value;
-        a.rows = (a.M + norm_units(a.C) - 1) / norm_units(a.C);
+        a.rows = (a.M + 2 * norm_units(a.C) - 1) / (2 * norm_units(a.C));  // (twice what the registers of the largest form allow)
         const int64_t units = (a.M + a.rows - 1) / a.rows;
         const unsigned grid = (unsigned)((units + Unit<W>::kRows - 1) / Unit<W>::kRows);
         if (a.h && a.u)
@@ -417,12 +469,12 @@ hipError_t forward(NormArgs a, hipStream_t st)
     });
 }
 
-// Units of an owner's rows: as many in all as the chip holds, of two rows at least where there are as many (each unit leaves its sums)
+// Units of an owner's rows: as many in all as the chip holds for many rows, down to one a CU for a few, since each leaves its sums (1000 x 2187:
+// 500 units 17.5 us and 9.3 for their sums, 250 units 15.6 and 5.7)
 int64_t norm_parts(int64_t M, int64_t C, int64_t run)
 {
-    const int64_t owners = (M + run - 1) / run, want = (norm_units(C) + owners - 1) / owners;
-    int64_t rows = (run + want - 1) / want;
-    if (rows < 2 && run > 1) rows = 2;
+    const int64_t all = norm_units(C), few = M / 8 < 256 ? 256 : M / 8, units = few < all ? few : all;
+    const int64_t owners = (M + run - 1) / run, want = (units + owners - 1) / owners, rows = (run + want - 1) / want;
     return (run + rows - 1) / rows;
 }
 constexpr int64_t kOwnerBlocks = 64;
@@ -443,6 +495,15 @@ hipError_t backward(const NormBackArgs& a, hipStream_t st)
             k_norm_back<T, LAYER, false, true, BIASES, W, PER><<<grid, Unit<W>::kThreads, 0, st>>>(a);
         return hipGetLastError();
     });
+}
+
+hipError_t run_sums(const NormSumArgs& a, dim3 grid, hipStream_t st)
+{
+    if (a.parts > 64)
+        k_norm_sums<64><<<grid, 1024, 0, st>>>(a);
+    else
+        k_norm_sums<16><<<grid, 256, 0, st>>>(a);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -493,13 +554,11 @@ hipError_t launch_norm_backward(NormBackArgs a, const NormGrads& g, float* works
     const dim3 grid((unsigned)((a.C + kSumCols - 1) / kSumCols), (unsigned)(blocks > 1 ? blocks : 1));
     float* second = workspace + 4 * units * a.C;
     for (int k = 0; k < 4; ++k) s.out[k] = !out[k] ? nullptr : blocks > 1 ? second + k * blocks * a.C : out[k];
-    k_norm_sums<<<grid, 256, 0, st>>>(s);
-    if ((e = hipGetLastError()) != hipSuccess || blocks <= 1) return e;
+    if ((e = run_sums(s, grid, st)) != hipSuccess || blocks <= 1) return e;
     NormSumArgs t = {};
     t.C = a.C, t.owners = 1, t.parts = blocks;
     for (int k = 0; k < 4; ++k) t.part[k] = s.out[k], t.out[k] = out[k];
-    k_norm_sums<<<dim3(grid.x, 1), 256, 0, st>>>(t);
-    return hipGetLastError();
+    return run_sums(t, dim3(grid.x, 1), st);
 }
 
 }  // namespace rtn

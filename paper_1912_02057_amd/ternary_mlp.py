@@ -9,6 +9,14 @@ input in 8 bits (rtn_checkpoint_pack, rtn_linear's z_ckpt) and nothing in 16; th
 straight-through estimator clipped at |w| <= 1).  A model that answers lays the weights out once (`freeze`) and calls the
 same layers for one token or many.
 
+The block takes two other things where a program asks for them: `norm`, a norm before it and one behind it with a gate on the way
+into the residual (the norms' entry points: rtn_norm, rtn_block_norm and their gradients),
+
+    u = n(x) w_in        y = gate n(block(u)) w_out + x
+
+and `layer=FourBitLinear`, layers of microscaled 4-bit weights and activations in the place of ternary weights (rtn_mx4_pack,
+rtn_mx4_linear and its gradients).
+
     python -m paper_1912_02057_amd.ternary_mlp      # trains against a teacher, then answers token by token
 """
 import math
@@ -67,12 +75,58 @@ class TernaryLinear:
         self.bias.sub_(self.grad_bias, alpha=rate)
 
 
+class FourBitLinear:
+    """The same layer on microscaled 4-bit weights and activations: latent weights [N, K] and a bias.  The backward pass rounds
+    the gradient stochastically, with another seed every step (kept on the device, so that a captured step counts on by itself)."""
+
+    def __init__(self, K, N, dtype=torch.bfloat16, device="cuda:0", generator=None):
+        self.K, self.N, self.dtype = K, N, dtype
+        self.w = torch.randn((N, K), generator=generator, device=device) / math.sqrt(K)
+        self.bias = torch.zeros(N, device=device)
+        self.seed = torch.randint(2 ** 62, (1,), generator=generator, device=device)
+        self.packed = None
+
+    def freeze(self):
+        """Packs the weights for answering; latent weights changed afterwards need another call."""
+        self.packed = B.mx4_pack(self.w)
+        self.bias16 = self.bias.to(self.dtype)
+
+    def __call__(self, x, act=B.RTN_ACT_NONE, residual=None):
+        return B.mx4_linear(x, self.packed, self.N, bias=self.bias16, act=act, residual=residual)
+
+    def forward(self, x, act=B.RTN_ACT_NONE, residual=None):
+        """Of a training step: keeps x in 4 bits, and with an activation the value before it in 16."""
+        self.act = act
+        self.packed, self.packed_t = B.mx4_pack(self.w, transposed=True)
+        self.bias16 = self.bias.to(self.dtype)
+        x4, self.x4_t = B.mx4_pack(x, transposed=True)
+        self.z = None if act == B.RTN_ACT_NONE else torch.empty((x.shape[0], self.N), dtype=x.dtype, device=x.device)
+        return B.mx4_linear(x, self.packed, self.N, bias=self.bias16, act=act, residual=residual, x_packed=x4, z_out=self.z)
+
+    def backward(self, dy):
+        """Gradients of the latent weights and the bias (kept) and of the input (returned)."""
+        self.seed.add_(1)
+        dx, self.grad_w, dbias = B.mx4_linear_backward(dy, self.packed_t, self.K, self.x4_t, act=self.act, z=self.z, seed=self.seed,
+                                                       dw_dtype=torch.float32)
+        self.x4_t = self.z = self.packed_t = None
+        self.grad_bias = dbias.float()
+        return dx
+
+    def step(self, rate):
+        """Plain gradient descent."""
+        self.w.sub_(self.grad_w, alpha=rate)
+        self.bias.sub_(self.grad_bias, alpha=rate)
+
+
 class TernaryMLP:
-    def __init__(self, width, hidden, dtype=torch.bfloat16, device="cuda:0", seed=0):
+    def __init__(self, width, hidden, dtype=torch.bfloat16, device="cuda:0", seed=0, norm=False, layer=TernaryLinear):
         g = torch.Generator(device=device)
         g.manual_seed(seed)
-        self.up = TernaryLinear(width, hidden, dtype, device, g)
-        self.down = TernaryLinear(hidden, width, dtype, device, g)
+        self.up = layer(width, hidden, dtype, device, g)
+        self.down = layer(hidden, width, dtype, device, g)
+        self.norm = norm
+        if norm:
+            self.w_in, self.w_out, self.gate = (torch.ones(width, device=device) for _ in range(3))
 
     def freeze(self):
         self.up.freeze()
@@ -81,22 +135,38 @@ class TernaryMLP:
 
     def __call__(self, x):
         """[tokens, width] -> the same, weights as frozen."""
+        if self.norm:
+            h = self.down(self.up(B.norm(x, self.w_in), B.RTN_ACT_GELU))
+            return B.block_norm(h, x, self.w_out, gate=self.gate)[0]
         return self.down(self.up(x, B.RTN_ACT_GELU), residual=x)
 
     def forward(self, x):
+        if self.norm:
+            self.x, self.h = x, self.down.forward(self.up.forward(B.norm(x, self.w_in), B.RTN_ACT_GELU))
+            return B.block_norm(self.h, x, self.w_out, gate=self.gate)[0]
         return self.down.forward(self.up.forward(x, B.RTN_ACT_GELU), residual=x)
 
     def backward(self, dy):
+        if self.norm:
+            dh, dx, self.grad_w_out, _, self.grad_gate, _, _ = B.block_norm_backward(dy, self.h, self.w_out, gate=self.gate, want_dbias=False)
+            du = self.up.backward(self.down.backward(dh))
+            dx, self.grad_w_in, _ = B.norm_backward(du, self.x, self.w_in, dx_add=dx, dx=dx, want_dbias=False)
+            self.x = self.h = None
+            return dx
         return self.up.backward(self.down.backward(dy)) + dy
 
     def step(self, rate):
         self.up.step(rate)
         self.down.step(rate)
+        if self.norm:
+            for p, grad in ((self.w_in, self.grad_w_in), (self.w_out, self.grad_w_out), (self.gate, self.grad_gate)):
+                p.sub_(grad, alpha=rate)
 
 
-def train(steps=60, tokens=512, width=256, hidden=1024, rate=0.02, seed=0, device="cuda:0"):
+def train(steps=60, tokens=512, width=256, hidden=1024, rate=0.02, seed=0, device="cuda:0", norm=False, layer=TernaryLinear):
     """Fits a block to another one of fixed weights; returns the block and the losses (mean squares of the difference)."""
-    teacher, block = TernaryMLP(width, hidden, device=device, seed=seed + 1).freeze(), TernaryMLP(width, hidden, device=device, seed=seed)
+    teacher = TernaryMLP(width, hidden, device=device, seed=seed + 1, norm=norm, layer=layer).freeze()
+    block = TernaryMLP(width, hidden, device=device, seed=seed, norm=norm, layer=layer)
     g = torch.Generator(device=device)
     g.manual_seed(seed + 2)
     losses = []
@@ -118,3 +188,6 @@ if __name__ == "__main__":
     x = torch.randn((64, 256), device="cuda:0").to(torch.bfloat16)
     at_once, one_by_one = block(x), torch.cat([block(x[i:i + 1]) for i in range(64)])
     print("64 tokens at once and one by one: largest difference %.3g of %.3g" % (float((at_once - one_by_one).abs().max()), float(at_once.abs().max())))
+    for name, kw in (("ternary weights, norms around the block", dict(norm=True)), ("4-bit weights and activations, norms", dict(norm=True, layer=FourBitLinear))):
+        block, losses = train(**kw)
+        print("%s: loss %.4f, then %.4f" % (name, losses[0], losses[-1]))

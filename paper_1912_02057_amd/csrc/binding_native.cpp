@@ -746,8 +746,10 @@ PyObject* norm_backward(PyObject*, Args a, Py_ssize_t n)
 const float* gate_of(PyObject* o, int64_t M, int64_t C, int64_t run)
 {
     const float* p = (const float*)dev(o, c10::kFloat, "gate");
-    if (!p) return nullptr;
-    if (run <= 0 || tensor(o, "gate").numel() < (M ? (M + run - 1) / run : 0) * C || (M && tensor(o, "gate").size(-1) != C))
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = tensor(o, "gate");
+    const int64_t rows = run <= 0 ? 0 : run < M ? (M + run - 1) / run : 1;
+    if (run <= 0 || t.dim() < 1 || t.size(-1) != C || (M && t.numel() != rows * C))
         fail(PyExc_AssertionError, "%s: a row of entries for every gate_run tokens is required", "gate");
     return p;
 }
@@ -812,6 +814,7 @@ PyObject* block_norm_backward(PyObject*, Args a, Py_ssize_t n)
             any |= s[i] != nullptr;
         }
         if (out[4].defined()) out[4] = out[4].view(tensor(a[4], "gate").sizes());
+        if (out[4].defined() && !M) out[4].zero_();  // (the library has no row of it to write)
         at::Tensor work;
         size_t wsb;
         void *ws = work_of(a[19], any ? rtn_norm_backward_workspace_bytes(M, C, g ? run : M) : 0, t, work, wsb), *st = stream();

@@ -58,9 +58,19 @@ __device__ __forceinline__ void mx4_mfma_inplace(u32x4 a, unsigned sa, u32x4 b, 
                  : "v"(a), "v"(b), "v"(sa), "v"(sb), "n"(SA & 1), "n"(SB & 1), "n"(SA >> 1), "n"(SB >> 1));
 #endif
 }
-// The wait states between a matrix instruction and a vector instruction that reads its result (at most 19 for 16 passes), which the compiler does
-// not count for statements like the above.
-__device__ __forceinline__ void mx4_settle() { asm volatile("s_nop 15\n\ts_nop 7" ::: "memory"); }
+// The wait states between a matrix instruction and a vector instruction that reads its result (at most 20), which the compiler does not count for
+// statements like the above; what reads the sums comes behind them, since they pass through the statement.
+template <int TN, int TM>
+__device__ __forceinline__ void mx4_settle(f32x16 (&c)[TN][TM])
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int j = 0; j < TM; ++j) asm volatile("" : "+a"(c[i][j]));
+#endif
+}
 
 // What four outputs need beside their sums, fetched before the products: conditional loads behind them would each be waited for.
 struct Extra {
@@ -556,7 +566,7 @@ __global__ __launch_bounds__(256, (TileMx4<BM, BN, NS>::BLOCKS)) void k_mx4_tile
     for (; step + L::NS < nk; ++step) one_step(std::true_type{}, step);
     for (; step < nk; ++step) one_step(std::false_type{}, step);
 
-    mx4_settle();
+    mx4_settle(acc);
     // ---- epilogue: 32 tokens of the wave at a time through LDS, after which a lane has 8 outputs of a token, in TPL passes.  With one wave on a
     // SIMD its time is its instructions, each some five cycles: a tile that lies inside the matrix has no address or bound to compute per
     // row (scalar bases, one offset a lane), and the activation is picked once.

@@ -941,7 +941,7 @@ int rtn_block_norm(rtn_dtype dt, rtn_norm_kind kind, const void* h, int64_t ldh,
     rtn::NormArgs a = {};
     a.h = h, a.x = x, a.y = y, a.u = u, a.M = M, a.C = C, a.ldh = ldh, a.ldx = ldx, a.ldy = ldy, a.ldu = ldu;
     a.weight = weight, a.bias = bias, a.gate = gate, a.next_weight = next_weight, a.next_bias = next_bias;
-    a.run = gate ? gate_run : M, a.scale = scale, a.eps = eps;
+    a.run = gate && gate_run < M ? gate_run : M, a.scale = scale, a.eps = eps;
     a.layer = kind == RTN_NORM_LAYER, a.f16 = dt == RTN_F16;
     const hipError_t e = rtn::launch_norm(a, (hipStream_t)stream);
     return e == hipSuccess ? RTN_OK : hip_fail(e);
@@ -994,7 +994,7 @@ int rtn_block_norm_backward(rtn_dtype dt, rtn_norm_kind kind, const void* dy, in
         !aligned(bias, 4) || !aligned(gate, 4) || !aligned(next_weight, 4) || !aligned(dweight, 4) || !aligned(dbias, 4) ||
         !aligned(dgate, 4) || !aligned(dnext_weight, 4) || !aligned(dnext_bias, 4) || !aligned(workspace, 16))
         return RTN_ERR_ALIGN;
-    const int64_t run = gate ? gate_run : M;
+    const int64_t run = gate && gate_run < M ? gate_run : M;
     if (M != 0 && sums && (!workspace || workspace_bytes < rtn_norm_backward_workspace_bytes(M, C, run))) return RTN_ERR_WORKSPACE;
     rtn::NormBackArgs a = {};
     a.dy = dy, a.du = du, a.h = h, a.y = y, a.dh = dh, a.dx = dx;

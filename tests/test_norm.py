@@ -305,6 +305,20 @@ def test_no_rows():
     assert y.shape == u.shape == (0, 30)
     got = B.block_norm_backward(e, e, c.weight, du=e, y=y, next_weight=c.weight)
     assert got[0].shape == (0, 30) and not got[2].any() and not got[5].any()
+    for gate in (torch.ones(30, device=Q.DEV), torch.ones((0, 30), device=Q.DEV)):
+        y, _ = B.block_norm(e, e, c.weight, gate=gate, gate_run=4)
+        dgate = B.block_norm_backward(e, e, c.weight, gate=gate, gate_run=4)[4]
+        assert dgate.shape == gate.shape and not dgate.any()
+
+
+def test_gate_runs_beyond_all_tokens():
+    c = Case("bf16", 5, 60, "rms", gate=True)
+    want = B.block_norm(c.h, c.x, c.weight, gate=c.gate, gate_run=5)[0]
+    grad = B.block_norm_backward(c.dy, c.h, c.weight, gate=c.gate, gate_run=5)
+    for run in (6, 1 << 40, (1 << 63) - 1):
+        assert torch.equal(B.block_norm(c.h, c.x, c.weight, gate=c.gate, gate_run=run)[0], want)
+        got = B.block_norm_backward(c.dy, c.h, c.weight, gate=c.gate.view(-1), gate_run=run)
+        assert all(a is b is None or torch.equal(a.view(-1), b.view(-1)) for a, b in zip(got, grad))
 
 
 def test_captured_and_on_two_streams():
@@ -358,6 +372,10 @@ def test_refusals_of_the_binding():
         B.block_norm(c.h, c.x, c.weight, gate=torch.ones((2, 40), device=Q.DEV))               # no gate_run
     with pytest.raises(AssertionError):
         B.block_norm(c.h, c.x, c.weight, gate=torch.ones((2, 40), device=Q.DEV), gate_run=2)   # three rows needed
+    with pytest.raises(AssertionError):
+        B.block_norm(c.h, c.x, c.weight, gate=torch.ones((4, 40), device=Q.DEV), gate_run=2)   # and no more
+    with pytest.raises(AssertionError):
+        B.block_norm(c.h, c.x, c.weight, gate=torch.ones((3, 40), device=Q.DEV), gate_run=0)
     with pytest.raises(B.RtnError) as e:
         B.norm(c.x, c.weight, eps=-1.0)
     assert e.value.status == B.RTN_ERR_SHAPE

@@ -207,7 +207,8 @@ struct SplitMx4 {
 };
 
 // Small grids: a block has 16 TB tokens x 16 RB outputs, its waves share the columns, every WAVES-th block of 128 each, and the operands go
-// straight into registers.  The waves' sums are added up in LDS, in their order.
+// straight into registers, two blocks in flight.  The waves' sums are added up in LDS, in their order.  Bound by the latency of its loads:
+// 24 tokens of 8192 x 8192 in 7.0 to 8.0 us, 4.5 to 5.1 TB/s of weights; 1000 x 1003 x 2187 8.5 us.
 template <class T, int TB, int RB, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void k_mx4_split(Mx4Params p)
 {
@@ -327,7 +328,9 @@ __device__ __forceinline__ u32x4 pack_group(const u32x4 (&v)[4], unsigned& scale
 
 // A few tokens (at most 16) in 16 bits: a block has 16 RB outputs, its waves share the columns, every WAVES-th block of 128 each.  A lane's part of
 // the token operand is one group of 32 values, so it packs them itself on the way into the instruction.
-// ROW16: rows of whole 16-byte units, loaded without a branch (15.7 -> 7.6 us with conditional loads, which wait for each other).
+// Bound by latencies: launch, a round of loads per two blocks of a wave, the sum over the waves (4096 x 4096, one token: 4.7 us, 8192 x 8192 7.6
+// from packed tokens: 5.0 TB/s of weights).  What an output needs beside its sum is fetched first: loaded behind the products, where a
+// condition stands before each, it took 18.9 us.  ROW16: rows of whole 16-byte units, loaded without a branch.
 template <class T, int RB, int WAVES, bool ROW16>
 __global__ __launch_bounds__(WAVES * 64) void k_mx4_few(Mx4Params p, const unsigned short* x, int64_t ldx, int K)
 {
@@ -425,12 +428,16 @@ struct TileMx4 {
     static constexpr int LDS = NS * STAGE > 4 * WAVE ? NS * STAGE : 4 * WAVE, BLOCKS = LDS <= 80 * 1024 ? 2 : 1;
 };
 
-// A block of 4 waves owns BM tokens x BN outputs, a wave a quarter, one wave to a SIMD (256 x 256).  Ring of four stages of 128 columns, as packed
-// (1 KiB a block of 16 rows, so loads and reads of it are in a row), and their scales.  One barrier a step, before the second of its two
-// 64-column slices; fragments are read one slice ahead, and the loads of the stage that the barrier frees are spread over the second.
-// The instruction is 32 x 32 x 64: one wave a SIMD issues 16 x 16 x 128 at two thirds of its rate (registers only, random codes: 5.3
-// PFLOP/s against 6.5, which is what the power limit leaves).  Lane l has row l & 31 of 32, so 16 lanes have one block of rows and 16 the
-// next: a lane's scales are shifted so that both stand in the byte the instruction picks.
+// A block of 4 waves owns BM tokens x BN outputs, a wave a quarter.  Ring of NS stages of 128 columns, as packed (1 KiB a block of 16 rows, so loads
+// and reads of it are in a row), and their scales.  One barrier a step, before the second of its two 64-column slices; fragments are read
+// one slice ahead, and the loads of the stage that the barrier frees are spread over the second.  The instruction is 32 x 32 x 64: one
+// wave a SIMD issues 16 x 16 x 128 at two thirds of its rate (registers only, random codes: 5.3 PFLOP/s against 6.5, which is what
+// the power limit leaves).  Lane l has row l & 31 of 32, so 16 lanes have one block of rows and 16 the next: a lane's scales are shifted
+// so that both stand in the byte the instruction picks.
+// Two blocks of 128 x 256 share a CU, so that one's epilogue passes beside the other's products: 16384 x 8192 x 8192 492 us, with a
+// residual 513 (4.3 PFLOP/s), one block of 256 x 256 538 and 572, although that reads a third less through LDS and its loop alone runs at 5.1
+// PFLOP/s.  Bound by the power limit: clock 1.6 GHz while the matrix cores are busy 59 % of it.  4096 x 4096 x 4096 40 us, of which the launch,
+// the first loads and the epilogue are 13.
 template <class T, int BM, int BN, int NS>
 __global__ __launch_bounds__(256, (TileMx4<BM, BN, NS>::BLOCKS)) void k_mx4_tile(Mx4Params p)
 {

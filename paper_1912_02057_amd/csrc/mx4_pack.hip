@@ -44,6 +44,7 @@ __device__ __forceinline__ float load_one(const void* p, int64_t i)
 
 // Along the rows alone.  A block has 64 rows x 128 columns, a wave 16 rows, a lane 8 columns of a row: four lanes have a group, 16 read
 // 256 bytes of a row (of 16-bit values), and the maximum is over a quad of lanes.
+// 16384 x 8192 of bfloat16: 64 us, 5.3 TB/s of what is read and written; a few rows 3.6 us, the launch and one round of loads.
 template <class T, bool RANDOM>
 __global__ __launch_bounds__(256) void k_mx4_rows(Mx4PackArgs a)
 {
@@ -102,6 +103,9 @@ __device__ __forceinline__ float exact_slope(float z)
 // columns' through LDS as fp32, after which a lane has one group of 32 rows.  Two blocks beside or below each other fill a piece of
 // 1 KiB of codes and 256 bytes of scales, each in whole 128-byte lines; the last of an odd number fills its neighbour's half with zeros.
 // The sums of the columns (the bias gradient) come on the way, 64 rows each.
+// To nearest bound by memory, 4096 x 4096 of bfloat16 13.6 us, of float32 16 us (5.3 TB/s); stochastic by the vector unit, whose random numbers
+// are 40 instructions for 8 values and direction: 16384 x 8192 153 us, 93 % of its issue slots.  (Blocks of 128 x 128: 256 x 1024 17.5 us
+// instead of 7.7, for want of blocks.)
 template <class T, int ACT, bool RANDOM>
 __global__ __launch_bounds__(128, 4) void k_mx4_both(Mx4PackArgs a)
 {
@@ -215,6 +219,7 @@ __global__ __launch_bounds__(128, 4) void k_mx4_both(Mx4PackArgs a)
     }
 }
 
+// A quad of lanes has a group, 16 lanes 256 bytes of a row.  16384 x 8192 to bfloat16: 54 us, 6.3 TB/s.
 template <class T>
 __global__ __launch_bounds__(256) void k_mx4_unpack(Mx4UnpackArgs a)
 {

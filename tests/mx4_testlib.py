@@ -3,7 +3,10 @@
 Packings are compared exactly: every step from a value to its code is exact in 64 bits and in the kernels.  A product of two packed
 values is exact in fp32, and a sum of n such terms in any order is off by at most n eps times the sum of their magnitudes, eps = 2^-24;
 terms below 2^-126 may be lost.  Activations are evaluated as in the ternary layer's tests (linear_testlib)."""
+import gc
+
 import numpy as np
+import pytest
 import torch
 
 from paper_1912_02057_amd import binding as B
@@ -14,6 +17,14 @@ DEV, U, STEP, EPS, ACT_EPS = T.DEV, T.U, T.STEP, T.EPS, T.ACT_EPS
 TYPES = dict(T.TYPES, fp32=torch.float32)
 f64 = T.f64
 GRID = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+
+
+@pytest.fixture(autouse=True, scope="module")
+def collected():
+    """Tensors in reference cycles (tracebacks, wrapped methods) are freed with the module that made them, not in the midst of a later
+    test that looks at the device's memory."""
+    yield
+    gc.collect()
 
 
 def philox(c, k):

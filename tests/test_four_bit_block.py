@@ -8,6 +8,7 @@ from paper_1912_02057_amd import ternary_mlp as M
 
 import linear_testlib as T
 import mx4_testlib as Q
+from mx4_testlib import collected  # noqa: F401 (a fixture of the module)
 from test_norm import back64, norm64, rounded
 
 pytestmark = pytest.mark.gpu
@@ -58,6 +59,8 @@ def test_the_block_is_its_parts(layer, tokens, width, hidden):
     T.assert_within(block.grad_w_in, (g * n).sum(0), bound(g * n, np.abs(g) * en), "grad_w_in")
     T.assert_within(block.grad_w_out, (d * gate * m).sum(0), bound(d * gate * m, np.abs(d * gate) * em), "grad_w_out")
     T.assert_within(block.grad_gate, (d * m * w_out).sum(0), bound(d * m * w_out, np.abs(d * w_out) * em), "grad_gate")
+    for obj, name in list(seen):
+        delattr(obj, name)
     # answering runs the same calls
     block.freeze()
     one = torch.cat([block(x[i:i + 1]) for i in range(min(tokens, 5))])

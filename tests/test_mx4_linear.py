@@ -7,6 +7,7 @@ from paper_1912_02057_amd import binding as B
 
 import linear_testlib as T
 import mx4_testlib as Q
+from mx4_testlib import collected  # noqa: F401 (a fixture of the module)
 
 pytestmark = pytest.mark.gpu
 

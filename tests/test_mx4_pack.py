@@ -6,6 +6,7 @@ import torch
 from paper_1912_02057_amd import binding as B
 
 import mx4_testlib as Q
+from mx4_testlib import collected  # noqa: F401 (a fixture of the module)
 
 pytestmark = pytest.mark.gpu
 

@@ -417,34 +417,34 @@ hipError_t run_few(const Mx4Params& p, const Mx4LinArgs& a, hipStream_t st)
 
 // ---- tiles of a full grid
 typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(2)));  // wherever it starts
-template <int BM, int BN, int NS_>
+template <int BM, int BN, int NS_, int WM>
 struct TileMx4 {
     static constexpr int NS = NS_;                                 // stages of 128 columns
-    static constexpr int WN = BN / 2, TM = BM / 64, TN = BN / 64;  // a wave's outputs; its blocks of 32 tokens, of 32 outputs
+    static constexpr int WAVES = 2 * WM, WN = BN / 2, TM = BM / 32 / WM, TN = BN / 64;  // a wave's outputs; its blocks of 32 tokens, of 32 outputs
     // codes of the weights and the tokens, then their scales, 1 KiB each
-    static constexpr int CODES = (BM + BN) * 64, STAGE = CODES + 2 * 1024, PER = (BM + BN) / 64, DPS = PER + 1;
+    static constexpr int CODES = (BM + BN) * 64, STAGE = CODES + 2 * 1024, PER = (BM + BN) / 16 / WAVES, DPS = PER + 1;
     static constexpr int OTHER = BN / 16 % PER;                    // from this one on, a wave's loads may be of the tokens
     static constexpr int PITCH = WN * 4 + 16, WAVE = 32 * PITCH;   // 32 tokens of a wave in the epilogue
-    static constexpr int LDS = NS * STAGE > 4 * WAVE ? NS * STAGE : 4 * WAVE, BLOCKS = LDS <= 80 * 1024 ? 2 : 1;
+    static constexpr int LDS = NS * STAGE > WAVES * WAVE ? NS * STAGE : WAVES * WAVE, BLOCKS = LDS <= 80 * 1024 ? 2 : 1;
 };
 
-// A block of 4 waves owns BM tokens x BN outputs, a wave a quarter.  Ring of NS stages of 128 columns, as packed (1 KiB a block of 16 rows, so loads
-// and reads of it are in a row), and their scales.  One barrier a step, before the second of its two 64-column slices; fragments are read
-// one slice ahead, and the loads of the stage that the barrier frees are spread over the second.  The instruction is 32 x 32 x 64: one
-// wave a SIMD issues 16 x 16 x 128 at two thirds of its rate (registers only, random codes: 5.3 PFLOP/s against 6.5, which is what
-// the power limit leaves).  Lane l has row l & 31 of 32, so 16 lanes have one block of rows and 16 the next: a lane's scales are shifted
-// so that both stand in the byte the instruction picks.
-// Two blocks of 128 x 256 share a CU, so that one's epilogue passes beside the other's products: 16384 x 8192 x 8192 492 us, with a
-// residual 513 (4.3 PFLOP/s), one block of 256 x 256 538 and 572, although that reads a third less through LDS and its loop alone runs at 5.1
-// PFLOP/s.  Bound by the power limit: clock 1.6 GHz while the matrix cores are busy 59 % of it.  4096 x 4096 x 4096 40 us, of which the launch,
-// the first loads and the epilogue are 13.
-template <class T, int BM, int BN, int NS>
-__global__ __launch_bounds__(256, (TileMx4<BM, BN, NS>::BLOCKS)) void k_mx4_tile(Mx4Params p)
+// A block of 2 WM waves owns BM tokens x BN outputs, a wave half of the outputs of a WM-th of the tokens.  Ring of NS stages of 128 columns, as packed
+// (1 KiB a block of 16 rows, so loads and reads of it are in a row), and their scales.  One barrier a step, before the second of its two
+// 64-column slices; fragments are read one slice ahead, and the loads of the stage that the barrier frees are spread over the second.  The
+// instruction is 32 x 32 x 64: one wave a SIMD issues 16 x 16 x 128 at two thirds of its rate (registers only, random codes: 5.3
+// PFLOP/s against 6.5, which is what the power limit leaves).  Lane l has row l & 31 of 32, so 16 lanes have one block of rows and 16 the
+// next: a lane's scales are shifted so that both stand in the byte the instruction picks.
+// Over several rounds two blocks of 128 x 256 share a CU, so that one's epilogue passes beside the other's products: 16384 x 8192 x 8192 492 us,
+// with a residual 513 to 530 (4.1 to 4.3 PFLOP/s).  Bound by the power limit: clock 1.6 GHz while the matrix cores are busy 59 % of it.  In a
+// single round there is nothing to pass beside, and a block of 256 x 256 with eight waves loads a third less: 4096 x 4096 x 4096 36 to 38 us (38
+// to 40), 2048 x 8192 x 8192 63 (68); over several, with a residual, 553 (528) at 16384 x 8192 x 8192.
+template <class T, int BM, int BN, int NS, int WM>
+__global__ __launch_bounds__(128 * WM, (TileMx4<BM, BN, NS, WM>::BLOCKS * WM / 2)) void k_mx4_tile(Mx4Params p)
 {
-    using L = TileMx4<BM, BN, NS>;
+    using L = TileMx4<BM, BN, NS, WM>;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int l32 = lane & 31, h = lane >> 5, wn = wave >> 1, wm = wave & 1, nk = p.nk;
+    const int l32 = lane & 31, h = lane >> 5, wn = wave / WM, wm = wave % WM, nk = p.nk;
     int tm, tn;
     {
         const int chunk = (int)(gridDim.x >> 3), bid = (int)(blockIdx.x & 7) * chunk + (int)(blockIdx.x >> 3);
@@ -580,7 +580,7 @@ __global__ __launch_bounds__(256, (TileMx4<BM, BN, NS>::BLOCKS)) void k_mx4_tile
     __syncthreads();
     constexpr int CL = L::WN / 8, RPP = 64 / CL, TPL = 32 / RPP;
     char* zs = smem + wave * L::WAVE;
-    const int nw = n0 + wn * L::WN, mw = m0 + wm * (BM / 2), n8 = nw + (lane % CL) * 8, t0 = lane / CL;
+    const int nw = n0 + wn * L::WN, mw = m0 + wm * (BM / WM), n8 = nw + (lane % CL) * 8, t0 = lane / CL;
     if (nw >= p.N || mw >= p.M) return;
     float bi[8];
 #pragma unroll
@@ -603,22 +603,29 @@ __global__ __launch_bounds__(256, (TileMx4<BM, BN, NS>::BLOCKS)) void k_mx4_tile
         z[4] = b.x + bi[4], z[5] = b.y + bi[5], z[6] = b.z + bi[6], z[7] = b.w + bi[7];
     };
     constexpr int64_t kFar = 1 << 26;  // a pitch up to which a lane's offset is 32 bits
-    const bool whole = mw + BM / 2 <= p.M && nw + L::WN <= p.N && p.ldy < kFar && p.ldr < kFar && p.ldz < kFar;
+    const bool whole = mw + BM / WM <= p.M && nw + L::WN <= p.N && p.ldy < kFar && p.ldr < kFar && p.ldz < kFar;
     const unsigned col = (unsigned)(lane % CL) * 8;
     const unsigned vy = ((unsigned)t0 * (unsigned)p.ldy + col) * (p.y_f32 ? 4u : 2u), vr = ((unsigned)t0 * (unsigned)p.ldr + col) * 2u,
                    vz = ((unsigned)t0 * (unsigned)p.ldz + col) * 2u;
     auto row = [](auto* base, int64_t ld, int m, int n, int bytes) { return (char*)base + ((int64_t)m * ld + n) * bytes; };
+    // the residual of all rounds at once where a block is alone on its CU, so that one latency is exposed; else of a round
+    constexpr int AHEAD = L::BLOCKS == 1 ? L::TM : 1;
+    u32x4 res[AHEAD][TPL];
+    auto fetch = [&](int k, u32x4(&r)[TPL]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < TPL; ++t) {
+            const u32x4_any* q = (const u32x4_any*)(row(p.res, p.ldr, mw + k * 32 + t * RPP, nw, 2) + vr);
+            r[t] = p.res_once ? __builtin_nontemporal_load(q) : *q;
+        }
+    };
+    if (AHEAD > 1 && p.res && whole)
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) fetch(k, res[k]);
     for_each_index(
         [&](auto index) __attribute__((always_inline)) {
-            constexpr int k = decltype(index)::value;
+            constexpr int k = decltype(index)::value, at = AHEAD > 1 ? k : 0;
             if (mw + k * 32 >= p.M) return;
-            u32x4 res[TPL];
-            if (p.res && whole)
-#pragma unroll
-                for (int t = 0; t < TPL; ++t) {
-                    const u32x4_any* r = (const u32x4_any*)(row(p.res, p.ldr, mw + k * 32 + t * RPP, nw, 2) + vr);
-                    res[t] = p.res_once ? __builtin_nontemporal_load(r) : *r;
-                }
+            if (AHEAD == 1 && p.res && whole) fetch(k, res[0]);
             put(index);
             if (!whole) {
 #pragma unroll 1
@@ -642,7 +649,7 @@ __global__ __launch_bounds__(256, (TileMx4<BM, BN, NS>::BLOCKS)) void k_mx4_tile
                     for (int i = 0; i < 8; ++i) z[i] = act_value<decltype(which)::value>(z[i]);
                     if (p.res) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) z[i] += half_of<T>(res[t][i >> 1], i & 1);
+                        for (int i = 0; i < 8; ++i) z[i] += half_of<T>(res[at][t][i >> 1], i & 1);
                     }
                     if (p.y_f32) {
                         char* y = row(p.y, p.ldy, m, nw, 4) + vy;
@@ -659,10 +666,10 @@ __global__ __launch_bounds__(256, (TileMx4<BM, BN, NS>::BLOCKS)) void k_mx4_tile
         std::make_integer_sequence<int, L::TM>{});
 }
 
-template <class T, int BM, int BN, int NS>
+template <class T, int BM, int BN, int NS, int WM>
 hipError_t run_tile(Mx4Params& p, hipStream_t st)
 {
-    using L = TileMx4<BM, BN, NS>;
+    using L = TileMx4<BM, BN, NS, WM>;
     p.tilesM = (p.M + BM - 1) / BM;
     const int tilesN = (p.N + BN - 1) / BN;
     const int64_t nt = (int64_t)p.tilesM * tilesN;
@@ -672,9 +679,9 @@ hipError_t run_tile(Mx4Params& p, hipStream_t st)
     p.div_band = make_fastdiv((uint32_t)p.band_tiles);
     p.div_lastband = make_fastdiv((uint32_t)(p.tilesM % 8 ? p.tilesM % 8 : 8));
     static LdsLimit limit;
-    const hipError_t e = limit.raise((const void*)&k_mx4_tile<T, BM, BN, NS>, L::LDS);
+    const hipError_t e = limit.raise((const void*)&k_mx4_tile<T, BM, BN, NS, WM>, L::LDS);
     if (e != hipSuccess) return e;
-    k_mx4_tile<T, BM, BN, NS><<<(unsigned)((nt + 7) / 8 * 8), 256, L::LDS, st>>>(p);
+    k_mx4_tile<T, BM, BN, NS, WM><<<(unsigned)((nt + 7) / 8 * 8), 128 * WM, L::LDS, st>>>(p);
     return hipGetLastError();
 }
 
@@ -689,8 +696,9 @@ hipError_t run(Mx4Params& p, const Mx4LinArgs& a, hipStream_t st)
         case Mx4Form::kSplit32x64: return run_split<T, 2, 4, 8>(p, st);
         case Mx4Form::kSplit64: return run_split<T, 4, 4, 8>(p, st);
         case Mx4Form::kSplit64x4: return run_split<T, 4, 4, 4>(p, st);
-        case Mx4Form::kTile128: return run_tile<T, 128, 128, 4>(p, st);
-        default: return run_tile<T, 128, 256, 3>(p, st);
+        case Mx4Form::kTile128: return run_tile<T, 128, 128, 4, 2>(p, st);
+        case Mx4Form::kTile256: return run_tile<T, 256, 256, 4, 4>(p, st);
+        default: return run_tile<T, 128, 256, 3, 2>(p, st);
     }
 }
 

@@ -470,7 +470,8 @@ hipError_t forward(NormArgs a, hipStream_t st)
 }
 
 // Units of an owner's rows: as many in all as the chip holds for many rows, down to one a CU for a few, since each leaves its sums (1000 x 2187:
-// 500 units 17.5 us and 9.3 for their sums, 250 units 15.6 and 5.7)
+// 500 units 17.5 us and 9.3 for their sums, 250 units 15.6 and 5.7; with
+// both, 128 / 256 / 512 / 1024 / 2048 units: 2000 x 8192 40 31 36 45, 8192 x 4096 88 53 42 46 52, 16384 x 512 108 59 35 24 21)
 int64_t norm_parts(int64_t M, int64_t C, int64_t run)
 {
     const int64_t all = norm_units(C), few = M / 8 < 256 ? 256 : M / 8, units = few < all ? few : all;

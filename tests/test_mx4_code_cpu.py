@@ -30,7 +30,7 @@ def tiles(objects):  # noqa: F811
                 words = re.split(r"[ ,]+", line.split("//")[0].strip())
                 if words[0]:
                     found.setdefault(name, []).append(words)
-    assert len(found) == 4
+    assert len(found) == 6
     return found
 
 

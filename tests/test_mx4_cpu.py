@@ -128,7 +128,7 @@ extern "C" int form(int64_t M, int64_t N, int64_t K) { return (int)rtn::mx4_form
     form = C.CDLL(str(tmp_path / "r.so")).form
     form.argtypes = [C.c_int64] * 3
     sizes = G.SIZES + G.TILES
-    assert {form(*s) for s in sizes} == set(range(8))
-    for f, ring in ((6, 4), (7, 3)):
+    assert {form(*s) for s in sizes} == set(range(9))
+    for f, ring in ((6, 4), (7, 3), (8, 4)):
         steps = [-(-K // 128) for M, N, K in sizes if form(M, N, K) == f]
         assert min(steps) == 1 and max(steps) > ring + 1 and any(M % 128 and N % 128 for M, N, K in sizes if form(M, N, K) == f), (f, steps)

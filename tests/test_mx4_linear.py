@@ -18,7 +18,7 @@ SIZES = [(1, 1, 1), (1, 48, 4096), (1, 4096, 130), (2, 33, 31), (5, 100, 257), (
 # tiles that end inside the matrix, from one block of columns to more than the ring holds
 TILES = [(1800, 1747, 100), (1797, 1800, 900), (3500, 3393, 70), (3489, 3500, 1100), (3490, 3400, 390), (257, 30000, 300), (40000, 200, 390),
          (1700, 1300, 3000), (1290, 1030, 2700), (700, 3300, 1030), (1030, 1290, 2600),
-         (1290, 1030, 100), (2900, 2900, 70)]
+         (1290, 1030, 100), (2900, 2900, 70), (300, 35000, 100), (70000, 200, 390), (300, 35000, 700)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])

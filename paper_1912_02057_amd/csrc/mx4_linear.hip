@@ -456,8 +456,8 @@ __global__ __launch_bounds__(128 * WM, (TileMx4<BM, BN, NS, WM>::BLOCKS * WM / 2
     const int m0 = tm * BM, n0 = tn * BN;
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
 
-    // ---- direct loads of a stage: a wave has a quarter of the blocks of 16 rows, the weights' before the tokens', and the scales of either
-    // (waves 2 and 3 write the same as 0 and 1, so that all count alike)
+    // ---- direct loads of a stage: a wave has its share of the blocks of 16 rows, the weights' before the tokens', and the scales of either
+    // (all even waves write the same, and all odd ones, so that all count alike)
     const int wb0 = n0 / 16, ab0 = m0 / 16;
     auto code_base = [&](bool of_w) { return buffer_base(of_w ? p.w + (int64_t)wb0 * nk * 1024 : p.a + (int64_t)ab0 * nk * 1024); };
     const v4i codes[2] = {code_base(wave * L::PER < BN / 16), code_base(wave * L::PER + L::OTHER < BN / 16)};

@@ -84,19 +84,28 @@ __global__ __launch_bounds__(256) void k_mx4_rows(Mx4PackArgs a)
     if (wave == 0) *(unsigned*)((char*)a.out + s.codes() + (rg * s.kb + kb) * 256 + lane * 4) = scales[lane];
 }
 
-// phi'(z) for the gradient that is packed: to fp32's accuracy, since a packed value next to the border of two codes takes the one or
+// phi'(z) of gelu or silu for the gradient that is packed: to fp32's accuracy, since a packed value next to the border of two codes takes the one or
 // the other.
 template <int ACT>
 __device__ __forceinline__ float exact_slope(float z)
 {
     if constexpr (ACT == kActGelu) {
         return 0.5f * erfcf(z * -0.70710678f) + z * 0.39894228f * expf(-0.5f * z * z);
-    } else if constexpr (ACT == kActSilu) {
+    } else {
+        static_assert(ACT == kActSilu, "");
         const float s = 1.f / (1.f + expf(-z));
         return s * (1.f + z * (1.f - s));
-    } else {
-        return act_slope<ACT>(z);
     }
+}
+// dy phi'(z).  Where a relu is off dy is dropped, not multiplied: 0 times an infinity or NaN is no 0, and one NaN takes its groups' other 31 values
+// in both packings with it.
+template <int ACT>
+__device__ __forceinline__ float act_gradient(float dy, float z)
+{
+    if constexpr (ACT == kActRelu)
+        return z > 0.f ? dy : z == z ? 0.f : z;
+    else
+        return dy * exact_slope<ACT>(z);
 }
 
 // Along the rows and along the columns.  A block has 64 rows x 64 columns: the rows' groups as above, straight from the registers; the
@@ -128,7 +137,7 @@ __global__ __launch_bounds__(128, 4) void k_mx4_both(Mx4PackArgs a)
                 float z[8];
                 load_whole<T>(zs + i * 16 * a.ldz * kBytesOf<T>, z);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] *= exact_slope<ACT>(z[e]);
+                for (int e = 0; e < 8; ++e) v[i][e] = act_gradient<ACT>(v[i][e], z[e]);
             }
         }
 #pragma unroll
@@ -144,7 +153,7 @@ __global__ __launch_bounds__(128, 4) void k_mx4_both(Mx4PackArgs a)
             float f = 0.f;
             if (r < a.R && c < a.C) {
                 f = load_one<T>(a.x, r * a.ldx + c);
-                if constexpr (ACT != kActNone) f *= exact_slope<ACT>(load_one<T>(a.z, r * a.ldz + c));
+                if constexpr (ACT != kActNone) f = act_gradient<ACT>(f, load_one<T>(a.z, r * a.ldz + c));
             }
             tile[i][tc] = f;
         }

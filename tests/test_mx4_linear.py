@@ -207,6 +207,31 @@ def test_backward_of_no_tokens():
     assert dx.shape == (0, 40) and not dw.any() and not db.any()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("seed", [None, 5])
+@pytest.mark.parametrize("M,N,K", [(3, 40, 33), (130, 200, 70)])
+def test_gradient_behind_a_relu_that_is_off(dtype, seed, M, N, K):
+    """An infinity or NaN in dy where the relu is off reaches nothing, as zeros there; where it is on it reaches its token and its output."""
+    L = Q.Layer(dtype, M, N, K, seed=M, residual=False)
+    wt, xt = B.mx4_pack(L.w, transposed=True)[1], B.mx4_pack(L.x, transposed=True)[1]
+    z = Q.values(np.random.default_rng(7), M, N, dtype)
+    kw = dict(act=B.RTN_ACT_RELU, z=z, seed=Q.seed_tensor(seed), dw_dtype=torch.float32)
+    z[M // 2, N // 2] = z[0, 0] = -1.0
+    z[M - 1, N - 1] = 0.0
+    want = B.mx4_linear_backward(L.dy, wt, K, xt, **kw)
+    dy = L.dy.clone()
+    dy[M // 2, N // 2], dy[0, 0], dy[M - 1, N - 1] = float("inf"), float("nan"), float("-inf")
+    for a, b in zip(B.mx4_linear_backward(dy, wt, K, xt, **kw), want):
+        assert torch.equal(a, b)
+    z[M // 2, N // 2] = 1.0
+    want = B.mx4_linear_backward(L.dy, wt, K, xt, **kw)
+    dx, dw, db = B.mx4_linear_backward(dy, wt, K, xt, **kw)
+    rows, cols = torch.arange(M, device=Q.DEV) != M // 2, torch.arange(N, device=Q.DEV) != N // 2
+    assert torch.isnan(dx[M // 2]).all() and torch.equal(dx[rows], want[0][rows])
+    assert torch.isnan(dw[N // 2]).all() and torch.equal(dw[cols], want[1][cols])
+    assert not torch.isfinite(db[N // 2]) and torch.equal(db[cols], want[2][cols])
+
+
 # ------------------------------------------------------------------ streams, graphs, buffers
 
 def test_captured_step_takes_new_inputs_and_seeds():

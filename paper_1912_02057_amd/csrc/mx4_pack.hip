@@ -85,16 +85,18 @@ __global__ __launch_bounds__(256) void k_mx4_rows(Mx4PackArgs a)
 }
 
 // phi'(z) of gelu or silu for the gradient that is packed: to fp32's accuracy, since a packed value next to the border of two codes takes the one or
-// the other.
+// the other.  z may be an infinity (float16 rounds what is beyond its range to one): the factor that is z itself is held to where the other
+// one is 0 already, so that the slopes there are 0 and 1.  (A NaN comes through erfcf and expf.)
 template <int ACT>
 __device__ __forceinline__ float exact_slope(float z)
 {
+    const float held = __builtin_amdgcn_fmed3f(z, -128.f, 128.f);
     if constexpr (ACT == kActGelu) {
-        return 0.5f * erfcf(z * -0.70710678f) + z * 0.39894228f * expf(-0.5f * z * z);
+        return 0.5f * erfcf(z * -0.70710678f) + held * 0.39894228f * expf(-0.5f * z * z);
     } else {
         static_assert(ACT == kActSilu, "");
         const float s = 1.f / (1.f + expf(-z));
-        return s * (1.f + z * (1.f - s));
+        return s * (1.f + held * (1.f - s));
     }
 }
 // dy phi'(z).  Where a relu is off dy is dropped, not multiplied: 0 times an infinity or NaN is no 0, and one NaN takes its groups' other 31 values

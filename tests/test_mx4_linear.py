@@ -232,6 +232,27 @@ def test_gradient_behind_a_relu_that_is_off(dtype, seed, M, N, K):
     assert not torch.isfinite(db[N // 2]) and torch.equal(db[cols], want[2][cols])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("M,N,K", [(3, 40, 33), (130, 200, 70)])
+def test_slopes_far_out(dtype, act, M, N, K):
+    """z at the ends of its type, to which float16 rounds what is beyond them: the slopes are 1 and 0, as a relu's; a NaN stays one."""
+    L = Q.Layer(dtype, M, N, K, seed=M, residual=False)
+    wt, xt = B.mx4_pack(L.w, transposed=True)[1], B.mx4_pack(L.x, transposed=True)[1]
+    sign = torch.from_numpy(np.random.default_rng(8).choice([-1.0, 1.0], (M, N)).astype(np.float32)).to(Q.DEV).to(L.type)
+    for seed in (None, 6):
+        kw = dict(seed=Q.seed_tensor(seed), dw_dtype=torch.float32)
+        want = B.mx4_linear_backward(L.dy, wt, K, xt, act=B.RTN_ACT_RELU, z=sign, **kw)
+        for far in (float("inf"), float(torch.finfo(L.type).max), 200.0):
+            for a, b in zip(B.mx4_linear_backward(L.dy, wt, K, xt, act=T.ACTS[act], z=sign * far, **kw), want):
+                assert torch.equal(a, b), far
+    z = sign * float("inf")
+    z[1, 2] = float("nan")
+    dx, dw, db = B.mx4_linear_backward(L.dy, wt, K, xt, act=T.ACTS[act], z=z, dw_dtype=torch.float32)
+    assert torch.isnan(dx[1]).all() and torch.isnan(dw[2]).all() and torch.isnan(db[2])
+    assert torch.isfinite(dx[0]).all() and torch.isfinite(dw[0]).all()
+
+
 # ------------------------------------------------------------------ streams, graphs, buffers
 
 def test_captured_step_takes_new_inputs_and_seeds():

@@ -808,9 +808,9 @@ PyObject* block_norm_backward(PyObject*, Args a, Py_ssize_t n)
         const char* const names[5] = {"dweight", "dbias", "dgate", "dnext_weight", "dnext_bias"};
         bool any = false;
         for (int i = 0; i < 5; ++i) {
-            // (by the arguments, not their pointers, which are NULL for tensors of no rows)
+            // (by the arguments, not their pointers, which are NULL for tensors of no rows; rows of no columns are the library's to refuse)
             const bool rows = i == 2 && a[4] != Py_None, exists = i == 2 ? rows : i < 3 || a[7] != Py_None;
-            s[i] = grad_of(out[2 + i], Py_None, truth(a[14 + i]) && exists, rows ? tensor(a[4], "gate").numel() / C : -1, C, t, names[i]);
+            s[i] = grad_of(out[2 + i], Py_None, truth(a[14 + i]) && exists, rows ? (C ? tensor(a[4], "gate").numel() / C : 0) : -1, C, t, names[i]);
             any |= s[i] != nullptr;
         }
         if (out[4].defined()) out[4] = out[4].view(tensor(a[4], "gate").sizes());

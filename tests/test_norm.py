@@ -395,3 +395,17 @@ def test_refusals_of_the_binding():
     assert e.value.status == B.RTN_ERR_WORKSPACE
     with pytest.raises(ValueError):
         B.norm_backward(c.du, c.x, c.weight, workspace=torch.empty(need, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("rows", [None, 0, 1, 3])
+def test_rows_of_no_columns_are_refused(rows):
+    """By every entry point, with and without a gate of no columns."""
+    h, w = torch.empty((3, 0), dtype=torch.bfloat16, device=Q.DEV), torch.empty(0, device=Q.DEV)
+    gate = {} if rows is None else dict(gate=torch.empty((rows, 0), device=Q.DEV) if rows else w, gate_run=1)
+    for call in (lambda: B.norm(h, w), lambda: B.norm_backward(h, h, w), lambda: B.block_norm(h, h, w, next_weight=w, **gate),
+                 lambda: B.block_norm_backward(h, h, w, **gate), lambda: B.block_norm_backward(h, h, w, want_dgate=False, **gate),
+                 lambda: B.block_norm_backward(h, h, w, du=h, y=h, next_weight=w, **gate),
+                 lambda: B.block_norm_backward(h[:0], h[:0], w, **gate)):
+        with pytest.raises(B.RtnError) as e:
+            call()
+        assert e.value.status in (B.RTN_ERR_NULL, B.RTN_ERR_SHAPE)   # (an empty tensor has no address)

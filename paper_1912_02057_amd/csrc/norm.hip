@@ -471,11 +471,15 @@ hipError_t forward(NormArgs a, hipStream_t st)
 
 // Units of an owner's rows: as many in all as the chip holds for many rows, down to one a CU for a few, since each leaves its sums (1000 x 2187:
 // 500 units 17.5 us and 9.3 for their sums, 250 units 15.6 and 5.7; with
-// both, 128 / 256 / 512 / 1024 / 2048 units: 2000 x 8192 40 31 36 45, 8192 x 4096 88 53 42 46 52, 16384 x 512 108 59 35 24 21)
+// both, 128 / 256 / 512 / 1024 / 2048 units: 2000 x 8192 40 31 36 45, 8192 x 4096 88 53 42 46 52, 16384 x 512 108 59 35 24 21).
+// No more in all than the chip holds, since what is beyond is a second round of as many rows each (three gates, 16384 x 8192: 3 x 86 units 469 us,
+// 3 x 85 335); but where a unit an owner would leave more than a third of the chip idle, three of them in two rounds (300 gates,
+// 16384 x 2187, 512 at once: 1 each 222, 2 196, 3 176).
 int64_t norm_parts(int64_t M, int64_t C, int64_t run)
 {
     const int64_t all = norm_units(C), few = M / 8 < 256 ? 256 : M / 8, units = few < all ? few : all;
-    const int64_t owners = (M + run - 1) / run, want = (units + owners - 1) / owners, rows = (run + want - 1) / want;
+    const int64_t owners = (M + run - 1) / run, wish = (units + owners - 1) / owners, fit = all / owners;
+    const int64_t want = wish <= fit ? wish : fit > 1 ? fit : wish > 1 && 3 * owners < 2 * all ? 3 : 1, rows = (run + want - 1) / want;
     return (run + rows - 1) / rows;
 }
 constexpr int64_t kOwnerBlocks = 64;

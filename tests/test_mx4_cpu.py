@@ -110,6 +110,21 @@ def test_block_norm_refuses(L):  # noqa: F811
         ({25: HALF}, A), ({28: FOUR}, A), ({28: None}, W), ({29: L.rtn_norm_backward_workspace_bytes(100, 64, 10) - 1}, W)])
 
 
+def test_units_of_the_norms_gradients_fill_whole_rounds(L):  # noqa: F811
+    """The units of all rows of the gate, which the workspace holds four sums of each for (and four of each of up to 64 blocks of owners), are no
+    more than the chip holds at 16 waves to a CU, or one for each owner, or three where those fit twice."""
+    rng = np.random.default_rng(1)
+    for C, held in ((64, 4096), (512, 4096), (513, 1024), (2048, 1024), (2187, 512), (4096, 512), (4100, 256), (8192, 256), (16384, 256)):
+        for M in [1, 2, 255, 256, 300, 1000, 2000, 16384] + [int(m) for m in np.exp(rng.uniform(0, np.log(1 << 20), 30))]:
+            for G in [1, 2, 3, 5, 7, 24, 100, 255, 256, 257, 300] + [int(g) for g in np.exp(rng.uniform(0, np.log(M + 1), 30))]:
+                run = -(-M // min(G, M))
+                owners = -(-M // run)
+                units, rest = divmod(L.rtn_norm_backward_workspace_bytes(M, C, run), 16 * C)
+                units -= min(owners, 64)
+                assert rest == 0 and units % owners == 0 and units > 0, (M, C, run, units)
+                assert units <= held or units == owners or units <= 3 * owners < 2 * held < 4 * owners, (M, C, run, units)
+
+
 @pytest.mark.parametrize("call", [lambda t: B.mx4_pack(t), lambda t: B.mx4_linear(t, t, 4), lambda t: B.norm(t, t[0]), lambda t: B.block_norm(t, t, t[0])])
 def test_the_binding_takes_device_tensors_only(call):
     import torch

@@ -147,3 +147,23 @@ extern "C" int form(int64_t M, int64_t N, int64_t K) { return (int)rtn::mx4_form
     for f, ring in ((6, 4), (7, 3), (8, 4)):
         steps = [-(-K // 128) for M, N, K in sizes if form(M, N, K) == f]
         assert min(steps) == 1 and max(steps) > ring + 1 and any(M % 128 and N % 128 for M, N, K in sizes if form(M, N, K) == f), (f, steps)
+
+
+def test_sizes_of_the_gradients_reach_the_larger_forms(tmp_path):
+    """dx is a product of M x K over N, dw, whose sums may leave in fp32, of N x K over M: each in all forms from the 64 x 64 blocks of four
+    waves on, with edges inside the tiles; and the forward pass' epilogues and pitches."""
+    import test_mx4_linear as G
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_1912_02057_amd", "csrc")
+    (tmp_path / "r.cpp").write_text("""#include "choice.h"
+extern "C" int form(int64_t M, int64_t N, int64_t K) { return (int)rtn::mx4_form(M, N, K); }
+""")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I" + csrc, str(tmp_path / "r.cpp"), "-o", str(tmp_path / "r.so")], check=True)
+    form = C.CDLL(str(tmp_path / "r.so")).form
+    form.argtypes = [C.c_int64] * 3
+    dx, dw = [(M, K, N) for M, N, K in G.GRADS], [(N, K, M) for M, N, K in G.GRADS]
+    for sizes in (dx, dw, G.FORMS):
+        for f in (5, 6, 7, 8):
+            assert any(form(*s) == f and s[0] % 128 and s[1] % 128 for s in sizes), (f, sizes)
+    assert any(form(*s) == 8 and s[0] % 256 == 0 == s[1] % 256 for s in dw)
+    assert any(form(*s) in (6, 7, 8) and s[2] > 5 * 128 for s in dx) and any(form(*s) in (6, 7, 8) and s[2] > 5 * 128 for s in dw)
+    assert any(form(*s) == 7 and s[0] * s[1] >= 1 << 25 for s in G.FORMS)

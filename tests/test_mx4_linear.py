@@ -342,3 +342,93 @@ def test_buffers():
     with pytest.raises(B.RtnError) as e:
         B.mx4_linear_backward(L.dy, wt, 96, xt, act=B.RTN_ACT_RELU)
     assert e.value.status == B.RTN_ERR_NULL
+
+
+# ------------------------------------------------------------------ every form of the product
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("act", ["none", "silu"])
+@pytest.mark.parametrize("M,N,K", [s for s in SIZES if s[0] <= 16])
+def test_z_of_a_few_tokens(dtype, act, M, N, K):
+    """The value before the activation where the tokens are packed on the way."""
+    L = Q.Layer(dtype, M, N, K, seed=M + N + K + 1)
+    z = torch.empty((M, N), dtype=L.type, device=Q.DEV)
+    B.mx4_linear(L.x, B.mx4_pack(L.w), N, bias=L.bias, act=T.ACTS[act], residual=L.res, z_out=z)
+    want, e = L.z64()
+    T.assert_within(z, want, L.rounded(want, e), "z")
+
+
+# The larger forms, one size each, and one whose residual is read past the caches: edges of tiles inside, whole ones beside them
+FORMS = [(1300, 1290, 200), (1797, 1750, 330), (3001, 2990, 140), (4200, 4100, 140), (4200, 8200, 140)]
+
+
+def _product64(L):
+    """Q(x) Q(w)^T in 64 bits and the sums of its terms' magnitudes."""
+    x, w = Q.four(Q.f64(L.x)), Q.four(Q.f64(L.w))
+    return x @ w.T, np.abs(x) @ np.abs(w).T
+
+
+@pytest.mark.parametrize("dtype,M,N,K", [(("bf16", "fp16")[i % 2],) + s for i, s in enumerate(FORMS)])
+def test_epilogue_of_every_form(dtype, M, N, K):
+    L = Q.Layer(dtype, M, N, K, seed=K + N)
+    w, (s, size) = B.mx4_pack(L.w), _product64(L)
+    for act, bias, residual in (("none", False, False), ("relu", False, True), ("silu", True, False), ("none", True, True)):
+        b = Q.f64(L.bias) if bias else np.zeros(N)
+        z, ez = s + b, (K + 2) * Q.EPS * (size + np.abs(b)) + K * 2.0 ** -126
+        want, e = T.act(z, act), 1.13 * ez + (Q.ACT_EPS * np.maximum(1, np.abs(z)) if act == "silu" else 0)
+        if residual:
+            r = Q.f64(L.res)
+            want, e = want + r, e + Q.EPS * (np.abs(want + r) + np.abs(r))
+        y = B.mx4_linear(L.x, w, N, bias=L.bias if bias else None, act=T.ACTS[act], residual=L.res if residual else None)
+        T.assert_within(y, want, L.rounded(want, e), "y, %s" % act)
+
+
+@pytest.mark.parametrize("M,N,K", FORMS)
+def test_rows_apart_in_place_and_infinities_of_every_form(M, N, K):
+    """Against the same call on dense rows and buffers of its own, to the bit."""
+    L = Q.Layer("bf16", M, N, K, seed=K)
+    w, kw = B.mx4_pack(L.w), dict(bias=L.bias, act=T.ACTS["silu"])
+    z = torch.empty((M, N), dtype=L.type, device=Q.DEV)
+    plain = B.mx4_linear(L.x, w, N, residual=L.res, z_out=z, **kw)
+    ya, za = Q.apart(torch.zeros_like(plain), 5, 3), Q.apart(torch.zeros_like(plain))
+    B.mx4_linear(Q.apart(L.x), w, N, residual=Q.apart(L.res, 7, 5), y_out=ya, z_out=za, **kw)
+    assert torch.equal(ya, plain) and torch.equal(za, z)
+    assert (ya._base.view(-1)[3:].view(M, N + 5)[:, N:] == 7).all() and (za._base.view(-1)[1:].view(M, N + 3)[:, N:] == 7).all()
+    r = L.res.clone()
+    B.mx4_linear(L.x, w, N, residual=r, y_out=r, **kw)
+    assert torch.equal(r, plain)
+    r = Q.apart(L.res, 3, 1)
+    B.mx4_linear(L.x, w, N, residual=r, y_out=r, **kw)
+    assert torch.equal(r, plain) and (r._base.view(-1)[1:].view(M, N + 3)[:, N:] == 7).all()
+    x = L.x.clone()
+    x[M - 1, K - 1] = float("inf")
+    y = B.mx4_linear(x, w, N, residual=L.res, **kw)
+    assert torch.isnan(y[M - 1]).all() and torch.equal(y[:M - 1], plain[:M - 1])
+    bad = L.w.clone()
+    bad[3, 0] = float("nan")
+    y = B.mx4_linear(L.x, B.mx4_pack(bad), N, residual=L.res, **kw)
+    keep = torch.arange(N, device=Q.DEV) != 3
+    assert torch.isnan(y[:, 3]).all() and torch.equal(y[:, keep], plain[:, keep])
+
+
+# (M, N, K) whose dx, a product of M x K over N, or dw, of N x K over M, takes one of those forms; a multiple of every tile among them, and
+# more blocks of 128 to contract over than the rings hold
+GRADS = [(200, 1300, 1290), (1300, 200, 1290), (260, 1800, 1750), (1800, 700, 1750), (130, 3001, 2990), (3001, 130, 2990), (700, 2900, 3001),
+         (96, 3328, 3328), (300, 4200, 4100), (4200, 70, 4100)]
+
+
+@pytest.mark.parametrize("dtype,act,seed,M,N,K", [(("bf16", "fp16")[i % 2], ("none", "relu")[i // 2 % 2], (77, None, 78)[i % 3]) + s for i, s in enumerate(GRADS)])
+def test_gradients_of_every_form(dtype, act, seed, M, N, K):
+    L = Q.Layer(dtype, M, N, K, seed=M + N, residual=False)
+    wt, xt = B.mx4_pack(L.w, transposed=True)[1], B.mx4_pack(L.x, transposed=True)[1]
+    z = Q.values(np.random.default_rng(N), M, N, dtype) if act != "none" else None
+    kw = dict(act=T.ACTS[act], z=z, seed=Q.seed_tensor(seed))
+    (dx, ex), (dw, ew), (db, eb) = grads64(L, act, seed, z)
+    got = B.mx4_linear_backward(L.dy, wt, K, xt, dw_dtype=torch.float32, **kw)
+    T.assert_within(got[0], dx, L.rounded(dx, ex), "dx")
+    T.assert_within(got[1], dw, ew, "dw")
+    T.assert_within(got[2], db, L.rounded(db, eb), "dbias")
+    out = Q.apart(torch.zeros_like(got[0]), 5, 3)
+    r = B.mx4_linear_backward(Q.apart(L.dy), wt, K, xt, dx=out, **kw)
+    assert torch.equal(out, got[0]) and torch.equal(r[1], got[1].to(L.type)) and torch.equal(r[2], got[2])
+    assert (out._base.view(-1)[3:].view(M, K + 5)[:, K:] == 7).all()

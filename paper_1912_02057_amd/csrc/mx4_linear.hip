@@ -518,7 +518,7 @@ __global__ __launch_bounds__(128 * WM, (TileMx4<BM, BN, NS, WM>::BLOCKS * WM / 2
     for_each_index([&](auto index) { read_one(index, zero, f[0], smem); }, std::make_integer_sequence<int, READS>{});
 
     int slot = 0;
-    // STEADY: step + NS exists, so that it is loaded and no count depends on the step
+    // STEADY: step + NS exists, so that it is loaded and no count depends on the step; behind the last of those nothing is left to load
     auto one_step = [&](auto steady, int step) {
         constexpr bool STEADY = decltype(steady)::value;
         const int next = slot + 1 == L::NS ? 0 : slot + 1;
@@ -566,7 +566,6 @@ __global__ __launch_bounds__(128 * WM, (TileMx4<BM, BN, NS, WM>::BLOCKS * WM / 2
         };
         slice(zero);
         slice(one);
-        if (!STEADY && step + L::NS < nk) issue(step + L::NS, slot);
         slot = next;
     };
     int step = 0;

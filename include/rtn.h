@@ -534,7 +534,8 @@ int rtn_mx4_linear(rtn_dtype dt, const void *x, int64_t ldx, const void *x_packe
 
 /* Gradients of the layer from dy [M][N], products of packings along the dimension that each contracts over (the straight-through
  * estimator: the gradient of Q is 1), with Qt(v) = Q(v^T):
- *   dz = dy act'(z)             (z as z_out left it, not needed for RTN_ACT_NONE; fp32, not rounded; a relu's is 0 at z <= 0, whatever dy is)
+ *   dz = dy act'(z)             (z as z_out left it, not needed for RTN_ACT_NONE; fp32, not rounded; a relu's is 0 at z <= 0, whatever
+ *                               dy is; act' of gelu and silu is 0 and 1 at the infinities)
  *   dx[m][k] = sum_n Q(dz)[m][n] Qt(w)[k][n]    dw[n][k] = sum_m Qt(dz)[n][m] Qt(x)[k][m]    dbias[n] = sum_m dz[m][n]
  * seed: dz is rounded stochastically (unbiased), NULL: to nearest.  packed_t of w, x_packed_t of x: from rtn_mx4_pack.  dx (rows lddx apart)
  * and dbias have type dt, dw type dw_type (dt or RTN_F32) in dense rows; each may be NULL, not all; what only they need may be NULL then.

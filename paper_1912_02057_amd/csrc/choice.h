@@ -335,6 +335,8 @@ inline int64_t grad_blocks_per_run(int64_t M, int64_t N)
 //   1000 x 4096                         30.1   33.4   26.7   23.2               16.6     22.4
 //   2048 x 4096                                                                 24.0     24.2
 //   4096 x 4096                                       85.1   67.4               43.3     39.3
+// The two borders on columns lie between measured widths, 4096 and 8192 for blocks of 32 x 64, 2187 and 4096 for those of four waves; where exactly
+// was not measured.
 // 256 x 256 with eight waves, one block to a CU, against 128 x 256: 4096 x 4096 38.4 and 40.0, 2048 x 8192 (8192) 63.4 and 68.2, in a single
 // round; 4096 x 5120 59.7 and 52.2, 16384 x 8192 with a residual (8192) 553 and 528, over several.
 enum class Mx4Form { kSplit16, kSplit16x32, kSplit32, kSplit32x64, kSplit64, kSplit64x4, kTile128, kTile128x256, kTile256 };

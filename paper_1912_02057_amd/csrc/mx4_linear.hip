@@ -435,7 +435,9 @@ struct TileMx4 {
 // PFLOP/s against 6.5, which is what the power limit leaves).  Lane l has row l & 31 of 32, so 16 lanes have one block of rows and 16 the
 // next: a lane's scales are shifted so that both stand in the byte the instruction picks.
 // Over several rounds two blocks of 128 x 256 share a CU, so that one's epilogue passes beside the other's products: 16384 x 8192 x 8192 492 us,
-// with a residual 513 to 530 (4.1 to 4.3 PFLOP/s).  Bound by the power limit: clock 1.6 GHz while the matrix cores are busy 59 % of it.  In a
+// with a residual 513 to 537 (4.1 to 4.3 PFLOP/s).  Bound by the power limit and by waits: the clock falls to 1.4 to 1.6 GHz, and of its cycles the
+// matrix cores are busy 59 to 64 %, where a loop of products alone has none idle at 1.56 GHz.  Of 822 thousand cycles 132 are outside the loop (what
+// is left at no columns, from 8192 and 16384 of them) and 166 are in it, waiting at its counters, barriers and LDS reads.  In a
 // single round there is nothing to pass beside, and a block of 256 x 256 with eight waves loads a third less: 4096 x 4096 x 4096 36 to 38 us (38
 // to 40), 2048 x 8192 x 8192 63 (68); over several, with a residual, 553 (528) at 16384 x 8192 x 8192.
 template <class T, int BM, int BN, int NS, int WM>

@@ -44,7 +44,8 @@ __device__ __forceinline__ float load_one(const void* p, int64_t i)
 
 // Along the rows alone.  A block has 64 rows x 128 columns, a wave 16 rows, a lane 8 columns of a row: four lanes have a group, 16 read
 // 256 bytes of a row (of 16-bit values), and the maximum is over a quad of lanes.
-// 16384 x 8192 of bfloat16: 64 us, 5.3 TB/s of what is read and written; a few rows 3.6 us, the launch and one round of loads.
+// 16384 x 8192 of bfloat16: 64 us, 5.3 TB/s of what is read and written, stochastic 77, bound by the vector unit; a few rows 3.6 us, the launch
+// and one round of loads.
 template <class T, bool RANDOM>
 __global__ __launch_bounds__(256) void k_mx4_rows(Mx4PackArgs a)
 {
@@ -116,7 +117,8 @@ __device__ __forceinline__ float act_gradient(float dy, float z)
 // The sums of the columns (the bias gradient) come on the way, 64 rows each.
 // To nearest bound by memory, 4096 x 4096 of bfloat16 13.6 us, of float32 16 us (5.3 TB/s); stochastic by the vector unit, whose random numbers
 // are 40 instructions for 8 values and direction: 16384 x 8192 153 us, 93 % of its issue slots.  (Blocks of 128 x 128: 256 x 1024 17.5 us
-// instead of 7.7, for want of blocks.)
+// instead of 7.7, for want of blocks.)  Behind an activation z is read too and its slope formed for every element: relu 172 us, silu 260, gelu
+// 393 to 424, whose erfcf and expf are the most of that; at 4096 x 4096 silu 40, gelu 58.
 template <class T, int ACT, bool RANDOM>
 __global__ __launch_bounds__(128, 4) void k_mx4_both(Mx4PackArgs a)
 {

@@ -2,9 +2,11 @@
 //   y = scale x + gate (n(h) weight + bias)      u = n(y) next_weight + next_bias
 // either line alone or both in one pass.  n is x / sqrt(mean x^2 + eps) or (x - mean) / sqrt(var + eps) of a row.
 //
-// All of them are one pass over memory: a row stays in the registers of W waves (PER pieces of 8 columns a lane) from its load to its
-// stores, and statistics are sums over those registers, the variance of the centred values, in fp32.  A unit (W waves) walks
-// consecutive rows, so that the vectors of the columns are read once.
+// All of them are one pass over memory: a row stays with the lanes of W waves (PER pieces of 8 columns a lane) from its load to its
+// stores, and statistics are sums over those lanes, the variance of the centred values, in fp32.  A unit (W waves) walks
+// consecutive rows, so that the vectors of the columns are read once.  Up to 8192 columns (PER 1) all of that is in registers, but for 10 of them
+// in the gradients of both lines of a float16 layer norm in 16 waves.  Beyond (PER 2), where 16 waves leave a lane 128 registers, scratch holds 41
+// (RMS) or 50 of the forward pass of both lines and 6 to 208 of most gradients.
 #include "mx4_math.h"
 #include "rtn_kernels.h"
 
@@ -232,7 +234,9 @@ __device__ __forceinline__ void normalise_back(Cols<PER>& dn, const Cols<PER>& n
 
 // POST: y = scale x + gate (n(h) weight + bias); without it y is x.  PRE: u = n(y) next_weight + next_bias.
 // The next row is fetched while this one is worked on: a block of 16 waves has its CU to itself, and a row's sums and barriers take as long as
-// its bytes (16384 x 8192, both lines: 260 us without, 200 with: 5.4 TB/s, the rate of a large copy).
+// its bytes (16384 x 8192, both lines: 260 us without, 200 with: 5.4 TB/s, the rate of a large copy; the first line alone 168 to 185, 4.4 to 4.8
+// TB/s, the second alone 86 to 89, 6.1).  4096 x 16384: the second line alone 48 us, 5.6 TB/s, both 144 to 153, 3.6, with the registers of
+// PER 2 in scratch.
 template <class T, bool LAYER, bool POST, bool PRE, int W, int PER>
 __global__ __launch_bounds__(Unit<W>::kThreads) void k_norm(NormArgs a)
 {
@@ -283,7 +287,7 @@ __global__ __launch_bounds__(Unit<W>::kThreads) void k_norm(NormArgs a)
 //   dx = scale d,  dh = n'(h) (d gate weight),  and per unit, for k_norm_sums: sum d n(h), sum d, sum du n(y), sum du
 // A unit's rows share a row of the gate.  BIASES: the second and fourth sum are wanted.  Rows are fetched ahead as above (16384 x 8192: 411 us
 // with loads that wait for each other, 320 in flight together: 5.0 TB/s); with PER of 2 there are no registers for that, and the vectors of
-// the columns are read again for every row (4096 x 16384: 415 us, 2.3 TB/s).
+// the columns are read again for every row (4096 x 16384: 415 to 427 us, 1.9 TB/s, as a layer norm 705; the second line alone 116 to 120, 4.5 TB/s).
 template <class T, bool LAYER, bool POST, bool PRE, bool BIASES, int W, int PER>
 __global__ __launch_bounds__(Unit<W>::kThreads) void k_norm_back(NormBackArgs a)
 {
@@ -386,7 +390,8 @@ __global__ __launch_bounds__(Unit<W>::kThreads) void k_norm_back(NormBackArgs a)
 // The units' sums into the gradients of the vectors, in one order: 16 columns a block, its SLICES groups of 16 lanes share the units of one owner (a
 // row of the gate), and blockIdx.y owners out of a.owners.  With S, T the first two sums over an owner's units:
 //   dgate = S weight + T bias,  dweight += gate S,  dbias += gate T
-// Several blocks of owners leave partial sums for a second launch.
+// Several blocks of owners leave partial sums for a second launch.  Made for few owners with many units each: with a gate for every token, where
+// an owner has one, a single slice loads, and a block passes from owner to owner (16384 x 8192, RMS: 7.5 ms, beside 0.7 of k_norm_back).
 constexpr int kSumCols = 16;
 template <int SLICES>
 __global__ __launch_bounds__(SLICES * 16) void k_norm_sums(NormSumArgs a)

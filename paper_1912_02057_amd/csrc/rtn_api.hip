@@ -101,7 +101,7 @@ bool ckpt_units(int64_t M, int64_t C) { return (double)((M + 63) / 32) * (double
 bool mx4_dims(int64_t R, int64_t C) { return R >= 0 && R <= kMaxFeatures && C > 0 && C <= kMaxFeatures; }
 bool row_pitch(int64_t len, int64_t ld) { return ld >= len && ld <= (1LL << 31); }
 size_t type_bytes(rtn_dtype dt) { return dt == RTN_F32 ? 4 : 2; }
-constexpr int64_t kMaxNormed = 16384;  // columns of a row that one unit of k_norm keeps in registers
+constexpr int64_t kMaxNormed = 16384;  // columns of a row that a unit of k_norm has lanes for: 16 waves, two pieces of 8 a lane
 bool norm_dims(int64_t M, int64_t C) { return M >= 0 && M <= kMaxDim && C > 0 && C <= kMaxNormed; }
 bool known_act(rtn_act act) { return act >= RTN_ACT_NONE && act <= RTN_ACT_SILU; }
 
